@@ -209,7 +209,7 @@ def prepare(case, seed):
         if own:
             import paper_2403_09636_amd as dmc
             cfg = dmc.make_causal_config(case["hq"], case["hkv"], case["d"], case["dtype"])
-            st["causal"] = dmc.DMCCausal(cfg, len(q), case["rows"], device=DEVICE)
+            st["causal"] = dmc.DMCCausal(cfg, len(q), device=DEVICE)
         return st
 
     pieces = case.get("pieces", 1)
