@@ -333,6 +333,66 @@ dmc_status dmc_train_backward(const dmc_train_config *cfg, const void *q_dev, co
                               void *dk_dev, void *dv_dev, void *workspace_dev,
                               size_t workspace_bytes, dmc_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Plain causal attention of packed sequences (Sec. 2.1: softmax of q.k/sqrt(d),
+ * every element of q and k, no cache, no compression), forward and backward:
+ * for layers that keep their full cache, and for the uncompressed model that a
+ * DMC model is trained from and measured against.  Query i of a sequence
+ * attends to its tokens j <= i; query heads g*G .. g*G+G-1 read kv head g
+ * (num_q_heads a multiple of num_kv_heads, any G).
+ *   Tensors are [total_tokens, heads, d] in the config dtype with element
+ *   strides of the token and head axes (d contiguous), 16-byte aligned, strides
+ *   non-negative multiples of 8, token strides of q, k, v and dout below 32 MiB
+ *   (else DMC_ERR_UNSUPPORTED: the kernels address 32 tokens from one base).
+ *   Inputs may be broadcast (strides of 0); the rows of an output may not
+ *   overlap each other, nor an output any other tensor of the call.
+ *   cu_seqlens_dev: int32 [num_seqs + 1], not decreasing; sequence b holds the
+ *     tokens cu[b] .. cu[b+1]-1 (possibly none).  Values outside [0,
+ *     total_tokens] are clamped; boundaries that decrease give undefined
+ *     results, but no access outside the tensors.
+ *   Tokens outside every sequence (behind the last one) are neither read nor
+ *   written: their rows in the outputs stay as they were.
+ *   lse_dev: fp32 [total_tokens, num_q_heads] contiguous: log sum exp of every
+ *     query's scores (natural logarithm).
+ * A non-finite token of a sequence reaches the tokens after it, never those
+ * before it or other sequences.  Nothing is accumulated with atomics: results
+ * are the same from run to run.
+ * ------------------------------------------------------------------------- */
+typedef struct dmc_causal_config {
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t dtype;             /* dmc_dtype of q, k, v, out and the gradients */
+} dmc_causal_config;
+
+/* Bytes of workspace of dmc_causal_backward for up to total_tokens tokens (the
+ * rows' statistics); 0 if invalid (see dmc_last_error). */
+size_t dmc_causal_workspace_bytes(const dmc_causal_config *cfg, int32_t total_tokens);
+
+/* Forward: out_dev [total, Hq, d] and lse_dev. */
+dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q_dev,
+                              const int64_t q_strides[2], const void *k_dev,
+                              const int64_t k_strides[2], const void *v_dev,
+                              const int64_t v_strides[2], const int32_t *cu_seqlens_dev,
+                              int32_t num_seqs, int32_t total_tokens, void *out_dev,
+                              const int64_t out_strides[2], float *lse_dev, dmc_stream_t stream);
+
+/* Backward: gradients of sum(out * dout) with respect to q, k and v (summed
+ * over the query heads of a kv head's group), given the forward's inputs, out
+ * and lse.  workspace_dev: caller-owned device memory, 256-byte aligned; it
+ * carries nothing between calls, and calls that may overlap need one each. */
+dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q_dev,
+                               const int64_t q_strides[2], const void *k_dev,
+                               const int64_t k_strides[2], const void *v_dev,
+                               const int64_t v_strides[2], const int32_t *cu_seqlens_dev,
+                               int32_t num_seqs, int32_t total_tokens, const void *out_dev,
+                               const int64_t out_strides[2], const float *lse_dev,
+                               const void *dout_dev, const int64_t dout_strides[2], void *dq_dev,
+                               const int64_t dq_strides[2], void *dk_dev,
+                               const int64_t dk_strides[2], void *dv_dev,
+                               const int64_t dv_strides[2], void *workspace_dev,
+                               size_t workspace_bytes, dmc_stream_t stream);
+
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *dmc_last_error(void);
 

@@ -29,7 +29,8 @@ EXPORTS = ("dmc_cache_workspace_bytes", "dmc_cache_alloc", "dmc_cache_free", "dm
            "dmc_prefill_compress", "dmc_prefill_attend", "dmc_decode_step", "dmc_decode_step_static",
            "dmc_cache_lengths", "dmc_cache_export",
            "dmc_cache_import", "dmc_cache_check", "dmc_cache_pages_used", "dmc_last_error",
-           "dmc_train_workspace_bytes", "dmc_train_forward", "dmc_train_backward")
+           "dmc_train_workspace_bytes", "dmc_train_forward", "dmc_train_backward",
+           "dmc_causal_workspace_bytes", "dmc_causal_forward", "dmc_causal_backward")
 
 
 class CacheConfig(ctypes.Structure):
@@ -47,6 +48,12 @@ class TrainConfig(ctypes.Structure):
                 ("num_kv_heads", c_int32), ("head_dim", c_int32), ("dtype", c_int32),
                 ("decision_bias", c_float), ("temperature", c_float), ("window", c_int32),
                 ("omega_src", c_int32)]
+
+
+class CausalConfig(ctypes.Structure):
+    """Mirror of dmc_causal_config."""
+    _fields_ = [("num_q_heads", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32),
+                ("dtype", c_int32)]
 
 
 class DMCError(RuntimeError):
@@ -95,8 +102,15 @@ def _load():
     lib.dmc_train_backward.argtypes = [POINTER(TrainConfig), c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_size_t, c_void_p]
+    lib.dmc_causal_workspace_bytes.argtypes = [POINTER(CausalConfig), c_int32]
+    lib.dmc_causal_workspace_bytes.restype = c_size_t
+    packed = [c_void_p, i64p]   # a tensor [tokens, heads, d] and its strides
+    lib.dmc_causal_forward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
+                                       *packed, c_void_p, c_void_p]
+    lib.dmc_causal_backward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
+                                        *packed, c_void_p, *packed * 4, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
-        if name not in ("dmc_cache_workspace_bytes", "dmc_last_error", "dmc_train_workspace_bytes"):
+        if not name.endswith("workspace_bytes") and name != "dmc_last_error":
             getattr(lib, name).restype = c_int32
     return lib
 
@@ -330,6 +344,68 @@ def check_train_args(cfg, device, q, k, v, noise, extra=()):
     _on_device(device, **{name: t for name, t, _ in items})
 
 
+def _spans(t):
+    """Byte range of a tensor [tokens, heads, d], and of its first token in it."""
+    es = t.element_size()
+    row = ((t.shape[1] - 1) * t.stride(1) + t.shape[2]) * es
+    return t.data_ptr(), t.data_ptr() + (t.shape[0] - 1) * t.stride(0) * es + row, row
+
+
+def _packed_overlap(x, y):
+    """Whether two tensors [tokens, heads, d] share memory; views of one projection whose tokens
+    interleave without sharing any element do not."""
+    if x.numel() == 0 or y.numel() == 0:
+        return False
+    x0, x1, xr = _spans(x)
+    y0, y1, yr = _spans(y)
+    if x0 >= y1 or y0 >= x1:
+        return False
+    step = x.stride(0) * x.element_size()
+    if step != y.stride(0) * y.element_size() or step < max(xr, yr):
+        return True
+    shift = (y0 - x0) % step   # y's tokens start this far behind x's
+    return shift < xr or shift + yr > step
+
+
+def _check_packed(inputs, outputs, dtype, d):
+    """Packed tensors (name, tensor, tokens, heads): [tokens, heads, d], contiguous last dimension,
+    strides multiples of 8 elements, 16-byte aligned; an output shares memory with no other one."""
+    for name, t, tokens, heads in (*inputs, *outputs):
+        _check(name, t, dtype, (tokens, heads, d), contiguous=False, last_dim_contiguous=True,
+               stride_mult=8)
+    for i, (name, t, _, _) in enumerate(outputs):
+        for other, x, _, _ in (*inputs, *outputs[:i]):
+            if _packed_overlap(t, x):
+                _fail(f"{name} overlaps {other}")
+
+
+def _check_cu(cu_seqlens, rows=None):
+    import torch
+    _check("cu_seqlens", cu_seqlens, torch.int32, (None if rows is None else rows + 1,), align16=False)
+    if cu_seqlens.numel() < 1:
+        _fail("cu_seqlens is empty")
+
+
+def check_causal_args(cfg, device, q, k, v, cu_seqlens, out, lse, dout=None, dq=None, dk=None, dv=None):
+    """dmc_causal_forward / dmc_causal_backward (with dout and the gradients): q-shaped [T, Hq, d] and
+    k-shaped [T, Hkv, d] packed tensors, cu_seqlens int32 [sequences + 1], lse float32 [T, Hq]."""
+    import torch
+    dt = torch.float32 if cfg.dtype == DMC_FP32 else torch.bfloat16
+    Hq, Hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    _check("q", q, dt, (None, Hq, d), contiguous=False, last_dim_contiguous=True, stride_mult=8)
+    T = q.shape[0]
+    inputs = [("q", q, T, Hq), ("k", k, T, Hkv), ("v", v, T, Hkv)]
+    outputs = [("out", out, T, Hq)]
+    if dout is not None:
+        inputs += [*outputs, ("dout", dout, T, Hq)]
+        outputs = [("dq", dq, T, Hq), ("dk", dk, T, Hkv), ("dv", dv, T, Hkv)]
+    _check_packed(inputs, outputs, dt, d)
+    _check_cu(cu_seqlens)
+    _check("lse", lse, torch.float32, (T, Hq), align16=False)
+    _on_device(device, cu_seqlens=cu_seqlens, lse=lse,
+               **{name: t for name, t, _, _ in (*inputs, *outputs)})
+
+
 def _stream(stream):
     import torch
     if stream is not None:
@@ -525,4 +601,62 @@ class DMCTrainer:
                                      _ptr(noise), _ptr(out), _ptr(dout), _ptr(dalpha), _ptr(dq),
                                      _ptr(dk), _ptr(dv), self._ws, self._ws_bytes,
                                      _stream(stream)))
+        return dq, dk, dv
+
+
+def make_causal_config(num_q_heads, num_kv_heads, head_dim, dtype="bf16") -> CausalConfig:
+    """A dmc_causal_config: plain causal attention (no cache, no compression)."""
+    return CausalConfig(num_q_heads, num_kv_heads, head_dim,
+                        DMC_FP32 if dtype in ("fp32", "float32") else DMC_BF16)
+
+
+def _strides(t):
+    return (c_int64 * 2)(t.stride(0), t.stride(1))
+
+
+class DMCCausal:
+    """Plain causal attention of packed sequences (forward + backward), for layers without
+    compression; the backward's workspace, for up to max_tokens tokens, is one torch allocation."""
+
+    def __init__(self, cfg: CausalConfig, max_tokens, device="cuda"):
+        import torch
+        self.cfg = cfg
+        n = lib.dmc_causal_workspace_bytes(ctypes.byref(cfg), max_tokens)
+        if n == 0:
+            raise DMCError(DMC_ERR_INVALID_ARG, last_error())
+        self.max_tokens = max_tokens
+        self.device = _cuda_device(device)
+        self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
+        self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
+        self._ws_bytes = n
+
+    def forward(self, q, k, v, cu_seqlens, out=None, lse=None, stream=None):
+        """(out [T, Hq, d], lse [T, Hq] fp32) of q [T, Hq, d], k, v [T, Hkv, d], sequence b holding
+        the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1; other rows of out and lse stay as they
+        are."""
+        import torch
+        if out is None:
+            out = torch_empty_like(q)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse)
+        check(lib.dmc_causal_forward(ctypes.byref(self.cfg), _ptr(q), _strides(q), _ptr(k), _strides(k),
+                                     _ptr(v), _strides(v), _ptr(cu_seqlens), cu_seqlens.numel() - 1,
+                                     q.shape[0], _ptr(out), _strides(out), _ptr(lse), _stream(stream)))
+        return out, lse
+
+    def backward(self, q, k, v, cu_seqlens, out, lse, dout, dq=None, dk=None, dv=None, stream=None):
+        """(dq, dk, dv) of sum(out * dout), given the forward's inputs and outputs."""
+        dq = torch_empty_like(q) if dq is None else dq
+        dk = torch_empty_like(k) if dk is None else dk
+        dv = torch_empty_like(v) if dv is None else dv
+        check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse, dout, dq, dk, dv)
+        if q.shape[0] > self.max_tokens:
+            _fail(f"{q.shape[0]} tokens, the workspace holds {self.max_tokens}")
+        check(lib.dmc_causal_backward(ctypes.byref(self.cfg), _ptr(q), _strides(q), _ptr(k), _strides(k),
+                                      _ptr(v), _strides(v), _ptr(cu_seqlens), cu_seqlens.numel() - 1,
+                                      q.shape[0], _ptr(out), _strides(out), _ptr(lse), _ptr(dout),
+                                      _strides(dout), _ptr(dq), _strides(dq), _ptr(dk), _strides(dk),
+                                      _ptr(dv), _strides(dv), self._ws, self._ws_bytes,
+                                      _stream(stream)))
         return dq, dk, dv

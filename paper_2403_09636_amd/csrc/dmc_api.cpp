@@ -701,13 +701,13 @@ dmc_status validate_train(const dmc_train_config *c) {
 
 int train_elem_bytes(const dmc_train_config &c) { return c.dtype == DMC_FP32 ? 4 : 2; }
 
-// Device that holds a training workspace (the configuration names none).
-dmc_status workspace_device(const void *ws, int *dev) {
+// Device that holds a buffer, for entry points whose configuration names none.
+dmc_status memory_device(const void *ptr, const char *what, int *dev) {
   hipPointerAttribute_t attr{};
-  hipError_t e = hipPointerGetAttributes(&attr, ws);
-  if (e != hipSuccess) return hip_fail(e, "hipPointerGetAttributes(workspace)");
+  hipError_t e = hipPointerGetAttributes(&attr, ptr);
+  if (e != hipSuccess) return hip_fail(e, "hipPointerGetAttributes");
   if (attr.type != hipMemoryTypeDevice)
-    return fail(DMC_ERR_INVALID_ARG, "the training workspace is not device memory");
+    return fail(DMC_ERR_INVALID_ARG, "%s is not device memory", what);
   *dev = attr.device;
   return DMC_OK;
 }
@@ -780,7 +780,7 @@ dmc_status dmc_train_forward(const dmc_train_config *cfg, const void *q, const v
   p.out = out;
   p.alpha_out = alpha;
   int dev = 0;
-  st = workspace_device(ws, &dev);
+  st = memory_device(ws, "the workspace", &dev);
   if (st != DMC_OK) return st;
   DeviceGuard g(dev);   // enqueue on the workspace's device, restoring the caller's
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the workspace's device");
@@ -809,7 +809,7 @@ dmc_status dmc_train_backward(const dmc_train_config *cfg, const void *q, const 
   p.dk = dk;
   p.dv = dv;
   int dev = 0;
-  st = workspace_device(ws, &dev);
+  st = memory_device(ws, "the workspace", &dev);
   if (st != DMC_OK) return st;
   DeviceGuard g(dev);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the workspace's device");
@@ -817,6 +817,195 @@ dmc_status dmc_train_backward(const dmc_train_config *cfg, const void *q, const 
                                             cfg->num_q_heads / cfg->num_kv_heads, p,
                                             static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "training backward launch");
+  return DMC_OK;
+}
+
+// A packed tensor [rows, heads, d]: pointer and strides.  An input that is read
+// 32 tokens from one base has bounded token strides; an output's rows may not
+// overlap.
+struct Packed {
+  const char *name;
+  const void *ptr;
+  const int64_t *st;
+  int32_t heads;
+  bool bounded, output;
+};
+
+static dmc_status check_packed(const Packed &t, int64_t rows, int head_dim, int es) {
+  if (!t.ptr || !t.st) return fail(DMC_ERR_INVALID_ARG, "%s and its strides must be non-NULL", t.name);
+  if (!aligned16(t.ptr)) return fail(DMC_ERR_INVALID_ARG, "%s must be 16-byte aligned", t.name);
+  for (int i = 0; i < 2; ++i)
+    if (t.st[i] < 0 || t.st[i] % 8)
+      return fail(DMC_ERR_INVALID_ARG, "%s strides must be non-negative multiples of 8", t.name);
+  // (divided, not multiplied: strides may be anything)
+  if (t.bounded && t.st[0] >= (int64_t(1) << 25) / es)
+    return fail(DMC_ERR_UNSUPPORTED, "%s token stride must be below 32 MiB", t.name);
+  const int64_t far = (int64_t(1) << 58) / (rows + t.heads);
+  if (t.st[0] > far || t.st[1] > far)
+    return fail(DMC_ERR_INVALID_ARG, "%s strides exceed the address space", t.name);
+  if (t.output && rows > 1 && t.st[0] < t.st[1] * (t.heads - 1) + head_dim &&
+      (t.heads == 1 || t.st[1] < t.st[0] * (rows - 1) + head_dim || t.st[0] < head_dim))
+    return fail(DMC_ERR_INVALID_ARG, "the rows of %s overlap", t.name);
+  if (t.output && t.heads > 1 && t.st[1] < head_dim)
+    return fail(DMC_ERR_INVALID_ARG, "the rows of %s overlap", t.name);
+  return DMC_OK;
+}
+
+constexpr int32_t kMaxPackedTokens = 1 << 28;
+
+static dmc_status validate_causal(const dmc_causal_config *c) {
+  if (!c) return fail(DMC_ERR_INVALID_ARG, "config is NULL");
+  if (c->num_q_heads < 1 || c->num_kv_heads < 1)
+    return fail(DMC_ERR_INVALID_ARG, "head counts must be >= 1");
+  if (c->num_q_heads % c->num_kv_heads != 0)
+    return fail(DMC_ERR_INVALID_ARG, "num_q_heads (%d) must be a multiple of num_kv_heads (%d)",
+                c->num_q_heads, c->num_kv_heads);
+  if (c->num_q_heads > 4096) return fail(DMC_ERR_UNSUPPORTED, "more than 4096 query heads");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(DMC_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", c->head_dim);
+  if (c->dtype != DMC_BF16 && c->dtype != DMC_FP32)
+    return fail(DMC_ERR_INVALID_ARG, "unknown dtype %d", c->dtype);
+  return DMC_OK;
+}
+
+static dmc_status check_packed_counts(int32_t num_seqs, int32_t total) {
+  if (total < 0 || num_seqs < 0) return fail(DMC_ERR_INVALID_ARG, "token and sequence counts must be >= 0");
+  if (total > kMaxPackedTokens || num_seqs > kMaxPackedTokens)
+    return fail(DMC_ERR_UNSUPPORTED, "more than %d tokens or sequences", kMaxPackedTokens);
+  return DMC_OK;
+}
+
+static size_t causal_workspace(const dmc_causal_config &c, int32_t total) {
+  return align_up(size_t(c.num_q_heads) * (size_t(total) + 32) * 8, 256);
+}
+
+static void copy_strides(int64_t (&dst)[2], const int64_t *src) {
+  dst[0] = src[0];
+  dst[1] = src[1];
+}
+
+static void causal_params(const dmc_causal_config &c, const int32_t *cu, int32_t seqs, int32_t total, dmc::CausalParams *p) {
+  p->cu = cu;
+  p->seqs = seqs;
+  p->total = total;
+  p->hq = c.num_q_heads;
+  p->hkv = c.num_kv_heads;
+  p->stat_stride = int64_t(total) + 32;
+  p->scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(c.head_dim)));
+}
+
+// Whether a launch with one workgroup per head and tile (of at least 32 tokens) fits a grid.
+static bool causal_grid_fits(const dmc_causal_config &c, int32_t seqs, int32_t total) {
+  const int64_t tiles = int64_t(total) / 32 + seqs;
+  return tiles * c.num_q_heads <= 0x7fffffff;
+}
+
+size_t dmc_causal_workspace_bytes(const dmc_causal_config *cfg, int32_t total) {
+  if (validate_causal(cfg) != DMC_OK || check_packed_counts(0, total) != DMC_OK) return 0;
+  return causal_workspace(*cfg, total);
+}
+
+dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q, const int64_t q_strides[2],
+                              const void *k, const int64_t k_strides[2], const void *v,
+                              const int64_t v_strides[2], const int32_t *cu, int32_t num_seqs,
+                              int32_t total, void *out, const int64_t out_strides[2], float *lse,
+                              dmc_stream_t stream) {
+  dmc_status st = validate_causal(cfg);
+  if (st == DMC_OK) st = check_packed_counts(num_seqs, total);
+  if (st != DMC_OK) return st;
+  if (total == 0 || num_seqs == 0) return DMC_OK;
+  const int es = cfg->dtype == DMC_FP32 ? 4 : 2, hq = cfg->num_q_heads, hkv = cfg->num_kv_heads;
+  const Packed tensors[] = {{"q", q, q_strides, hq, true, false},
+                            {"k", k, k_strides, hkv, true, false},
+                            {"v", v, v_strides, hkv, true, false},
+                            {"out", out, out_strides, hq, false, true}};
+  for (const Packed &t : tensors) {
+    st = check_packed(t, total, cfg->head_dim, es);
+    if (st != DMC_OK) return st;
+  }
+  if (!cu || !lse) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens and lse must be non-NULL");
+  if (!causal_grid_fits(*cfg, num_seqs, total))
+    return fail(DMC_ERR_UNSUPPORTED, "too many tokens and sequences for one launch");
+  dmc::CausalParams p{};
+  causal_params(*cfg, cu, num_seqs, total, &p);
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.out = out;
+  p.lse = lse;
+  copy_strides(p.qs, q_strides);
+  copy_strides(p.ks, k_strides);
+  copy_strides(p.vs, v_strides);
+  copy_strides(p.os, out_strides);
+  int dev = 0;
+  st = memory_device(out, "out", &dev);
+  if (st != DMC_OK) return st;
+  DeviceGuard g(dev);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the tensors' device");
+  hipError_t e = dmc::launch_causal_forward(es, cfg->head_dim, p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "causal forward launch");
+  return DMC_OK;
+}
+
+dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, const int64_t q_strides[2],
+                               const void *k, const int64_t k_strides[2], const void *v,
+                               const int64_t v_strides[2], const int32_t *cu, int32_t num_seqs,
+                               int32_t total, const void *out, const int64_t out_strides[2],
+                               const float *lse, const void *dout, const int64_t dout_strides[2],
+                               void *dq, const int64_t dq_strides[2], void *dk,
+                               const int64_t dk_strides[2], void *dv, const int64_t dv_strides[2],
+                               void *ws, size_t bytes, dmc_stream_t stream) {
+  dmc_status st = validate_causal(cfg);
+  if (st == DMC_OK) st = check_packed_counts(num_seqs, total);
+  if (st != DMC_OK) return st;
+  if (total == 0 || num_seqs == 0) return DMC_OK;
+  const int es = cfg->dtype == DMC_FP32 ? 4 : 2, hq = cfg->num_q_heads, hkv = cfg->num_kv_heads;
+  const Packed tensors[] = {{"q", q, q_strides, hq, true, false},
+                            {"k", k, k_strides, hkv, true, false},
+                            {"v", v, v_strides, hkv, true, false},
+                            {"out", out, out_strides, hq, false, false},
+                            {"dout", dout, dout_strides, hq, true, false},
+                            {"dq", dq, dq_strides, hq, false, true},
+                            {"dk", dk, dk_strides, hkv, false, true},
+                            {"dv", dv, dv_strides, hkv, false, true}};
+  for (const Packed &t : tensors) {
+    st = check_packed(t, total, cfg->head_dim, es);
+    if (st != DMC_OK) return st;
+  }
+  if (!cu || !lse || !ws) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens, lse and workspace must be non-NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u)
+    return fail(DMC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (bytes < causal_workspace(*cfg, total))
+    return fail(DMC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", bytes, causal_workspace(*cfg, total));
+  if (!causal_grid_fits(*cfg, num_seqs, total))
+    return fail(DMC_ERR_UNSUPPORTED, "too many tokens and sequences for one launch");
+  dmc::CausalParams p{};
+  causal_params(*cfg, cu, num_seqs, total, &p);
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.out = const_cast<void *>(out);
+  p.lse = const_cast<float *>(lse);
+  p.dout = dout;
+  p.dq = dq;
+  p.dk = dk;
+  p.dv = dv;
+  p.stats = static_cast<float *>(ws);
+  copy_strides(p.qs, q_strides);
+  copy_strides(p.ks, k_strides);
+  copy_strides(p.vs, v_strides);
+  copy_strides(p.os, out_strides);
+  copy_strides(p.dos, dout_strides);
+  copy_strides(p.dqs, dq_strides);
+  copy_strides(p.dks, dk_strides);
+  copy_strides(p.dvs, dv_strides);
+  int dev = 0;
+  st = memory_device(ws, "the workspace", &dev);
+  if (st != DMC_OK) return st;
+  DeviceGuard g(dev);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the tensors' device");
+  hipError_t e = dmc::launch_causal_backward(es, cfg->head_dim, p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "causal backward launch");
   return DMC_OK;
 }
 

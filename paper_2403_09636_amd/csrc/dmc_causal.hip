@@ -1,0 +1,920 @@
+// gfx950 kernels of plain causal attention on packed sequences, forward and
+// backward: the attention of Sec. 2.1 of the DMC paper, for layers that keep
+// their full cache (and for the uncompressed model that DMC is measured
+// against or taught by).  Query i of a sequence attends to its tokens j <= i:
+//   S = Q K^T / sqrt(d),  P = softmax(S),  O = P V,  L = log sum exp(S)
+//   dV = P^T dO,  dS = P (dO V^T - D),  D = sum(dO O),
+//   dQ = dS K / sqrt(d),  dK = dS^T Q / sqrt(d)
+// with dK and dV summed over the query heads of a kv head's group.
+//
+// Bound by the matrix cores: 2 products forward, 7 of the backward's (dq and
+// the two halves of dk, dv each form S again; one kernel for all of them would
+// need the scores once, but either atomics, whose order changes results, or
+// more accumulators than the register file holds).
+//
+// A workgroup owns a tile of one head (128 columns in bf16, 32 in fp32) of one
+// sequence, whose other side streams past it in blocks of 32 rows.  Blocks and
+// tiles start at the sequence's first token, so that a wave's 32 columns meet
+// the diagonal in exactly one block.  Rows past a sequence's end are its last
+// row again (in bounds whatever lies behind) with weight 0.
+#include <type_traits>
+
+#include "dmc_mfma.h"
+
+namespace dmc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kTileShift = 7, kTile = 1 << kTileShift;     // bf16: tokens per workgroup
+constexpr int kTileShift32 = 5, kTile32 = 1 << kTileShift32;   // fp32
+
+// Head and tile index of a workgroup.  Heads are dealt to the XCDs (workgroup
+// i runs on XCD i mod 8) in runs where their count allows, so that a kv head's
+// keys and values stay in one L2; tiles in descending order, a sequence's
+// heaviest first.
+__device__ __forceinline__ void tile_of_block(const CausalParams &p, int ntiles, bool descending, int &head, int &idx) {
+  const int bid = blockIdx.x;
+  int rank;
+  if ((p.hq & 7) == 0) {
+    const int per = p.hq >> 3, r = bid >> 3;
+    rank = r / per;
+    head = (bid & 7) * per + r - rank * per;
+  } else {
+    rank = bid / p.hq;
+    head = bid - rank * p.hq;
+  }
+  idx = descending ? ntiles - 1 - rank : rank;
+}
+// The same for tiles of keys: heads are kv heads, tiles in ascending order.
+__device__ __forceinline__ void key_tile_of_block(const CausalParams &p, int &head, int &idx) {
+  const int bid = blockIdx.x;
+  if ((p.hkv & 7) == 0) {
+    const int per = p.hkv >> 3, r = bid >> 3;
+    idx = r / per;
+    head = (bid & 7) * per + r - idx * per;
+  } else {
+    idx = bid / p.hkv;
+    head = bid - idx * p.hkv;
+  }
+}
+
+// Row `token`, head `h` of a strided tensor of ES-byte elements.
+template <int ES>
+__device__ __forceinline__ const char *row_at(const void *base, const int64_t (&st)[2], int64_t token, int h) {
+  return static_cast<const char *>(base) + (token * st[0] + h * st[1]) * ES;
+}
+
+// ---------------------------------------------------------------------------
+// bf16.  MODE 0 = forward, 1 = dq.  One workgroup = 4 waves = 128 queries of one
+// head, a wave owning 32 (lane l: column l % 32, half l / 32).  Keys and values
+// stream through LDS in blocks of 32 tokens (direct global -> LDS transfers, a
+// ring of four blocks, three ahead):
+//   S^T[key][col] = K . Q^T;   O^T[dim][col] += V^T P^T;   dQ^T[dim][col] += K^T dS^T
+// Score row m is key pi(m) (bits 2 and 3 of m swapped), which makes a lane's
+// score registers the operand of the second product.  Forward: block kb's
+// exponentials run between the score products of block kb + 1.
+// ---------------------------------------------------------------------------
+template <int D, int MODE>
+__global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams p, int ntiles) {
+  constexpr int kSt = 4;               // ring slots
+  constexpr int KS = D / 16, NTL = D / 32, RB = D * 2, CPR = D / 8, BLK = 32 * RB;
+  constexpr int DPW = BLK / 16 / kThreads;
+  constexpr int KSW = MODE == 0 ? 0 : 2;     // dq also reads keys transposed
+  constexpr int VSW = MODE == 0 ? 1 : KSW;   // forward reads values transposed
+  static_assert(DPW >= 1 && BLK % (16 * kThreads) == 0, "block split");
+  static_assert(KS == 2 * NTL && KS > 3, "one transposed operand per score product");
+  __shared__ __align__(16) unsigned char ring0[2 * BLK], ring1[2 * BLK], ring2[2 * BLK], ring3[2 * BLK];
+  auto slot = [&](auto st_c) -> unsigned char * {
+    constexpr int S = decltype(st_c)::value;
+    if constexpr (S == 0) return ring0;
+    else if constexpr (S == 1) return ring1;
+    else if constexpr (S == 2) return ring2;
+    else return ring3;
+  };
+  int h, idx;
+  tile_of_block(p, ntiles, true, h, idx);
+  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift);
+  const int n = pt.n;
+  if (pt.tile < 0 || pt.tile * kTile >= n) return;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hb = lane >> 5;
+  const int a = pt.tile * kTile + wave * 32;    // this wave's first token
+  const int t = a + col;
+  const bool colv = t < n;
+  const int64_t token = pt.start + (colv ? t : 0);
+  const int nblk = (min(n, pt.tile * kTile + kTile) + 31) >> 5;
+  const int wave_hi = a < n ? min(a + 32, n) : 0;   // keys < wave_hi feed this wave
+  const int g = h / (p.hq / p.hkv);
+  const uint4 zero4 = make_uint4(0, 0, 0, 0);
+  const float sl2 = p.scale_log2;
+
+  uint4 qop[KS], dop[MODE == 1 ? KS : 1];
+  float Lc = 0.0f, Dc = 0.0f;
+  {
+    const char *qr = row_at<2>(p.q, p.qs, token, h);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qop[ks] = colv ? ld16(qr + ks * 32 + hb * 16) : zero4;
+    if constexpr (MODE == 1) {
+      const char *dr = row_at<2>(p.dout, p.dos, token, h), *orow = row_at<2>(p.out, p.os, token, h);
+      float part = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        dop[ks] = colv ? ld16(dr + ks * 32 + hb * 16) : zero4;
+        const uint4 ov = colv ? ld16(orow + ks * 32 + hb * 16) : zero4;
+        float df[8], of[8];
+        V16<2>::unpack(dop[ks], df);
+        V16<2>::unpack(ov, of);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part = fmaf(df[e], of[e], part);
+      }
+      Dc = part + __shfl_xor(part, 32, 64);
+      if (colv) Lc = p.lse[token * p.hq + h] * kLog2e;
+      if (colv && hb == 0) {   // for the key kernels
+        *reinterpret_cast<float2 *>(p.stats + (h * p.stat_stride + token) * 2) = make_float2(Lc, Dc);
+      }
+    }
+  }
+
+  // (the lowest finite value: no score may lie below the running maximum's start)
+  float m = lowest(), ls = 0.0f;
+  f32x16_t acc[NTL];
+#pragma unroll
+  for (int i = 0; i < NTL; ++i) acc[i] = f32x16_t{};
+
+  // This thread's chunks of a block: row, byte offset within the row, and the
+  // offset from the block's first row while the block lies inside the sequence.
+  const uint32_t kst = static_cast<uint32_t>(p.ks[0] * 2), vst = static_cast<uint32_t>(p.vs[0] * 2);
+  uint32_t krow[DPW], kchunk[DPW], vchunk[DPW];
+#pragma unroll
+  for (int i = 0; i < DPW; ++i) {
+    const int c = (i * kWaves + wave) * 64 + lane;
+    const int row = c / CPR, pc = c - row * CPR;
+    krow[i] = row;
+    kchunk[i] = (pc ^ block_swizzle<CPR, KSW>(row)) * 16;
+    vchunk[i] = (pc ^ block_swizzle<CPR, VSW>(row)) * 16;
+  }
+  const char *kbase = row_at<2>(p.k, p.ks, pt.start, g), *vbase = row_at<2>(p.v, p.vs, pt.start, g);
+  // Every call issues 2 DPW transfers per wave; those of blocks past the last
+  // one are switched off.
+  auto issue = [&](int kb, auto st_c) {
+    const bool on = kb < nblk;
+    const char *kp = uniform_ptr(kbase + int64_t(kb) * 32 * kst), *vp = uniform_ptr(vbase + int64_t(kb) * 32 * vst);
+    const uint32_t last = static_cast<uint32_t>(max(n - 1 - kb * 32, 0));   // the block's last row inside the sequence
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) {
+      unsigned char *dst = slot(st_c) + (i * kWaves + wave) * 1024;
+      const uint32_t row = min(krow[i], last);
+      dma16_s(dst, kp, row * kst + kchunk[i], on);
+      dma16_s(dst + BLK, vp, row * vst + vchunk[i], on);
+    }
+  };
+  const int krow_s = score_slot(col);
+  uint32_t kaddr[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_offset<D, KSW>(krow_s, ks, hb);
+  uint32_t traddr[NTL][2];
+  tr_offsets<D, MODE == 0 ? VSW : KSW>(lane, traddr);
+  bool left_out = false;
+
+  issue(0, std::integral_constant<int, 0>{});
+  issue(1, std::integral_constant<int, 1>{});
+  issue(2, std::integral_constant<int, 2>{});
+  if constexpr (MODE == 0) {
+    f32x16_t scn = f32x16_t{};
+    wait_vmcnt<(kSt - 2) * 2 * DPW>();   // block 0 has landed
+    ring_barrier();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      scn = mfma_32x32x16(*reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(ring0) + kaddr[ks]),
+                          qop[ks], scn);
+    auto step = [&](auto stage_c, int kb) {
+      constexpr int ST = decltype(stage_c)::value, SN = (ST + 1) % kSt;
+      wait_vmcnt<(kSt - 3) * 2 * DPW>();   // block kb + 1 has landed
+      ring_barrier();   // every wave is past step kb - 1: the slot of kb - 1 is free
+      issue(kb + kSt - 1, std::integral_constant<int, (ST + kSt - 1) % kSt>{});
+      if (kb * 32 >= wave_hi) return;
+      const bool diagonal = kb * 32 == a;
+      const char *vd = reinterpret_cast<const char *>(slot(stage_c)) + BLK;
+      const char *kn = reinterpret_cast<const char *>(slot(std::integral_constant<int, SN>{}));   // block kb + 1's keys
+      // (past the last block the next scores are not used)
+      uint4 kr[4], va[NTL][2];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kn + kaddr[i]);
+      float sv[16];
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) sv[rr] = scn[rr];
+      if (diagonal) {
+        const int tr = one_register(col - 8 * hb);
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr)
+          if (score_row(rr) > tr) sv[rr] = neg_inf();
+      }
+      float mx = fmaxf(fmaxf(sv[0], sv[1]), sv[2]);
+#pragma unroll
+      for (int rr = 3; rr < 15; rr += 2) mx = fmaxf(fmaxf(mx, sv[rr]), sv[rr + 1]);
+      mx = fmaxf(mx, sv[15]);
+      mx = max_halves(mx) * sl2;
+      if (__any(mx > m + kLazyRescale)) {
+        const float mn = fmaxf(m, mx);
+        const float f = fast_exp2(m - mn);
+        m = mn;
+        ls *= f;
+#pragma unroll
+        for (int i = 0; i < NTL; ++i) acc[i] *= f;
+      }
+      f32x16_t sc = f32x16_t{};
+      float ev[16];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 3 < KS) kr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(kn + kaddr[ks + 3]);
+        sc = mfma_32x32x16(kr[ks & 3], qop[ks], sc);
+#pragma unroll
+        for (int e = 0; e < 16 / KS; ++e) {
+          const int i = ks * (16 / KS) + e;
+          ev[i] = fast_exp2(fmaf(sv[i], sl2, -m));
+          computed_here(ev[i]);
+        }
+        va[ks >> 1][ks & 1] = tr_operand<RB>(vd, traddr[ks >> 1], ks & 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      scn = sc;
+      // P enters the value product rounded to bf16 (half a step of 2^-9 of a
+      // probability), and its sum is taken over the rounded values, so that the
+      // weights of a row add up to 1.
+      uint4 pb[2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          w[q] = cvt_pk_bf16(ev[8 * kk + 2 * q], ev[8 * kk + 2 * q + 1]);
+          ls = add_pair(w[q], ls);
+        }
+        pb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      if (diagonal) {
+#pragma unroll
+        for (int i = 0; i < NTL; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(va[i][kk]);
+      }
+#pragma unroll
+      for (int i = 0; i < NTL; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(va[i][kk], pb[kk], acc[i]);
+    };
+    // Whole rounds of four steps (a step past the last block only keeps the
+    // barriers and transfer counts in step).
+    for (int kb = 0; kb < nblk; kb += kSt) {
+      step(std::integral_constant<int, 0>{}, kb);
+      step(std::integral_constant<int, 1>{}, kb + 1);
+      step(std::integral_constant<int, 2>{}, kb + 2);
+      step(std::integral_constant<int, 3>{}, kb + 3);
+    }
+  } else {
+    auto step = [&](auto stage_c, int kb) {
+      constexpr int ST = decltype(stage_c)::value;
+      wait_vmcnt<(kSt - 2) * 2 * DPW>();   // block kb has landed
+      ring_barrier();   // block kb is in LDS for every wave; the slot of kb - 1 is free
+      issue(kb + kSt - 1, std::integral_constant<int, (ST + kSt - 1) % kSt>{});
+      if (kb * 32 >= wave_hi) return;
+      const bool diagonal = kb * 32 == a;
+      const char *kd = reinterpret_cast<const char *>(slot(stage_c));
+      const char *vd = kd + BLK;
+      // Row operands are read three products ahead (order pinned).
+      f32x16_t sc = f32x16_t{};
+      uint4 kr[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) kr[i] = *reinterpret_cast<const uint4 *>(kd + kaddr[i]);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 3 < KS) kr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(kd + kaddr[ks + 3]);
+        sc = mfma_32x32x16(kr[ks & 3], qop[ks], sc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      uint4 vr[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) vr[i] = *reinterpret_cast<const uint4 *>(vd + kaddr[i]);
+      float sv[16];
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) sv[rr] = sc[rr];
+      const int tr = one_register(diagonal ? col - 8 * hb : 32);
+      if (diagonal) {
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr)
+          if (score_row(rr) > tr) sv[rr] = neg_inf();
+      }
+      // dP^T = V . dO^T, with P = exp2(S - L) formed between its products and
+      // the transposed keys read, then dS^T = P^T (dP^T - D).
+      f32x16_t dp = f32x16_t{};
+      float pe[16];
+      uint4 kt[NTL][2];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 3 < KS) vr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(vd + kaddr[ks + 3]);
+        dp = mfma_32x32x16(vr[ks & 3], dop[ks], dp);
+#pragma unroll
+        for (int e = 0; e < 16 / KS; ++e) {
+          const int i = ks * (16 / KS) + e;
+          pe[i] = fast_exp2(fmaf(sv[i], sl2, -Lc));
+          computed_here(pe[i]);
+        }
+        kt[ks >> 1][ks & 1] = tr_operand<RB>(kd, traddr[ks >> 1], ks & 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (diagonal) {   // (a masked row's dP may be anything)
+#pragma unroll
+        for (int rr = 0; rr < 16; ++rr)
+          if (score_row(rr) > tr) dp[rr] = Dc;
+#pragma unroll
+        for (int i = 0; i < NTL; ++i)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(kt[i][kk]);
+      }
+      uint4 sb[2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r0 = 8 * kk + 2 * q;
+          w[q] = cvt_pk_bf16(pe[r0] * (dp[r0] - Dc), pe[r0 + 1] * (dp[r0 + 1] - Dc));
+        }
+        sb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+#pragma unroll
+      for (int i = 0; i < NTL; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(kt[i][kk], sb[kk], acc[i]);
+    };
+    for (int kb = 0; kb < nblk; kb += kSt) {
+      step(std::integral_constant<int, 0>{}, kb);
+      step(std::integral_constant<int, 1>{}, kb + 1);
+      step(std::integral_constant<int, 2>{}, kb + 2);
+      step(std::integral_constant<int, 3>{}, kb + 3);
+    }
+  }
+  if (__any(left_out)) {
+    const char *base = MODE == 0 ? vbase : kbase;
+    const uint32_t st = MODE == 0 ? vst : kst;
+    add_nonfinite<D, MODE != 0>(acc, [&](int i) { return base + int64_t(min(a + i, n - 1)) * st; },
+                                [&](int i) { return colv && i <= col; }, hb);
+  }
+
+  // Lane holds dims 32 i + 8 j + 4 hb .. + 4 of its column.
+  const float lt = ls + __shfl_xor(ls, 32, 64);
+  if (!colv) return;
+  char *orow = const_cast<char *>(MODE == 0 ? row_at<2>(p.out, p.os, token, h) : row_at<2>(p.dq, p.dqs, token, h));
+  float scale;
+  if constexpr (MODE == 0) {
+    scale = 1.0f / lt;
+    if (hb == 0) p.lse[token * p.hq + h] = (m + __log2f(lt)) * kLn2;
+  } else {
+    scale = sl2 / kLog2e;   // 1 / sqrt(d)
+  }
+#pragma unroll
+  for (int i = 0; i < NTL; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = cvt_pk_bf16(acc[i][4 * j] * scale, acc[i][4 * j + 1] * scale);
+      const uint32_t hi = cvt_pk_bf16(acc[i][4 * j + 2] * scale, acc[i][4 * j + 3] * scale);
+      *reinterpret_cast<uint2 *>(orow + (32 * i + 8 * j + 4 * hb) * 2) = make_uint2(lo, hi);
+    }
+}
+
+// dV (PART 1: S, P) and dK (PART 2: S, dP, dS) of 128 keys of one kv head, 32
+// per wave (its K and V rows are operands in registers); the queries of the
+// group's heads, one head after another, stream through LDS in blocks of 32
+// rows with their statistics (a ring of three blocks, two ahead).  In two parts,
+// each holds half the accumulators and runs two waves per SIMD.
+//   S[row][key] = Q . K^T,  dP[row][key] = dO . V^T   (rows pi-permuted)
+//   dV^T[dim][key] += dO^T P,  dK^T[dim][key] += Q^T dS
+template <int D, int PART>
+__global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p) {
+  static_assert(PART == 1 || PART == 2, "dV part or dK part");
+  constexpr int kSt = 3;
+  constexpr int KS = D / 16, NTL = D / 32, RB = D * 2, CPR = D / 8, BLK = 32 * RB;
+  constexpr int DPW = BLK / 16 / kThreads;
+  // One ring slot: query rows, dO rows, then per wave its own copy of the
+  // block's statistics (32 L, then 32 D).
+  constexpr int SLOT = 2 * BLK + kWaves * 256;
+  static_assert(DPW >= 1, "block split");
+  __shared__ __align__(16) unsigned char ring0[SLOT], ring1[SLOT], ring2[SLOT];
+  auto slot = [&](auto st_c) -> unsigned char * {
+    constexpr int S = decltype(st_c)::value;
+    if constexpr (S == 0) return ring0;
+    else if constexpr (S == 1) return ring1;
+    else return ring2;
+  };
+  int g, idx;
+  key_tile_of_block(p, g, idx);
+  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift);
+  const int n = pt.n;
+  if (pt.tile < 0 || pt.tile * kTile >= n) return;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hb = lane >> 5;
+  const int s0 = pt.tile * kTile + wave * 32;        // this wave's first key
+  const int js = s0 + col;                           // this lane's key (column)
+  const bool kv_ok = js < n;
+  const uint4 zero4 = make_uint4(0, 0, 0, 0);
+  const float sl2 = p.scale_log2;
+  const int G = p.hq / p.hkv;
+
+  uint4 kop[KS], vop[PART == 2 ? KS : 1];
+  {
+    const int64_t token = pt.start + (kv_ok ? js : 0);
+    const char *kr = row_at<2>(p.k, p.ks, token, g), *vr = row_at<2>(p.v, p.vs, token, g);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      kop[ks] = kv_ok ? ld16(kr + ks * 32 + hb * 16) : zero4;
+      if constexpr (PART == 2) vop[ks] = kv_ok ? ld16(vr + ks * 32 + hb * 16) : zero4;
+    }
+  }
+
+  const int qb0 = pt.tile * (kTile / 32), qb1 = (n + 31) >> 5;   // row blocks that see the tile
+  const int per_head = qb1 - qb0, nblk = G * per_head;
+  const uint32_t qst = static_cast<uint32_t>(p.qs[0] * 2), dst_ = static_cast<uint32_t>(p.dos[0] * 2);
+  uint32_t qrow[DPW], qchunk[DPW];
+#pragma unroll
+  for (int i = 0; i < DPW; ++i) {
+    const int c = (i * kWaves + wave) * 64 + lane;
+    const int row = c / CPR, pc = c - row * CPR;
+    qrow[i] = row;
+    qchunk[i] = (pc ^ dual_swizzle<CPR>(row)) * 16;
+  }
+  // Statistics, one 4-byte transfer per wave into its own area: lanes 0..31 the
+  // rows' L, lanes 32..63 their D (rows past the sequence: the next one's, or
+  // the workspace's padding, not used).
+  const uint32_t soff = uint32_t(col) * 8 + uint32_t(hb) * 4;
+  int ih = g * G, iq = qb0;   // next block to issue: head, row block
+  // Every call issues 2 DPW + 1 transfers per wave; those past the last block
+  // are switched off.
+  auto issue = [&](auto st_c) {
+    const bool on = ih < g * G + G;
+    const int hh = on ? ih : g * G;
+    unsigned char *dst = slot(st_c);
+    const char *qp = uniform_ptr(row_at<2>(p.q, p.qs, pt.start + iq * 32, hh));
+    const char *dp = uniform_ptr(row_at<2>(p.dout, p.dos, pt.start + iq * 32, hh));
+    const char *sp = uniform_ptr(reinterpret_cast<const char *>(p.stats + (hh * p.stat_stride + pt.start + iq * 32) * 2));
+    const uint32_t last = static_cast<uint32_t>(n - 1 - iq * 32);   // the block's last row inside the sequence
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) {
+      unsigned char *cdst = dst + (i * kWaves + wave) * 1024;
+      const uint32_t row = min(qrow[i], last);
+      dma16_s(cdst, qp, row * qst + qchunk[i], on);
+      dma16_s(cdst + BLK, dp, row * dst_ + qchunk[i], on);
+    }
+    dma_so<kCachePolicyDefault, 4>(dst + 2 * BLK + wave * 256, sp, soff, on);
+    if (on && ++iq == qb1) {
+      iq = qb0;
+      ++ih;
+    }
+  };
+  const int qrow_s = score_slot(col);
+  uint32_t raddr[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) raddr[ks] = row_offset<D, 2>(qrow_s, ks, hb);
+  uint32_t traddr[NTL][2];
+  tr_offsets<D, 2>(lane, traddr);
+
+  f32x16_t acc[NTL];
+#pragma unroll
+  for (int i = 0; i < NTL; ++i) acc[i] = f32x16_t{};
+  bool left_out = false;
+  int cq = qb0;   // row block of the next step
+
+  auto step = [&](auto stage_c, int kb) {
+    constexpr int ST = decltype(stage_c)::value;
+    wait_vmcnt<(kSt - 2) * (2 * DPW + 1)>();   // block kb has landed
+    ring_barrier();   // block kb is in LDS for every wave; the slot of kb - 1 is free
+    issue(std::integral_constant<int, (ST + kSt - 1) % kSt>{});
+    const int rb = cq * 32;                    // first row of the block
+    if (++cq == qb1) cq = qb0;
+    if (kb >= nblk || rb < s0) return;         // past the last block, or every row precedes this wave's keys
+    const char *qd = reinterpret_cast<const char *>(slot(stage_c));
+    const char *dd = qd + BLK;
+    const bool masked = rb == s0 || rb + 32 > n;   // the diagonal, or rows past the sequence
+    // Register 8 kk + q of this lane: row rb + 16 kk + 8 hb + q.
+    const float *sl = reinterpret_cast<const float *>(qd + 2 * BLK + wave * 256) + 8 * hb;
+    float Lr[16], Dr[PART == 2 ? 16 : 1];
+    auto statistics = [&](const float *e8, float *x) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float4 f = *reinterpret_cast<const float4 *>(e8 + 16 * (c >> 1) + 4 * (c & 1));
+        x[4 * c + 0] = f.x; x[4 * c + 1] = f.y; x[4 * c + 2] = f.z; x[4 * c + 3] = f.w;
+      }
+    };
+    f32x16_t sc = f32x16_t{};
+    uint4 qr[4];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) qr[i] = *reinterpret_cast<const uint4 *>(qd + raddr[i]);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks + 3 < KS) qr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(qd + raddr[ks + 3]);
+      sc = mfma_32x32x16(qr[ks & 3], kop[ks], sc);
+      if (ks == 0) statistics(sl, Lr);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float pe[16];
+    uint4 xt[NTL][2];   // transposed rows of the last product: dO (dV), Q (dK)
+    const char *xd = PART == 1 ? dd : qd;
+    f32x16_t dp = f32x16_t{};
+    if constexpr (PART == 2) {
+      statistics(sl + 32, Dr);
+      uint4 dr[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) dr[i] = *reinterpret_cast<const uint4 *>(dd + raddr[i]);
+      // dP's products with P's exponentials between them (order pinned).
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if (ks + 3 < KS) dr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(dd + raddr[ks + 3]);
+        dp = mfma_32x32x16(dr[ks & 3], vop[ks], dp);
+#pragma unroll
+        for (int e = 0; e < 16 / KS; ++e) {
+          const int i = ks * (16 / KS) + e;
+          pe[i] = fast_exp2(fmaf(sc[i], sl2, -Lr[i]));
+          computed_here(pe[i]);
+        }
+        xt[ks >> 1][ks & 1] = tr_operand<RB>(xd, traddr[ks >> 1], ks & 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NTL; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) xt[i][kk] = tr_operand<RB>(xd, traddr[i], kk);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) pe[i] = fast_exp2(fmaf(sc[i], sl2, -Lr[i]));
+    }
+    if (masked) {
+      // row 16 kk + 8 hb + q is seen from key col on, and up to the sequence's end
+      const int from = one_register(rb == s0 ? col - 8 * hb : -8), to = one_register(n - rb - 8 * hb);
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) {
+        const bool vis = score_row(rr) >= from && score_row(rr) < to;
+        pe[rr] = vis ? pe[rr] : 0.0f;
+        if constexpr (PART == 2) dp[rr] = vis ? dp[rr] - Dr[rr] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < NTL; ++i)
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(xt[i][kk]);
+    } else if constexpr (PART == 2) {
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) dp[rr] -= Dr[rr];
+    }
+    uint4 wb[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = 8 * kk + 2 * q;
+        if constexpr (PART == 1) w[q] = cvt_pk_bf16(pe[i], pe[i + 1]);
+        else w[q] = cvt_pk_bf16(pe[i] * dp[i], pe[i + 1] * dp[i + 1]);
+      }
+      wb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < NTL; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(xt[i][kk], wb[kk], acc[i]);
+  };
+
+  issue(std::integral_constant<int, 0>{});
+  issue(std::integral_constant<int, 1>{});
+  // Whole rounds of three steps (a step past the last block only keeps the
+  // barriers and transfer counts in step).
+  for (int kb = 0; kb < nblk; kb += kSt) {
+    step(std::integral_constant<int, 0>{}, kb);
+    step(std::integral_constant<int, 1>{}, kb + 1);
+    step(std::integral_constant<int, 2>{}, kb + 2);
+  }
+  if (__any(left_out)) {   // the masked blocks of every head again
+    const void *base = PART == 1 ? p.dout : p.q;
+    for (int hh = g * G; hh < g * G + G; ++hh)
+      for (int qb = qb0; qb < qb1; ++qb) {
+        const int rb = qb * 32;
+        if (rb < s0 || (rb != s0 && rb + 32 <= n)) continue;
+        add_nonfinite<D, PART == 2>(
+            acc,
+            [&](int i) { return row_at<2>(base, PART == 1 ? p.dos : p.qs, pt.start + min(rb + i, n - 1), hh); },
+            [&](int i) { return kv_ok && rb + i >= js && rb + i < n; }, hb);
+      }
+  }
+  if (!kv_ok) return;
+  const float scale = PART == 1 ? 1.0f : sl2 / kLog2e;
+  char *orow = const_cast<char *>(PART == 1 ? row_at<2>(p.dv, p.dvs, pt.start + js, g)
+                                            : row_at<2>(p.dk, p.dks, pt.start + js, g));
+#pragma unroll
+  for (int i = 0; i < NTL; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = cvt_pk_bf16(acc[i][4 * j] * scale, acc[i][4 * j + 1] * scale);
+      const uint32_t hi = cvt_pk_bf16(acc[i][4 * j + 2] * scale, acc[i][4 * j + 3] * scale);
+      *reinterpret_cast<uint2 *>(orow + (32 * i + 8 * j + 4 * hb) * 2) = make_uint2(lo, hi);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// fp32, on v_mfma_f32_32x32x2_f32 (operand forms: F32).  One workgroup = 32
+// columns of one head -- queries in the forward and dq, keys in the key kernel
+// -- whose four waves share the column operands and take every fourth 32-row
+// block of the other side straight from global memory; their results meet in
+// LDS.  Bound by the fp32 matrix rate and by the longest tile's chain of blocks.
+// ---------------------------------------------------------------------------
+template <int D, int MODE>
+__global__ __launch_bounds__(kThreads) void causal_query_f32_kernel(CausalParams p, int ntiles) {
+  using F = F32<D>;
+  constexpr int NT = F::NT;
+  __shared__ __align__(16) float s_acc[F::kArea];
+  __shared__ float s_m[kWaves * 32], s_l[kWaves * 32];
+  int h, idx;
+  tile_of_block(p, ntiles, true, h, idx);
+  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift32);
+  const int n = pt.n, a = pt.tile * kTile32;
+  if (pt.tile < 0 || a >= n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hb = lane >> 5;
+  const int g = h / (p.hq / p.hkv);
+  const int t = a + col;
+  const bool colv = t < n;
+  const int64_t token = pt.start + (colv ? t : 0);
+  const int nblk = pt.tile + 1;   // the last one holds the diagonal
+
+  auto col_row = [&](const void *base, const int64_t (&st)[2], int c) -> const float * {
+    return a + c < n ? reinterpret_cast<const float *>(row_at<4>(base, st, pt.start + a + c, h)) : nullptr;
+  };
+  F::stage(s_acc, [&](int c) { return col_row(p.q, p.qs, c); }, false);
+  if constexpr (MODE == 1) F::stage(s_acc + 32 * F::kCol, [&](int c) { return col_row(p.dout, p.dos, c); }, false);
+  __syncthreads();
+  const float *qs = F::staged(s_acc, lane), *dos = F::staged(s_acc + (MODE == 1 ? 32 * F::kCol : 0), lane);
+  typename F::f4_t kr[F::NJ], vr[MODE == 1 ? F::NJ : 1];
+  float Lc = 0.0f, Dc = 0.0f;
+  if constexpr (MODE == 1) {
+    if (colv) {
+      F::load_row(kr, col_row(p.out, p.os, col), hb);
+      Lc = p.lse[token * p.hq + h] * kLog2e;
+#pragma unroll
+      for (int j = 0; j < F::NJ; ++j) {
+        const typename F::f4_t d4 = *reinterpret_cast<const typename F::f4_t *>(dos + 8 * j);
+        float part = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part = fmaf(d4[i], kr[j][i], part);
+        Dc += part;
+      }
+    }
+    Dc += __shfl_xor(Dc, 32, 64);
+    if (tid < 32 && colv)
+      *reinterpret_cast<float2 *>(p.stats + (h * p.stat_stride + token) * 2) = make_float2(Lc, Dc);
+  }
+  float m = lowest(), ls = 0.0f;
+  f32x16_t acc[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) acc[i] = f32x16_t{};
+  auto key_at = [&](int s) { return reinterpret_cast<const float *>(row_at<4>(p.k, p.ks, pt.start + min(s, n - 1), g)); };
+  auto value_at = [&](int s) { return reinterpret_cast<const float *>(row_at<4>(p.v, p.vs, pt.start + min(s, n - 1), g)); };
+  F::load_row(kr, key_at(wave * 32 + col), hb);
+  bool left_out = false;
+  auto block = [&](int kb, auto last_c) {
+    constexpr bool LAST = decltype(last_c)::value;   // the diagonal's block
+    if constexpr (MODE == 1) F::load_row(vr, value_at(kb * 32 + col), hb);   // lands while the scores run
+    typename F::Cols xc;
+    auto x_row = [&](int i) { return MODE == 0 ? value_at(kb * 32 + i) : key_at(kb * 32 + i); };
+    xc.load(x_row, 0, lane);
+    const f32x16_t sc = F::dots(kr, qs);
+    f32x16_t dp = f32x16_t{};
+    if constexpr (MODE == 1) dp = F::dots(vr, dos);
+    if (!LAST) F::load_row(kr, key_at((kb + kWaves) * 32 + col), hb);
+    float x[16];
+    if constexpr (MODE == 0) {
+      float mx = neg_inf();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = sc[r] * p.scale_log2;
+        if (LAST && F::row(r, hb) > col) x[r] = neg_inf();
+        mx = fmaxf(mx, x[r]);
+      }
+      const float mn = fmaxf(m, max_halves(mx));
+      const float f = fast_exp2(m - mn);
+      m = mn;
+      ls *= f;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) acc[i] *= f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = fast_exp2(x[r] - mn);
+        ls += x[r];
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        x[r] = LAST && F::row(r, hb) > col ? 0.0f : fast_exp2(sc[r] * p.scale_log2 - Lc) * (dp[r] - Dc);
+    }
+    left_out |= F::template add_rows<LAST>(acc, xc, x_row, x, lane);
+  };
+#pragma unroll 1
+  for (int kb = wave; kb < nblk - 1; kb += kWaves) block(kb, std::false_type{});
+  if (((nblk - 1) & (kWaves - 1)) == wave) block(nblk - 1, std::true_type{});
+  if (__any(left_out))
+    F::add_nonfinite(acc, [&](int i) { return MODE == 0 ? value_at(a + i) : key_at(a + i); },
+                     [&](int i) { return colv && i <= col; }, lane);
+  if constexpr (MODE == 0) {
+    ls += __shfl_xor(ls, 32, 64);
+    if (hb == 0) {
+      s_m[wave * 32 + col] = m;
+      s_l[wave * 32 + col] = ls;
+    }
+    __syncthreads();   // (and the staged rows' last use)
+    float M = s_m[col], L = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w * 32 + col]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) L += s_l[w * 32 + col] * fast_exp2(s_m[w * 32 + col] - M);
+    const float f = fast_exp2(m - M) / L;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] *= f;
+    if (tid < 32 && colv) p.lse[token * p.hq + h] = (M + __log2f(L)) * kLn2;
+  } else {
+    const float scale = p.scale_log2 / kLog2e;   // 1 / sqrt(d)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] *= scale;
+    __syncthreads();   // the staged rows' last use
+  }
+  F::put(s_acc, wave, lane, acc);
+  __syncthreads();
+  for (int i = tid; i < 32 * D / 4; i += kThreads) {
+    const int c = i / (D / 4), e = i % (D / 4);
+    if (a + c >= n) continue;
+    const char *o = MODE == 0 ? row_at<4>(p.out, p.os, pt.start + a + c, h) : row_at<4>(p.dq, p.dqs, pt.start + a + c, h);
+    *reinterpret_cast<typename F::f4_t *>(const_cast<char *>(o) + 16 * e) = F::sum(s_acc, c, e);
+  }
+}
+
+// dK and dV of 32 keys.  PART 0 computes both; at d = 128, where both sets of
+// operands exceed the register file, PART 1 is dV alone and PART 2 dK.
+template <int D, int PART>
+__global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p) {
+  using F = F32<D>;
+  constexpr int NT = F::NT;
+  constexpr bool DV = PART != 2, DK = PART != 1;
+  __shared__ __align__(16) float s_acc[F::kArea];
+  int g, idx;
+  key_tile_of_block(p, g, idx);
+  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift32);
+  const int n = pt.n, s0 = pt.tile * kTile32;
+  if (pt.tile < 0 || s0 >= n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hb = lane >> 5;
+  const int G = p.hq / p.hkv;
+  const int js = s0 + col;   // this lane's key
+  const bool kv_ok = js < n;
+  const int qb0 = pt.tile, per_head = ((n + 31) >> 5) - qb0, nblk = G * per_head;   // the first of a head holds the diagonal
+
+  auto key_row = [&](const void *base, const int64_t (&st)[2], int c) -> const float * {
+    return s0 + c < n ? reinterpret_cast<const float *>(row_at<4>(base, st, pt.start + s0 + c, g)) : nullptr;
+  };
+  F::stage(s_acc, [&](int c) { return key_row(p.k, p.ks, c); }, false);
+  if constexpr (DK) F::stage(s_acc + 32 * F::kCol, [&](int c) { return key_row(p.v, p.vs, c); }, false);
+  __syncthreads();
+  const float *kst = F::staged(s_acc, lane), *vst = F::staged(s_acc + (DK ? 32 * F::kCol : 0), lane);
+  typename F::f4_t qr[F::NJ], dor[DK ? F::NJ : 1];
+  f32x16_t dk[DK ? NT : 1], dv[DV ? NT : 1];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    if constexpr (DK) dk[i] = f32x16_t{};
+    if constexpr (DV) dv[i] = f32x16_t{};
+  }
+  // block i: head, first row
+  auto at = [&](int i, int &hh, int &rb) {
+    const int q = i / per_head;
+    hh = g * G + q;
+    rb = (qb0 + i - q * per_head) * 32;
+  };
+  auto q_at = [&](int hh, int r) { return reinterpret_cast<const float *>(row_at<4>(p.q, p.qs, pt.start + min(r, n - 1), hh)); };
+  auto do_at = [&](int hh, int r) { return reinterpret_cast<const float *>(row_at<4>(p.dout, p.dos, pt.start + min(r, n - 1), hh)); };
+  int hh, rb;
+  at(min(wave, nblk - 1), hh, rb);
+  F::load_row(qr, q_at(hh, rb + col), hb);
+  bool out_v = false, out_k = false;
+#pragma unroll 1
+  for (int i = wave; i < nblk; i += kWaves) {
+    at(i, hh, rb);
+    const bool masked = rb == s0 || rb + 32 > n;
+    if constexpr (DK) F::load_row(dor, do_at(hh, rb + col), hb);   // lands while the scores run
+    typename F::Cols qc, oc;
+    auto q_row = [&](int r) { return q_at(hh, rb + r); };
+    auto do_row = [&](int r) { return do_at(hh, rb + r); };
+    if constexpr (DV) oc.load(do_row, 0, lane);
+    if constexpr (DK) qc.load(q_row, 0, lane);
+    float Lr[16], Dr[16];
+    const float *st = p.stats + (hh * p.stat_stride + pt.start + rb) * 2;   // (padded by 32 rows)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float x[8];
+      load4(st + (8 * c + 4 * hb) * 2, x);
+      load4(st + (8 * c + 4 * hb) * 2 + 4, x + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        Lr[4 * c + e] = x[2 * e];
+        Dr[4 * c + e] = x[2 * e + 1];
+      }
+    }
+    const f32x16_t sc = F::dots(qr, kst);
+    f32x16_t dp = f32x16_t{};
+    if constexpr (DK) dp = F::dots(dor, vst);
+    int hn, rn;
+    at(min(i + kWaves, nblk - 1), hn, rn);
+    F::load_row(qr, q_at(hn, rn + col), hb);
+    float pv[16], ds[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = rb + F::row(r, hb);
+      const bool vis = row >= js && row < n;
+      pv[r] = vis ? fast_exp2(sc[r] * p.scale_log2 - Lr[r]) : 0.0f;
+      if constexpr (DK) ds[r] = vis ? pv[r] * (dp[r] - Dr[r]) : 0.0f;
+    }
+    if constexpr (DV) out_v |= F::template add_rows<true>(dv, oc, do_row, pv, lane, masked);
+    if constexpr (DK) out_k |= F::template add_rows<true>(dk, qc, q_row, ds, lane, masked);
+  }
+  if (__any(out_v || out_k)) {
+    for (int i = wave; i < nblk; i += kWaves) {
+      at(i, hh, rb);
+      if (!(rb == s0 || rb + 32 > n)) continue;
+      auto sees = [&](int r) { return kv_ok && rb + r >= js && rb + r < n; };
+      if constexpr (DV) F::add_nonfinite(dv, [&](int r) { return do_at(hh, rb + r); }, sees, lane);
+      if constexpr (DK) F::add_nonfinite(dk, [&](int r) { return q_at(hh, rb + r); }, sees, lane);
+    }
+  }
+  auto emit = [&](void *out, const int64_t (&st)[2]) {   // the merged rows of the tile's keys
+    __syncthreads();
+    for (int i = tid; i < 32 * D / 4; i += kThreads) {
+      const int c = i / (D / 4), e = i % (D / 4);
+      if (s0 + c < n)
+        *reinterpret_cast<typename F::f4_t *>(const_cast<char *>(row_at<4>(out, st, pt.start + s0 + c, g)) + 16 * e) =
+            F::sum(s_acc, c, e);
+    }
+  };
+  __syncthreads();   // the staged rows' last use
+  if constexpr (DV) {
+    F::put(s_acc, wave, lane, dv);
+    emit(p.dv, p.dvs);
+    if constexpr (DK) __syncthreads();   // the merge area is reused
+  }
+  if constexpr (DK) {
+    const float scale = p.scale_log2 / kLog2e;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) dk[i] *= scale;
+    F::put(s_acc, wave, lane, dk);
+    emit(p.dk, p.dks);
+  }
+}
+
+template <int D>
+hipError_t causal_forward(int elem_bytes, const CausalParams &p, hipStream_t s) {
+  const int shift = elem_bytes == 2 ? kTileShift : kTileShift32;
+  const int ntiles = (p.total >> shift) + p.seqs;
+  const int64_t blocks = int64_t(ntiles) * p.hq;
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (elem_bytes == 2)
+    hipLaunchKernelGGL((causal_query_kernel<D, 0>), dim3(unsigned(blocks)), dim3(kThreads), 0, s, p, ntiles);
+  else
+    hipLaunchKernelGGL((causal_query_f32_kernel<D, 0>), dim3(unsigned(blocks)), dim3(kThreads), 0, s, p, ntiles);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t causal_backward(int elem_bytes, const CausalParams &p, hipStream_t s) {
+  const int shift = elem_bytes == 2 ? kTileShift : kTileShift32;
+  const int ntiles = (p.total >> shift) + p.seqs;
+  if (int64_t(ntiles) * p.hq > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const dim3 queries(unsigned(ntiles) * p.hq), keys(unsigned(ntiles) * p.hkv), threads(kThreads);
+  if (elem_bytes == 2) {
+    hipLaunchKernelGGL((causal_query_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
+    hipLaunchKernelGGL((causal_key_kernel<D, 1>), keys, threads, 0, s, p);
+    hipLaunchKernelGGL((causal_key_kernel<D, 2>), keys, threads, 0, s, p);
+  } else {
+    hipLaunchKernelGGL((causal_query_f32_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
+    if constexpr (D == 64) {
+      hipLaunchKernelGGL((causal_key_f32_kernel<D, 0>), keys, threads, 0, s, p);
+    } else {
+      hipLaunchKernelGGL((causal_key_f32_kernel<D, 1>), keys, threads, 0, s, p);
+      hipLaunchKernelGGL((causal_key_f32_kernel<D, 2>), keys, threads, 0, s, p);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s) {
+  return head_dim == 128 ? causal_forward<128>(elem_bytes, p, s) : causal_forward<64>(elem_bytes, p, s);
+}
+
+hipError_t launch_causal_backward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s) {
+  return head_dim == 128 ? causal_backward<128>(elem_bytes, p, s) : causal_backward<64>(elem_bytes, p, s);
+}
+
+}  // namespace dmc

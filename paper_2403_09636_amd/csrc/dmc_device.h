@@ -225,5 +225,38 @@ __device__ __forceinline__ int clamp_prompt_len(const int32_t *prompt_lens, int 
   return x < 0 ? 0 : (x > n ? n : x);
 }
 
+// Packed sequences: sequence b holds the tokens cu[b] .. cu[b + 1] - 1, both
+// clamped to [0, total] (so that no boundaries, whatever they hold, lead out of
+// the tensors).  Work is laid out in tiles of 2^shift tokens; sequence b's first
+// tile has the index first_tile, and as those never overlap for boundaries that
+// do not decrease, total / 2^shift + sequences tiles hold every token.
+__device__ __forceinline__ int clamp_token(int x, int total) { return x < 0 ? 0 : (x > total ? total : x); }
+__device__ __forceinline__ int first_tile(const int32_t *cu, int total, int b, int shift) {
+  return (clamp_token(cu[b], total) >> shift) + b;
+}
+struct PackedTile {
+  int seq, start, n, tile;   // sequence, its first token and length, the tile within it (< 0: none)
+};
+// The sequence and tile of tile index idx, by the whole wave (64 candidates a step).
+__device__ __forceinline__ PackedTile packed_tile(const int32_t *cu, int seqs, int total, int idx, int shift) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = seqs;   // the answer lies in [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 63) >> 6, i = lo + lane * step;
+    const bool le = lane == 0 || (i < lo + n && first_tile(cu, total, i, shift) <= idx);
+    const int k = 63 - __clzll(static_cast<long long>(__ballot(le)));
+    const int end = lo + n;
+    lo += k * step;
+    n = min(step, end - lo);
+  }
+  PackedTile t;
+  t.seq = __builtin_amdgcn_readfirstlane(lo);
+  t.start = __builtin_amdgcn_readfirstlane(clamp_token(cu[t.seq], total));
+  const int end = __builtin_amdgcn_readfirstlane(clamp_token(cu[t.seq + 1], total));
+  t.n = end > t.start ? end - t.start : 0;
+  t.tile = idx - ((t.start >> shift) + t.seq);
+  return t;
+}
+
 }  // namespace
 }  // namespace dmc

@@ -260,6 +260,22 @@ hipError_t launch_train_forward(int elem_bytes, int head_dim, int group, const T
 hipError_t launch_train_backward(int elem_bytes, int head_dim, int group, const TrainParams &p,
                                  hipStream_t s);
 
+// Causal attention of packed sequences (no cache, no compression).  Tensors are
+// [total, heads, d] with element strides of the token and head axes.
+struct CausalParams {
+  const void *q, *k, *v, *dout;
+  void *out, *dq, *dk, *dv;      // out: written by the forward, read by the backward
+  int64_t qs[2], ks[2], vs[2], os[2], dos[2], dqs[2], dks[2], dvs[2];
+  float *lse;                    // [total, hq], natural logarithm
+  const int32_t *cu;             // [seqs + 1]
+  float *stats;                  // workspace: [hq][stat_stride][2], per row log2-sum-exp, sum(dout * out)
+  int64_t stat_stride;           // total + 32
+  float scale_log2;              // log2(e) / sqrt(d)
+  int32_t seqs, total, hq, hkv;
+};
+hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
+hipError_t launch_causal_backward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
+
 // Launchers (return hipGetLastError() after enqueueing).
 hipError_t launch_reset(const ResetParams &p, hipStream_t s);
 hipError_t launch_fill_u8(void *p, size_t bytes, hipStream_t s);

@@ -205,6 +205,90 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float acc) {
                                          __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc, false);
 }
 
+// Swizzle of a block's rows: 0 key (row reads), 1 value (transposed reads),
+// 2 dual (both).
+template <int CPR, int SW>
+__device__ __forceinline__ int block_swizzle(int row) {
+  return SW == 0 ? k_swizzle<CPR>(row) : SW == 1 ? v_swizzle<CPR>(row) : dual_swizzle<CPR>(row);
+}
+
+// Transposed operand: A or B slice "rows 16 kk + 8 half + 0..7 of dim 32 t +
+// col" of a 32-row block (vaddr[t][h]: offsets of the two 4-row halves).
+template <int RB>
+__device__ __forceinline__ uint4 tr_operand(const char *blk, const uint32_t (&vaddr)[2], int kk) {
+  const uint2 h0 = ds_read_tr16(blk + vaddr[0] + 16 * kk * RB);
+  const uint2 h1 = ds_read_tr16(blk + vaddr[1] + 16 * kk * RB);
+  return make_uint4(h0.x, h0.y, h1.x, h1.y);
+}
+
+// Per-lane offsets of the transposed reads (per 32-dim tile and 4-row half)
+// for a block stored with swizzle SW (1 or 2): a 16-lane group points at
+// four 8-byte pieces of each of 4 rows.
+template <int D, int SW>
+__device__ __forceinline__ void tr_offsets(int lane, uint32_t (&vaddr)[D / 32][2]) {
+  constexpr int RB = D * 2, CPR = D / 8;
+  const int g16 = lane >> 4, r16 = lane & 15;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int row = 8 * (g16 >> 1) + 4 * h + (r16 >> 2);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      const int lc = 4 * t + 2 * (g16 & 1) + ((r16 & 3) >> 1);
+      vaddr[t][h] = row * RB + ((lc ^ block_swizzle<CPR, SW>(row)) * 16) + (r16 & 1) * 8;
+    }
+  }
+}
+
+// Row-read offsets: 16 bytes (dims 16 ks + 8 half .. + 8) of row `row` of a
+// block stored with swizzle SW.
+template <int D, int SW>
+__device__ __forceinline__ uint32_t row_offset(int row, int ks, int hb) {
+  constexpr int RB = D * 2, CPR = D / 8;
+  return row * RB + (((2 * ks + hb) ^ block_swizzle<CPR, SW>(row)) * 16);
+}
+
+// Whether a float is finite; the packed bf16 pair's halves likewise, as masks
+// (0xffff per half that is).
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+  return ((w & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u);
+}
+// A value operand of a block whose rows some columns do not see: their weight
+// is 0, but 0 times an infinity or NaN would reach them through the product.
+// Such elements are left out (set to 0) and reported, to be added after the
+// block loop to the columns that see them (add_nonfinite).
+__device__ __forceinline__ bool leave_out_nonfinite(uint4 &x) {
+  const uint32_t m0 = finite_halves(x.x), m1 = finite_halves(x.y), m2 = finite_halves(x.z), m3 = finite_halves(x.w);
+  x.x &= m0;
+  x.y &= m1;
+  x.z &= m2;
+  x.w &= m3;
+  return (m0 & m1 & m2 & m3) != 0xffffffffu;
+}
+// Adds the infinities and NaN of a block's 32 bf16 rows (row_ptr(i)) to the
+// columns that see them (sees(i): this lane's column sees row i); acc[t] holds
+// dims 32 t + 8 j + 4 half .. + 4 of the lane's column in registers 4 j .. + 4.
+// SIGNED: weights of either sign (or 0), with which such an element gives NaN;
+// otherwise weights are positive and it keeps its value.
+template <int D, bool SIGNED, typename Row, typename Sees>
+__device__ __forceinline__ void add_nonfinite(f32x16_t (&acc)[D / 32], Row &&row_ptr, Sees &&sees, int hb) {
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    if (!sees(i)) continue;
+    const char *x = row_ptr(i);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(x + (32 * t + 8 * j + 4 * hb) * 2);
+        const float f[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[t][4 * j + e] += is_finite(f[e]) ? 0.0f : SIGNED ? __builtin_nanf("") : f[e];
+      }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // fp32 on the matrix cores (v_mfma_f32_32x32x2_f32: lane l holds A[l % 32][l / 32],
 // B[l / 32][l % 32]; register r of the result is row 8 (r / 4) + 4 (l / 32) + r % 4,

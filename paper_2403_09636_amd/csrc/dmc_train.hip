@@ -1325,48 +1325,6 @@ __device__ __forceinline__ void wait_block(int after) {
   else wait_vmcnt<0>();
 }
 
-// Swizzle of a block's rows: 0 key (row reads), 1 value (transposed reads),
-// 2 dual (both).
-template <int CPR, int SW>
-__device__ __forceinline__ int block_swizzle(int row) {
-  return SW == 0 ? k_swizzle<CPR>(row) : SW == 1 ? v_swizzle<CPR>(row) : dual_swizzle<CPR>(row);
-}
-
-// Transposed operand: A or B slice "rows 16 kk + 8 half + 0..7 of dim 32 t +
-// col" of a 32-row block (vaddr[t][h]: offsets of the two 4-row halves).
-template <int RB>
-__device__ __forceinline__ uint4 tr_operand(const char *blk, const uint32_t (&vaddr)[2], int kk) {
-  const uint2 h0 = ds_read_tr16(blk + vaddr[0] + 16 * kk * RB);
-  const uint2 h1 = ds_read_tr16(blk + vaddr[1] + 16 * kk * RB);
-  return make_uint4(h0.x, h0.y, h1.x, h1.y);
-}
-
-// Per-lane offsets of the transposed reads (per 32-dim tile and 4-row half)
-// for a block stored with swizzle SW (1 or 2): a 16-lane group points at
-// four 8-byte pieces of each of 4 rows.
-template <int D, int SW>
-__device__ __forceinline__ void tr_offsets(int lane, uint32_t (&vaddr)[D / 32][2]) {
-  constexpr int RB = D * 2, CPR = D / 8;
-  const int g16 = lane >> 4, r16 = lane & 15;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = 8 * (g16 >> 1) + 4 * h + (r16 >> 2);
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t) {
-      const int lc = 4 * t + 2 * (g16 & 1) + ((r16 & 3) >> 1);
-      vaddr[t][h] = row * RB + ((lc ^ block_swizzle<CPR, SW>(row)) * 16) + (r16 & 1) * 8;
-    }
-  }
-}
-
-// Row-read offsets: 16 bytes (dims 16 ks + 8 half .. + 8) of row `row` of a
-// block stored with swizzle SW.
-template <int D, int SW>
-__device__ __forceinline__ uint32_t row_offset(int row, int ks, int hb) {
-  constexpr int RB = D * 2, CPR = D / 8;
-  return row * RB + (((2 * ks + hb) ^ block_swizzle<CPR, SW>(row)) * 16);
-}
-
 // Launch order of the bf16 attention kernels on one XCD (its r-th workgroup,
 // `groups` units of `ntiles` tiles each).  A unit's tiles run together, heaviest
 // (rank 0) first, so that they share the unit's states in L2 -- but with one

@@ -1,0 +1,270 @@
+"""Plain causal attention of packed sequences (dmc_causal_forward, dmc_causal_backward) against
+float64: outputs and gradients within bounds derived from the arithmetic (packed_reference), rows
+outside the sequences untouched, non-finite tokens kept to the tokens that see them, any stream,
+any strides, replayed graphs."""
+import math
+
+import pytest
+import torch
+
+from tests.packed_reference import causal, check, cu_of, dtype_of
+
+pytestmark = pytest.mark.gpu
+
+
+def make(lens, hq, hkv, d, dtype, tail=0, fused=False, seed=0, scale=1.0):
+    """Inputs of packed sequences on the CPU: q, k, v, dout [T, heads, d]."""
+    gen = torch.Generator().manual_seed(seed + 7 * sum(lens))
+    T, dt = sum(lens) + tail, dtype_of(dtype)
+    x = (torch.randn(T, hq + 2 * hkv, d, generator=gen) * scale).to(dt)
+    dout = torch.randn(T, hq, d, generator=gen).to(dt)
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    return (q, k, v, dout) if fused else (q.contiguous(), k.contiguous(), v.contiguous(), dout)
+
+
+def on_gpu(t):
+    """The tensor on the GPU with its strides kept (views of one projection stay views)."""
+    if t.is_contiguous():
+        return t.cuda()
+    base = t._base.cuda()
+    return base.as_strided(t.shape, t.stride(), t.storage_offset())
+
+
+def run(P, q, k, v, dout, lens, backward=True):
+    T, hq, d = q.shape
+    cfg = P.make_causal_config(hq, k.shape[1], d, "fp32" if q.dtype == torch.float32 else "bf16")
+    att = P.DMCCausal(cfg, max(T, 1))
+    q, k, v, dout, cu = on_gpu(q), on_gpu(k), on_gpu(v), dout.cuda(), cu_of(lens).cuda()
+    sentinel = 7.0
+    out = torch.full((T, hq, d), sentinel, dtype=q.dtype, device="cuda")
+    lse = torch.full((T, hq), sentinel, device="cuda")
+    att.forward(q, k, v, cu, out=out, lse=lse)
+    res = dict(out=out, lse=lse)
+    if backward:
+        grads = [torch.full((T, t.shape[1], d), sentinel, dtype=q.dtype, device="cuda") for t in (q, k, v)]
+        att.backward(q, k, v, cu, out, lse, dout, *grads)
+        res.update(zip(("dq", "dk", "dv"), grads))
+    torch.cuda.synchronize()
+    for name, x in res.items():
+        assert (x[sum(lens):] == sentinel).all(), f"{name}: rows behind the last sequence were written"
+    return res
+
+
+CASES = [
+    # lens, hq, hkv, d
+    ([1], 1, 1, 64), ([2, 1], 2, 1, 128), ([31, 32, 33], 4, 2, 128), ([0, 5, 0, 0, 129, 64, 0], 4, 4, 64),
+    ([128], 8, 2, 128), ([257, 3], 6, 2, 128), ([300], 8, 8, 64), ([96, 1, 160], 16, 2, 64), ([511], 3, 1, 128),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,hq,hkv,d", CASES)
+def test_against_float64(torch_cuda, dtype, lens, hq, hkv, d):
+    import paper_2403_09636_amd as P
+    fused = len(lens) % 2 == 1
+    q, k, v, dout = make(lens, hq, hkv, d, dtype, tail=3 * (len(lens) > 1), fused=fused)
+    got, want = run(P, q, k, v, dout, lens), causal(q, k, v, lens, dout)
+    n = sum(lens)
+    for name in got:
+        value, bound = want[name]
+        worst = check(got[name][:n], (value[:n], bound[:n]), name)
+        print(f"{name}: {worst:.3f} of its bound")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_long_and_many(torch_cuda, dtype):
+    """More sequences than a wave has lanes, one of them long."""
+    import paper_2403_09636_amd as P
+    gen = torch.Generator().manual_seed(5)
+    lens = [int(x) for x in torch.randint(0, 9, (70,), generator=gen)] + [900] + [0, 1] * 3
+    q, k, v, dout = make(lens, 2, 1, 64, dtype)
+    got, want = run(P, q, k, v, dout, lens), causal(q, k, v, lens, dout)
+    for name in got:
+        check(got[name], want[name], name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_large_scores(torch_cuda, dtype):
+    """Scores of several hundred: one key takes nearly all the weight of a row."""
+    import paper_2403_09636_amd as P
+    lens = [200, 37]
+    q, k, v, dout = make(lens, 4, 2, 64, dtype, scale=8.0)
+    got, want = run(P, q, k, v, dout, lens), causal(q, k, v, lens, dout)
+    for name in got:
+        check(got[name], want[name], name)
+
+
+def test_gradients_by_differences(torch_cuda):
+    """fp32 gradients along random directions against central differences of the float64 forward:
+    with step h = 1e-4 the differences are off by h^2 times a third derivative (below 1e-5 here) and
+    2^-52 / h, the gradients by their bound."""
+    import paper_2403_09636_amd as P
+    lens = [40, 0, 71]
+    q, k, v, dout = make(lens, 4, 2, 64, "fp32", scale=0.5)
+    got, want = run(P, q, k, v, dout, lens), causal(q, k, v, lens, dout)
+    h = 1e-4
+    for name, i in (("dq", 0), ("dk", 1), ("dv", 2)):
+        gen = torch.Generator().manual_seed(i)
+        x = [q, k, v]
+        dirn = torch.randn(x[i].shape, generator=gen, dtype=torch.float64)
+        loss = []
+        for sign in (1, -1):
+            y = [t.double() for t in x]
+            y[i] = y[i] + sign * h * dirn
+            loss.append((causal64(*y, lens) * dout.double()).sum())
+        fd = float(loss[0] - loss[1]) / (2 * h)
+        mine = float((got[name].cpu().double() * dirn).sum())
+        tol = float((want[name][1] * dirn.abs()).sum()) + 1e-5 * (1 + abs(fd))
+        assert abs(fd - mine) <= tol, (name, fd, mine, tol)
+
+
+def causal64(q, k, v, lens):
+    out, lo, G = torch.zeros_like(q), 0, q.shape[1] // k.shape[1]
+    for n in lens:
+        r = slice(lo, lo + n)
+        lo += n
+        for h in range(q.shape[1] if n else 0):
+            s = q[r, h] @ k[r, h // G].T / math.sqrt(q.shape[2])
+            s = s.masked_fill(torch.ones(n, n).triu(1) > 0, -math.inf)
+            out[r, h] = torch.softmax(s, 1) @ v[r, h // G]
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_non_finite_tokens(torch_cuda, dtype, bad):
+    """A bad token (every element of its q, k, v and output gradient) reaches the outputs of the tokens
+    after it in its sequence, and the gradients of that sequence's keys that it attends to; nothing before
+    it in the forward, and no other sequence."""
+    import paper_2403_09636_amd as P
+    lens, at = [50, 70, 45], 50 + 37
+    q, k, v, dout = make(lens, 4, 2, 64, dtype)
+    clean = causal(q, k, v, lens, dout)
+    for t in (q, k, v, dout):
+        t[at] = bad
+    got = run(P, q, k, v, dout, lens)
+    others = torch.ones(sum(lens), dtype=torch.bool)
+    others[50:120] = False
+    for name in got:
+        value, bound = clean[name]
+        check(got[name][:165][others], (value[others], bound[others]), name)
+    before = slice(50, at)
+    for name in ("out", "lse", "dq"):
+        check(got[name][before], tuple(x[before] for x in clean[name]), name)
+    assert not got["out"][at:120].isfinite().any()
+    # the keys after the bad token are not seen by it; queries after it see it: their rows are bad
+    assert not got["dk"][50:at + 1].isfinite().any() and not got["dv"][50:at + 1].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_bad_value_row(torch_cuda, dtype):
+    """An infinity in one element of a value row: that element of the outputs from its token on."""
+    import paper_2403_09636_amd as P
+    lens = [100]
+    q, k, v, dout = make(lens, 2, 1, 64, dtype)
+    want = causal(q, k, v, lens)["out"]
+    v[70, 0, 5] = math.inf
+    got = run(P, q, k, v, dout, lens, backward=False)["out"].cpu()
+    check(got[:70], tuple(x[:70] for x in want), "out before")
+    rest = [e for e in range(64) if e != 5]
+    check(got[70:][..., rest], tuple(x[70:][..., rest] for x in want), "other elements")
+    assert (got[70:, :, 5] == math.inf).all()
+
+
+def test_tail_of_nan(torch_cuda):
+    """Rows behind the last sequence may hold anything."""
+    import paper_2403_09636_amd as P
+    lens = [33, 40]
+    for dtype in ("bf16", "fp32"):
+        q, k, v, dout = make(lens, 4, 2, 128, dtype, tail=60)
+        want = causal(q, k, v, lens, dout)
+        for t in (q, k, v, dout):
+            t[73:] = math.nan
+        got = run(P, q, k, v, dout, lens)
+        for name in got:
+            check(got[name][:73], tuple(x[:73] for x in want[name]), name)
+
+
+def test_strides_and_views(torch_cuda):
+    """Head-major inputs, broadcast keys and values, outputs and gradients inside larger buffers."""
+    import paper_2403_09636_amd as P
+    lens, hq, hkv, d = [45, 90], 4, 2, 64
+    q, k, v, dout = make(lens, hq, hkv, d, "bf16")
+    k, v = k[:, :1].expand(-1, hkv, -1), v[:, :1].expand(-1, hkv, -1)
+    want = causal(q, k, v, lens, dout)
+    T, cu = 135, cu_of(lens).cuda()
+    att = P.DMCCausal(P.make_causal_config(hq, hkv, d), T)
+    qg = q.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+    kg, vg = (t[:, :1].contiguous().cuda().expand(-1, hkv, -1) for t in (k, v))
+    dog = dout.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+    buf = torch.full((T, hq + 2 * hkv + 1, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    out, lse = att.forward(qg, kg, vg, cu, out=torch.empty(hq, T, d, dtype=torch.bfloat16, device="cuda").transpose(0, 1))
+    dq, dk, dv = att.backward(qg, kg, vg, cu, out, lse, dog, dq=buf[:, :hq], dk=buf[:, hq:hq + hkv],
+                              dv=buf[:, hq + hkv:hq + 2 * hkv])
+    for name, x in dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        check(x, want[name], name)
+    assert (buf[:, -1] == 3.0).all()
+
+
+def test_streams_runs_and_graphs(torch_cuda):
+    """Same results on another stream, from run to run, and from a captured graph replayed between
+    eager calls (forward and backward of one handle)."""
+    import paper_2403_09636_amd as P
+    lens = [200, 0, 77, 150]
+    for dtype in ("bf16", "fp32"):
+        q, k, v, dout = (t.cuda() for t in make(lens, 4, 2, 128, dtype))
+        cu = cu_of(lens).cuda()
+        att = P.DMCCausal(P.make_causal_config(4, 2, 128, dtype), 427)
+
+        def step():
+            out, lse = att.forward(q, k, v, cu)
+            return (out, lse, *att.backward(q, k, v, cu, out, lse, dout))
+        want = step()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = step()
+        torch.cuda.current_stream().wait_stream(side)
+        for a, b in zip(want, other):
+            assert torch.equal(a, b)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept = step()
+        for i in range(3):
+            for x in kept:
+                x.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(want, kept):
+                assert torch.equal(a, b), f"replay {i}"
+            q.mul_(0.5)
+            want = step()
+
+
+def test_empty_calls(torch_cuda):
+    import paper_2403_09636_amd as P
+    att = P.DMCCausal(P.make_causal_config(4, 2, 64), 8)
+    for T, lens in ((0, [0, 0]), (8, []), (8, [0, 0, 0])):
+        q = torch.zeros(T, 4, 64, dtype=torch.bfloat16, device="cuda")
+        k = torch.zeros(T, 2, 64, dtype=torch.bfloat16, device="cuda")
+        out, lse = torch.ones_like(q), torch.ones(T, 4, device="cuda")
+        att.forward(q, k, k, cu_of(lens).cuda(), out=out, lse=lse)
+        dq, dk, dv = (torch.ones_like(t) for t in (q, k, k))
+        att.backward(q, k, k, cu_of(lens).cuda(), out, lse, q.clone(), dq, dk, dv)
+        assert all((x == 1).all() for x in (out, lse, dq, dk, dv))
+
+
+def test_boundaries_out_of_range(torch_cuda):
+    """Boundaries past the tensors are clamped: the rows inside come out as for the clamped ones."""
+    import paper_2403_09636_amd as P
+    lens = [60, 40]
+    q, k, v, dout = make(lens, 2, 2, 64, "bf16")
+    want = run(P, q, k, v, dout, lens)
+    att = P.DMCCausal(P.make_causal_config(2, 2, 64), 100)
+    cu = torch.tensor([-5, 60, 1 << 30], dtype=torch.int32, device="cuda")
+    out, lse = att.forward(q.cuda(), k.cuda(), v.cuda(), cu)
+    assert torch.equal(out, want["out"]) and torch.equal(lse, want["lse"])
+    cu = torch.tensor([40, 0, -100, 1 << 30, 90], dtype=torch.int32, device="cuda")   # decreasing: results undefined
+    att.forward(q.cuda(), k.cuda(), v.cuda(), cu, out=out, lse=lse)
+    att.backward(q.cuda(), k.cuda(), v.cuda(), cu, out, lse, dout.cuda())
+    torch.cuda.synchronize()
