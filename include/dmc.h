@@ -334,6 +334,73 @@ dmc_status dmc_train_backward(const dmc_train_config *cfg, const void *q_dev, co
                               size_t workspace_bytes, dmc_stream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * A chunk of new tokens per batch row on top of what the layer's cache holds:
+ * prompts fed in pieces, later turns of a conversation, whole prompts packed
+ * without padding (on an empty cache), drafted tokens to be checked.
+ * dmc_chunk_attend computes the chunk's attention and leaves the cache as it
+ * is; dmc_chunk_append commits the chunk, or of each row only the first
+ * accepted tokens (a draft that was partly rejected).  The semantics are those
+ * of dmc_prefill_attend continued: Algorithm 1 runs over the row's new tokens
+ * in order, from the unit's current open slot, and every token attends to the
+ * cache as it stands right after its own update.  (Committing a draft from a
+ * decode loop would merge rejected tokens into slots, which cannot be undone.)
+ *
+ * Row b's chunk is the tokens cu[b] .. cu[b+1]-1 of packed tensors:
+ *   cu_seqlens_dev: int32 [batch + 1], not decreasing; a row may have none.
+ *     Boundaries outside [0, total_tokens] or decreasing, and rows of more than
+ *     max_chunk tokens, raise the invalid-argument device flag (dmc_cache_check)
+ *     and are clamped: no access outside the tensors or the cache, results
+ *     undefined (of a longer row, the tokens past max_chunk are not processed).
+ *   k_dev, v_dev [total_tokens, Hkv, d], q_dev and out_dev [total_tokens, Hq, d]:
+ *     config dtype, element strides of the token and head axes (d contiguous),
+ *     16-byte aligned, strides non-negative multiples of 8, token strides of
+ *     the inputs below 32 MiB.  out must not overlap an input, nor its rows each
+ *     other; rows outside every chunk stay as they were.
+ *   max_chunk >= 1: the most tokens of any row.
+ *   workspace_dev: caller-owned device memory, 256-byte aligned,
+ *     dmc_chunk_workspace_bytes for at least this total_tokens and max_chunk; it
+ *     carries nothing between calls, and calls that may overlap need one each.
+ * Calls only enqueue kernels (no allocation, no memset, no synchronisation), so
+ * they can be captured in a HIP graph; lengths are read on the device.  Caches
+ * with a window return DMC_ERR_UNSUPPORTED.
+ * ------------------------------------------------------------------------- */
+
+/* Workspace bytes for chunks of up to total_tokens tokens in all and max_chunk
+ * in a row (0 if invalid, see dmc_last_error). */
+size_t dmc_chunk_workspace_bytes(const dmc_cache *cache, int32_t total_tokens, int32_t max_chunk);
+
+/* Attention of a chunk over one layer's cache and itself; the cache (slots,
+ * lengths, z, pages) is not changed. */
+dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q_dev,
+                            const int64_t q_strides[2], const void *k_dev,
+                            const int64_t k_strides[2], const void *v_dev,
+                            const int64_t v_strides[2], const int32_t *cu_seqlens_dev,
+                            int32_t total_tokens, int32_t max_chunk, void *out_dev,
+                            const int64_t out_strides[2], void *workspace_dev,
+                            size_t workspace_bytes, dmc_stream_t stream);
+
+/* Append a chunk to one layer's cache: new slots, lengths and z as after the
+ * same tokens' decode steps.
+ *   q_dev: logical [total_tokens, Hq, d]; only element 0 of each row is read (a
+ *     [total_tokens, Hq] tensor of q[..., 0] with strides (Hq, 1) is accepted),
+ *     no alignment requirement.
+ *   accepted_dev: optional int32 [batch]: of row b's chunk only its first
+ *     accepted[b] tokens are appended (values outside [0, its tokens] raise the
+ *     invalid-argument flag and are clamped).  NULL = all of them.
+ *   slot_index_dev: optional int32 [total_tokens, Hkv]: slot each token of a
+ *     chunk went to, -1 for tokens that were not appended; other rows stay as
+ *     they were.
+ * A unit without room for its whole chunk (slots, pages) keeps its cache as it
+ * was and raises the capacity flag. */
+dmc_status dmc_chunk_append(dmc_cache *cache, int32_t layer, const void *k_dev,
+                            const int64_t k_strides[2], const void *v_dev,
+                            const int64_t v_strides[2], const void *q_dev,
+                            const int64_t q_strides[2], const int32_t *cu_seqlens_dev,
+                            const int32_t *accepted_dev, int32_t total_tokens, int32_t max_chunk,
+                            int32_t *slot_index_dev, void *workspace_dev, size_t workspace_bytes,
+                            dmc_stream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Plain causal attention of packed sequences (Sec. 2.1: softmax of q.k/sqrt(d),
  * every element of q and k, no cache, no compression), forward and backward:
  * for layers that keep their full cache, and for the uncompressed model that a

@@ -30,6 +30,7 @@ EXPORTS = ("dmc_cache_workspace_bytes", "dmc_cache_alloc", "dmc_cache_free", "dm
            "dmc_cache_lengths", "dmc_cache_export",
            "dmc_cache_import", "dmc_cache_check", "dmc_cache_pages_used", "dmc_last_error",
            "dmc_train_workspace_bytes", "dmc_train_forward", "dmc_train_backward",
+           "dmc_chunk_workspace_bytes", "dmc_chunk_attend", "dmc_chunk_append",
            "dmc_causal_workspace_bytes", "dmc_causal_forward", "dmc_causal_backward")
 
 
@@ -102,9 +103,15 @@ def _load():
     lib.dmc_train_backward.argtypes = [POINTER(TrainConfig), c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_size_t, c_void_p]
+    packed = [c_void_p, i64p]   # a tensor [tokens, heads, d] and its strides
+    lib.dmc_chunk_workspace_bytes.argtypes = [c_void_p, c_int32, c_int32]
+    lib.dmc_chunk_workspace_bytes.restype = c_size_t
+    lib.dmc_chunk_attend.argtypes = [c_void_p, c_int32, *packed * 3, c_void_p, c_int32, c_int32,
+                                     *packed, c_void_p, c_size_t, c_void_p]
+    lib.dmc_chunk_append.argtypes = [c_void_p, c_int32, *packed * 3, c_void_p, c_void_p, c_int32,
+                                     c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.dmc_causal_workspace_bytes.argtypes = [POINTER(CausalConfig), c_int32]
     lib.dmc_causal_workspace_bytes.restype = c_size_t
-    packed = [c_void_p, i64p]   # a tensor [tokens, heads, d] and its strides
     lib.dmc_causal_forward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
                                        *packed, c_void_p, c_void_p]
     lib.dmc_causal_backward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
@@ -367,12 +374,17 @@ def _packed_overlap(x, y):
     return shift < xr or shift + yr > step
 
 
+def _check_rows(name, t, dtype, tokens, heads, d):
+    some = getattr(t, "shape", (1,))[:1] != (0,)   # (an empty tensor's strides mean nothing)
+    _check(name, t, dtype, (tokens, heads, d), contiguous=False, last_dim_contiguous=some,
+           stride_mult=8 if some else None)
+
+
 def _check_packed(inputs, outputs, dtype, d):
     """Packed tensors (name, tensor, tokens, heads): [tokens, heads, d], contiguous last dimension,
     strides multiples of 8 elements, 16-byte aligned; an output shares memory with no other one."""
     for name, t, tokens, heads in (*inputs, *outputs):
-        _check(name, t, dtype, (tokens, heads, d), contiguous=False, last_dim_contiguous=True,
-               stride_mult=8)
+        _check_rows(name, t, dtype, tokens, heads, d)
     for i, (name, t, _, _) in enumerate(outputs):
         for other, x, _, _ in (*inputs, *outputs[:i]):
             if _packed_overlap(t, x):
@@ -386,13 +398,38 @@ def _check_cu(cu_seqlens, rows=None):
         _fail("cu_seqlens is empty")
 
 
+def check_chunk_args(cfg, device, q, k, v, cu_seqlens, out=None, accepted=None, slot_index=None):
+    """dmc_chunk_attend (with out) and dmc_chunk_append: packed k, v [T, Hkv, d] and, for attention,
+    q, out [T, Hq, d]; otherwise q [T, Hq] or [T, Hq, *] (only element 0 is read); cu_seqlens int32
+    [B + 1]; accepted int32 [B]; slot_index int32 [T, Hkv]."""
+    import torch
+    dt = cache_dtype(cfg)
+    Hq, Hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    _check_rows("k", k, dt, None, Hkv, d)
+    T = k.shape[0]
+    inputs = [("k", k, T, Hkv), ("v", v, T, Hkv)]
+    if out is not None:
+        _check_packed([("q", q, T, Hq), *inputs], [("out", out, T, Hq)], dt, d)
+    else:
+        _check_packed(inputs, (), dt, d)
+        _check("q", q, dt, (T, Hq) if isinstance(q, torch.Tensor) and q.dim() == 2 else (T, Hq, None),
+               contiguous=False, align16=False)
+    _check_cu(cu_seqlens, cfg.batch)
+    if accepted is not None:
+        _check("accepted", accepted, torch.int32, (cfg.batch,), align16=False)
+    if slot_index is not None:
+        _check("slot_index", slot_index, torch.int32, (T, Hkv), align16=False)
+    _on_device(device, q=q, k=k, v=v, cu_seqlens=cu_seqlens, out=out, accepted=accepted,
+               slot_index=slot_index)
+
+
 def check_causal_args(cfg, device, q, k, v, cu_seqlens, out, lse, dout=None, dq=None, dk=None, dv=None):
     """dmc_causal_forward / dmc_causal_backward (with dout and the gradients): q-shaped [T, Hq, d] and
     k-shaped [T, Hkv, d] packed tensors, cu_seqlens int32 [sequences + 1], lse float32 [T, Hq]."""
     import torch
     dt = torch.float32 if cfg.dtype == DMC_FP32 else torch.bfloat16
     Hq, Hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
-    _check("q", q, dt, (None, Hq, d), contiguous=False, last_dim_contiguous=True, stride_mult=8)
+    _check_rows("q", q, dt, None, Hq, d)
     T = q.shape[0]
     inputs = [("q", q, T, Hq), ("k", k, T, Hkv), ("v", v, T, Hkv)]
     outputs = [("out", out, T, Hq)]
@@ -547,6 +584,51 @@ class DMCCache:
 
     def reset(self, stream=None):
         check(lib.dmc_cache_reset(self.handle, _stream(stream)))
+
+
+class DMCChunk:
+    """Chunks of new tokens on top of a cache (pieces of prompts, later turns, packed prompts,
+    drafted tokens): the workspace for up to max_tokens tokens in a call, at most max_chunk of them
+    in a batch row, in one torch allocation.  Keeps the cache alive."""
+
+    def __init__(self, cache: DMCCache, max_tokens, max_chunk=None):
+        import torch
+        self.cache = cache
+        self.max_tokens = max_tokens
+        self.max_chunk = max(1, max_tokens if max_chunk is None else max_chunk)
+        n = lib.dmc_chunk_workspace_bytes(cache.handle, max_tokens, self.max_chunk)
+        if n == 0:
+            raise DMCError(DMC_ERR_INVALID_ARG, last_error())
+        self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=cache.device)
+        self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
+        self._ws_bytes = n
+
+    def _tokens(self, k):
+        if k.shape[0] > self.max_tokens:
+            _fail(f"{k.shape[0]} tokens, the workspace holds {self.max_tokens}")
+        return k.shape[0]
+
+    def attend(self, layer, q, k, v, cu_seqlens, out=None, stream=None):
+        """Attention of packed new tokens q [T, Hq, d], k, v [T, Hkv, d] over the layer's cache and
+        themselves, row b's chunk being the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1; the cache
+        stays as it is.  Returns out [T, Hq, d]; rows outside every chunk stay as they are."""
+        if out is None:
+            out = torch_empty_like(q)
+        check_chunk_args(self.cache.cfg, self.cache.device, q, k, v, cu_seqlens, out)
+        check(lib.dmc_chunk_attend(self.cache.handle, layer, _ptr(q), _strides(q), _ptr(k), _strides(k),
+                                   _ptr(v), _strides(v), _ptr(cu_seqlens), self._tokens(k),
+                                   self.max_chunk, _ptr(out), _strides(out), self._ws, self._ws_bytes,
+                                   _stream(stream)))
+        return out
+
+    def append(self, layer, k, v, q, cu_seqlens, accepted=None, slot_index=None, stream=None):
+        """Append the chunk (of row b only its first accepted[b] tokens) to the layer's cache; only
+        q[..., 0] is read.  slot_index [T, Hkv] receives each token's slot, -1 if not appended."""
+        check_chunk_args(self.cache.cfg, self.cache.device, q, k, v, cu_seqlens, None, accepted, slot_index)
+        check(lib.dmc_chunk_append(self.cache.handle, layer, _ptr(k), _strides(k), _ptr(v), _strides(v),
+                                   _ptr(q), _strides(q), _ptr(cu_seqlens), _ptr(accepted),
+                                   self._tokens(k), self.max_chunk, _ptr(slot_index), self._ws,
+                                   self._ws_bytes, _stream(stream)))
 
 
 def torch_empty_like(t):

@@ -1009,6 +1009,195 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, cons
   return DMC_OK;
 }
 
+// Workspace of the chunk calls: byte offsets of its sections (256-byte aligned).
+struct ChunkLayout {
+  size_t state_k, state_v, closed_k, closed_v, before, starts, carry, visible, piece_base, pieces, record_base, old_len,
+      old_z, partials, total;
+};
+
+// Attention pieces beyond one per column tile, and the fewest 32-row blocks of
+// one.  Four per compute unit; none once the tiles themselves are eight per
+// compute unit.
+static int32_t chunk_piece_budget(const dmc_cache *c, int32_t total, int shift) {
+  const int64_t tiles = int64_t(total >> shift) * c->cfg.num_kv_heads;
+  return tiles >= int64_t(8) * c->cu_count ? 0 : 4 * c->cu_count;
+}
+constexpr int32_t kChunkPieceMin = 8;
+
+static ChunkLayout chunk_layout(const dmc_cache *c, int32_t total) {
+  const dmc_cache_config &cfg = c->cfg;
+  const size_t es = elem_bytes(cfg), d = cfg.head_dim, H = cfg.num_kv_heads, U = c->lay.units, B = cfg.batch;
+  const size_t blocks32 = size_t(total) / 32 + B, blocks64 = size_t(total) / 64 + B;
+  ChunkLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return at;
+  };
+  L.state_k = take(H * total * d * es);
+  L.state_v = take(H * total * d * es);
+  L.closed_k = take(H * blocks32 * 32 * d * es);
+  L.closed_v = take(H * blocks32 * 32 * d * es);
+  L.before = take(H * total * 4);
+  L.starts = take(H * blocks64 * 4);
+  L.carry = take(H * blocks64 * dmc::carry_stride(cfg.head_dim) * 4);
+  L.visible = take(U * 4);
+  L.piece_base = take((U + 1) * 4);
+  L.pieces = take(U * 4);
+  L.record_base = take(U * 4);
+  L.old_len = take(U * 4);
+  L.old_z = take(U * 4);
+  // (wide tiles' records, which narrow ones fit as well)
+  L.partials = take(size_t(4) * c->cu_count * (cfg.dtype == DMC_BF16 ? 128 : 32) * (d + 4) * 4);
+  L.total = off;
+  return L;
+}
+
+static dmc_status check_chunk_sizes(const dmc_cache *c, int32_t total, int32_t max_chunk) {
+  if (!c) return fail(DMC_ERR_INVALID_ARG, "cache is NULL");
+  if (c->lay.window > 0)
+    return fail(DMC_ERR_UNSUPPORTED, "chunks on a cache with a window are not supported");
+  if (total < 0) return fail(DMC_ERR_INVALID_ARG, "total_tokens must be >= 0");
+  if (max_chunk < 1) return fail(DMC_ERR_INVALID_ARG, "max_chunk must be >= 1");
+  if (total > (1 << 24)) return fail(DMC_ERR_UNSUPPORTED, "more than %d tokens in a call", 1 << 24);
+  // grids: a workgroup per 64-token block or column tile (of 4 tokens or more) and kv head; heads in grid.y
+  const int64_t tiles = int64_t(total) / 4 + c->cfg.batch;
+  if (c->cfg.num_kv_heads > 65535 || tiles * c->cfg.num_kv_heads + 4 * c->cu_count > 0x7fffffff)
+    return fail(DMC_ERR_UNSUPPORTED, "too many tokens, rows and heads for one launch");
+  return DMC_OK;
+}
+
+// Checks and parameters that both chunk calls share.
+static dmc_status chunk_params(const dmc_cache *c, int32_t layer, const void *k, const int64_t *k_strides, const void *v,
+                               const int64_t *v_strides, const void *q, const int64_t *q_strides, const int32_t *cu,
+                               int32_t total, int32_t max_chunk, void *ws, size_t bytes, dmc::ChunkParams *out) {
+  dmc_status st = check_layer(c, layer);
+  if (st == DMC_OK) st = check_chunk_sizes(c, total, max_chunk);
+  if (st != DMC_OK) return st;
+  const dmc_cache_config &cfg = c->cfg;
+  const dmc::Layout &L = c->lay;
+  const int es = elem_bytes(cfg);
+  if (total > 0) {
+    for (const Packed &t : {Packed{"k", k, k_strides, cfg.num_kv_heads, true, false},
+                            Packed{"v", v, v_strides, cfg.num_kv_heads, true, false}}) {
+      st = check_packed(t, total, cfg.head_dim, es);
+      if (st != DMC_OK) return st;
+    }
+    if (!q || !q_strides) return fail(DMC_ERR_INVALID_ARG, "q and its strides must be non-NULL");
+    if (q_strides[0] < 0 || q_strides[1] < 0) return fail(DMC_ERR_INVALID_ARG, "q strides must be non-negative");
+    if (q_strides[0] >= (int64_t(1) << 25) / es || q_strides[1] > (int64_t(1) << 40))
+      return fail(DMC_ERR_UNSUPPORTED, "q token stride must be below 32 MiB");
+    if (!cu || !ws) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens and workspace must be non-NULL");
+    if (reinterpret_cast<uintptr_t>(ws) & 255u)
+      return fail(DMC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  }
+  const ChunkLayout W = chunk_layout(c, total);
+  if (total > 0 && bytes < W.total)
+    return fail(DMC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", bytes, W.total);
+  dmc::ChunkParams &p = *out;
+  p = dmc::ChunkParams{};
+  p.pool = c->ws + L.pool;
+  p.page_bytes = L.page_bytes;
+  p.num_pages = cfg.num_pages;
+  p.ptab = at<int32_t>(c, L.ptab) + size_t(layer) * L.units * L.maxpages;
+  p.len = lens_of(c, layer, 0);
+  p.z = at<float>(c, L.z) + size_t(layer) * L.units;
+  p.ctrl = at<dmc::Control>(c, L.ctrl);
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  if (total > 0) {
+    copy_strides(p.qs, q_strides);
+    copy_strides(p.ks, k_strides);
+    copy_strides(p.vs, v_strides);
+  }
+  p.cu = cu;
+  char *w = static_cast<char *>(ws);
+  p.state_k = w + W.state_k;
+  p.state_v = w + W.state_v;
+  p.closed_k = w + W.closed_k;
+  p.closed_v = w + W.closed_v;
+  p.before = reinterpret_cast<int32_t *>(w + W.before);
+  p.starts = reinterpret_cast<int32_t *>(w + W.starts);
+  p.carry = reinterpret_cast<float *>(w + W.carry);
+  p.visible = reinterpret_cast<int32_t *>(w + W.visible);
+  p.piece_base = reinterpret_cast<int32_t *>(w + W.piece_base);
+  p.pieces = reinterpret_cast<int32_t *>(w + W.pieces);
+  p.record_base = reinterpret_cast<int32_t *>(w + W.record_base);
+  p.old_len = reinterpret_cast<int32_t *>(w + W.old_len);
+  p.old_z = reinterpret_cast<float *>(w + W.old_z);
+  p.partials = reinterpret_cast<float *>(w + W.partials);
+  p.c = cfg.decision_bias;
+  p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(cfg.head_dim)));
+  p.rows = cfg.batch;
+  p.total = total;
+  p.max_chunk = max_chunk;
+  p.units = L.units;
+  p.hq = cfg.num_q_heads;
+  p.hkv = cfg.num_kv_heads;
+  p.maxpages = L.maxpages;
+  p.max_slots = cfg.max_slots_per_seq;
+  p.log2p = ilog2(cfg.page_size);
+  p.omega_src = cfg.omega_src;
+  p.decision_src = cfg.decision_src;
+  p.blocks64 = total / 64 + cfg.batch;
+  p.blocks32 = total / 32 + cfg.batch;
+  p.piece_min = kChunkPieceMin;
+  return DMC_OK;
+}
+
+size_t dmc_chunk_workspace_bytes(const dmc_cache *cache, int32_t total, int32_t max_chunk) {
+  if (check_chunk_sizes(cache, total, max_chunk) != DMC_OK) return 0;
+  return chunk_layout(cache, total).total;
+}
+
+dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q, const int64_t q_strides[2],
+                            const void *k, const int64_t k_strides[2], const void *v, const int64_t v_strides[2],
+                            const int32_t *cu, int32_t total, int32_t max_chunk, void *out,
+                            const int64_t out_strides[2], void *ws, size_t bytes, dmc_stream_t stream) {
+  dmc::ChunkParams p;
+  dmc_status st = chunk_params(cache, layer, k, k_strides, v, v_strides, q, q_strides, cu, total, max_chunk, ws, bytes, &p);
+  if (st != DMC_OK) return st;
+  if (total == 0) return DMC_OK;
+  const dmc_cache_config &c = cache->cfg;
+  for (const Packed &t : {Packed{"q", q, q_strides, c.num_q_heads, true, false},
+                          Packed{"out", out, out_strides, c.num_q_heads, false, true}}) {
+    st = check_packed(t, total, c.head_dim, elem_bytes(c));
+    if (st != DMC_OK) return st;
+  }
+  p.out = out;
+  copy_strides(p.os, out_strides);
+  const bool wide = dmc::chunk_wide(elem_bytes(c), cache->lay.group, max_chunk);
+  p.tile_shift = dmc::chunk_tile_shift(cache->lay.group, wide);
+  p.piece_budget = chunk_piece_budget(cache, total, p.tile_shift);
+  DeviceGuard g(cache->device);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");
+  hipError_t e = dmc::launch_chunk_attend(elem_bytes(c), c.head_dim, cache->lay.group, cache->lay.v_trans, wide, p,
+                                          static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "chunk attention launch");
+  return DMC_OK;
+}
+
+dmc_status dmc_chunk_append(dmc_cache *cache, int32_t layer, const void *k, const int64_t k_strides[2],
+                            const void *v, const int64_t v_strides[2], const void *q, const int64_t q_strides[2],
+                            const int32_t *cu, const int32_t *accepted, int32_t total, int32_t max_chunk,
+                            int32_t *slot_index, void *ws, size_t bytes, dmc_stream_t stream) {
+  dmc::ChunkParams p;
+  dmc_status st = chunk_params(cache, layer, k, k_strides, v, v_strides, q, q_strides, cu, total, max_chunk, ws, bytes, &p);
+  if (st != DMC_OK) return st;
+  if (total == 0) return DMC_OK;
+  p.accepted = accepted;
+  p.slot_index = slot_index;
+  const dmc_cache_config &c = cache->cfg;
+  DeviceGuard g(cache->device);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");
+  hipError_t e = dmc::launch_chunk_append(elem_bytes(c), c.head_dim, cache->lay.v_trans, p,
+                                          static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "chunk append launch");
+  return DMC_OK;
+}
+
 static dmc_status read_control(dmc_cache *cache, dmc_stream_t stream, dmc::Control *out) {
   DeviceGuard g(cache->device);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");

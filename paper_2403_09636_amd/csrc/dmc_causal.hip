@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
   if (__any(left_out)) {
     const char *base = MODE == 0 ? vbase : kbase;
     const uint32_t st = MODE == 0 ? vst : kst;
-    add_nonfinite<D, MODE != 0>(acc, [&](int i) { return base + int64_t(min(a + i, n - 1)) * st; },
+    add_nonfinite<D, MODE != 0>(acc, [&](int i, int e) { return row4(base + int64_t(min(a + i, n - 1)) * st, e); },
                                 [&](int i) { return colv && i <= col; }, hb);
   }
 
@@ -602,7 +602,9 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
         if (rb < s0 || (rb != s0 && rb + 32 <= n)) continue;
         add_nonfinite<D, PART == 2>(
             acc,
-            [&](int i) { return row_at<2>(base, PART == 1 ? p.dos : p.qs, pt.start + min(rb + i, n - 1), hh); },
+            [&](int i, int e) {
+              return row4(row_at<2>(base, PART == 1 ? p.dos : p.qs, pt.start + min(rb + i, n - 1), hh), e);
+            },
             [&](int i) { return kv_ok && rb + i >= js && rb + i < n; }, hb);
       }
   }

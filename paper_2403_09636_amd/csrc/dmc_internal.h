@@ -276,6 +276,48 @@ struct CausalParams {
 hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 hipError_t launch_causal_backward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 
+// A chunk of new tokens per row, packed, on top of a layer's cache: attention
+// that leaves the cache as it is, and the commit of the chunk (or its accepted
+// part).  Tensors are [total, heads, d] with element strides of the token and
+// head axes.
+struct ChunkParams {
+  char *pool;
+  int64_t page_bytes, num_pages;
+  int32_t *ptab;                 // [U, maxpages] of this layer
+  int32_t *len;                  // [U]
+  float *z;                      // [U]
+  Control *ctrl;
+  const void *q, *k, *v;
+  int64_t qs[2], ks[2], vs[2], os[2];
+  void *out;
+  const int32_t *cu;             // [rows + 1]
+  const int32_t *accepted;       // optional [rows] (append)
+  int32_t *slot_index;           // optional [total, hkv] (append)
+  // workspace
+  char *state_k, *state_v;       // [hkv][total][d]: every token's slot as it stands after the token (attend)
+  char *closed_k, *closed_v;     // [hkv][blocks32][32][d]: a row's closed states in order, 32 to a block (values
+                                 // [d][32] per block where the cache's pages are transposed) (attend)
+  int32_t *before;               // [hkv][total]: closed states of the row before the token (attend)
+  int32_t *starts;               // [hkv][blocks64]: segment starts per 64-token block
+  float *carry;                  // [hkv][blocks64][carry_stride]: the open segment's sums at a block's end
+  int32_t *visible;              // [U]: cached slots that the chunk attends to (attend)
+  int32_t *piece_base;           // [U + 1]: pieces before the unit's (attend)
+  int32_t *pieces;               // [U]: pieces per tile of the unit's columns (attend)
+  int32_t *record_base;          // [U]: partial records before the unit's (attend)
+  float *partials;               // [piece_budget][columns][d + 4] (attend)
+  int32_t *old_len;              // [U]: length before the append, -1: the unit's chunk is dropped (append)
+  float *old_z;                  // [U] (append)
+  float c, scale_log2;
+  int32_t rows, total, max_chunk, units, hq, hkv, maxpages, max_slots, log2p, omega_src, decision_src;
+  int32_t blocks64, blocks32, tile_shift, piece_budget, piece_min;
+};
+// Tokens of a column tile of the attention (log2), and whether its workgroups take 128 columns or 32.
+bool chunk_wide(int elem_bytes, int group, int max_chunk);
+int chunk_tile_shift(int group, bool wide);
+hipError_t launch_chunk_attend(int elem_bytes, int head_dim, int group, bool vt, bool wide, const ChunkParams &p,
+                               hipStream_t s);
+hipError_t launch_chunk_append(int elem_bytes, int head_dim, bool vt, const ChunkParams &p, hipStream_t s);
+
 // Launchers (return hipGetLastError() after enqueueing).
 hipError_t launch_reset(const ResetParams &p, hipStream_t s);
 hipError_t launch_fill_u8(void *p, size_t bytes, hipStream_t s);

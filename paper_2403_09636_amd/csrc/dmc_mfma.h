@@ -265,22 +265,22 @@ __device__ __forceinline__ bool leave_out_nonfinite(uint4 &x) {
   x.w &= m3;
   return (m0 & m1 & m2 & m3) != 0xffffffffu;
 }
-// Adds the infinities and NaN of a block's 32 bf16 rows (row_ptr(i)) to the
-// columns that see them (sees(i): this lane's column sees row i); acc[t] holds
-// dims 32 t + 8 j + 4 half .. + 4 of the lane's column in registers 4 j .. + 4.
-// SIGNED: weights of either sign (or 0), with which such an element gives NaN;
-// otherwise weights are positive and it keeps its value.
-template <int D, bool SIGNED, typename Row, typename Sees>
-__device__ __forceinline__ void add_nonfinite(f32x16_t (&acc)[D / 32], Row &&row_ptr, Sees &&sees, int hb) {
+// Adds the infinities and NaN of a block's 32 bf16 rows to the columns that see
+// them (sees(i): this lane's column sees row i; load4(i, e): the packed elements
+// e .. e + 3 of row i); acc[t] holds dims 32 t + 8 j + 4 half .. + 4 of the
+// lane's column in registers 4 j .. + 4.  SIGNED: weights of either sign (or 0),
+// with which such an element gives NaN; otherwise weights are positive and it
+// keeps its value.
+template <int D, bool SIGNED, typename Load4, typename Sees>
+__device__ __forceinline__ void add_nonfinite(f32x16_t (&acc)[D / 32], Load4 &&load4, Sees &&sees, int hb) {
 #pragma unroll 1
   for (int i = 0; i < 32; ++i) {
     if (!sees(i)) continue;
-    const char *x = row_ptr(i);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(x + (32 * t + 8 * j + 4 * hb) * 2);
+        const uint2 w = load4(i, 32 * t + 8 * j + 4 * hb);
         const float f[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -288,6 +288,8 @@ __device__ __forceinline__ void add_nonfinite(f32x16_t (&acc)[D / 32], Row &&row
       }
   }
 }
+// The packed elements e .. e + 3 of a contiguous bf16 row.
+__device__ __forceinline__ uint2 row4(const char *row, int e) { return *reinterpret_cast<const uint2 *>(row + 2 * e); }
 
 // ---------------------------------------------------------------------------
 // fp32 on the matrix cores (v_mfma_f32_32x32x2_f32: lane l holds A[l % 32][l / 32],
