@@ -240,17 +240,18 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
         __builtin_amdgcn_sched_barrier(0);
       }
       scn = sc;
-      // P enters the value product rounded to bf16 (half a step of 2^-9 of a
-      // probability), and its sum is taken over the rounded values, so that the
-      // weights of a row add up to 1.
+      // P enters the value product rounded to bf16 (off by at most 2^-8 of a
+      // probability, at random); its sum is taken in fp32 before that, which L is
+      // the logarithm of (over the rounded values L was off by 1e-3).
       uint4 pb[2];
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
         uint32_t w[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          w[q] = cvt_pk_bf16(ev[8 * kk + 2 * q], ev[8 * kk + 2 * q + 1]);
-          ls = add_pair(w[q], ls);
+          const float e0 = ev[8 * kk + 2 * q], e1 = ev[8 * kk + 2 * q + 1];
+          w[q] = cvt_pk_bf16(e0, e1);
+          ls += e0 + e1;
         }
         pb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
       }

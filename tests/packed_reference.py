@@ -23,9 +23,9 @@ def causal(q, k, v, lens, dout=None):
     of its error: a dict name -> (value, bound).
 
     With u half a rounding step of the tensors' type and f = (n + d + 32) 2^-24 for fp32 chains:
-      out    rounding u |o|, and P rounded to the type (its sum over the rounded values):
-             sum P u |v - o| <= u (P |v| + |o|)
-      scores chains of d products: e_S = d 2^-24 |q|.|k| / sqrt(d), relative in P (twice: lse)
+      out    rounding u |o|, and P rounded to the type: u P |v|
+      lse    e_S and f
+      scores chains of d products: e_S = d 2^-24 |q|.|k| / sqrt(d), relative in P (twice: with lse's)
       D      = dO . o with the rounded o: e_D = sum |dO| bound(o)
       dS     = P (dP - D): u |dS| (rounded to the type) + P e_D + e_S |dS|
       dq     = sum dS k: sum e_dS |k| + u |dq|;  dk likewise;  dv = sum P dO: sum u P |dO| + u |dv|
@@ -58,9 +58,6 @@ def causal(q, k, v, lens, dout=None):
             for x, val, err in (("out", o, bo), ("lse", lse, es + f * (1 + lse.abs()))):
                 res[x][0][r, h] = val
                 res[x][1][r, h] = err
-            if name == "bf16":
-                # the sum of rounded probabilities: each within u, so lse within u
-                res["lse"][1][r, h] += u
             if dout is None:
                 continue
             do = dout[r, h].double()
@@ -68,14 +65,12 @@ def causal(q, k, v, lens, dout=None):
             D = (do * o).sum(1, keepdim=True)
             dS = P * (dp - D)
             eD = (do.abs() * (bo + f * o.abs())).sum(1, keepdim=True)
-            # lse of bf16 rows is off by up to u: every probability of the row with it
-            row = u if name == "bf16" else 0.0
             edp = f * (do.abs() @ vh.abs().T)
-            eS = (u + 2 * es + row + f) * dS.abs() + P * (eD + edp) * (1 + row)
+            eS = (u + 2 * es + f) * dS.abs() + P * (eD + edp)
             sc = 1 / math.sqrt(d)
             for x, hh, val, err in (("dq", h, dS @ kh * sc, (eS @ kh.abs() + f * dS.abs() @ kh.abs()) * sc),
                                     ("dk", h // G, dS.T @ qh * sc, (eS.T @ qh.abs() + f * dS.abs().T @ qh.abs()) * sc),
-                                    ("dv", h // G, P.T @ do, (pu + row + f) * (P.T @ do.abs()))):
+                                    ("dv", h // G, P.T @ do, (pu + f) * (P.T @ do.abs()))):
                 res[x][0][r, hh] += val
                 res[x][1][r, hh] += 1.1 * err + 1e-30
     for x in ("dq", "dk", "dv"):
