@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdmc.so")
@@ -103,7 +103,7 @@ def _load():
     lib.dmc_train_backward.argtypes = [POINTER(TrainConfig), c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_size_t, c_void_p]
-    packed = [c_void_p, i64p]   # a tensor [tokens, heads, d] and its strides
+    packed = [c_void_p, c_void_p]   # a tensor [tokens, heads, d] and its strides (int64 [2])
     lib.dmc_chunk_workspace_bytes.argtypes = [c_void_p, c_int32, c_int32]
     lib.dmc_chunk_workspace_bytes.restype = c_size_t
     lib.dmc_chunk_attend.argtypes = [c_void_p, c_int32, *packed * 3, c_void_p, c_int32, c_int32,
@@ -398,6 +398,53 @@ def _check_cu(cu_seqlens, rows=None):
         _fail("cu_seqlens is empty")
 
 
+class _PackedCall:
+    """The checks of a packed call's tensors in one pass, for calls whose GPU time is a few
+    microseconds: the conditions of _check_packed, tested without a message.  tensors() returns the
+    addresses of the tensors and their strides as one int64 array, or None if any condition fails (the
+    caller's full check then names it, or finds that nothing is wrong)."""
+
+    def __init__(self, dtype, device, d, es):
+        import torch
+        self.Tensor, self.f32, self.i32 = torch.Tensor, torch.float32, torch.int32
+        self.dtype, self.device, self.d, self.es = dtype, device, d, es
+        self.strides = {n: c_int64 * (2 * n) for n in range(1, 9)}
+
+    def tensors(self, T, inputs, outputs):
+        """inputs, outputs: (tensor, heads) each; outputs must lie apart from everything."""
+        dtype, device, d, es, tensor = self.dtype, self.device, self.d, self.es, self.Tensor
+        ptrs, strides, spans = [], [], []
+        for t, heads in (*inputs, *outputs):
+            if not (isinstance(t, tensor) and t.dtype is dtype and t.shape == (T, heads, d) and t.device == device):
+                return None
+            s0, s1, s2 = t.stride()
+            p = t.data_ptr()
+            if s2 != 1 or (s0 | s1) & 7 or p & 15:
+                return None
+            ptrs.append(p)
+            strides += (s0, s1)
+            spans.append((p, p + ((T - 1) * s0 + (heads - 1) * s1 + d) * es))
+        n = len(inputs)
+        for i in range(n, len(spans)):
+            lo, hi = spans[i]
+            for a, b in spans[:i]:
+                if lo < b and a < hi:
+                    return None
+        return ptrs, self.strides[len(ptrs)](*strides)
+
+    def rows(self, t):
+        return t.shape[0] if isinstance(t, self.Tensor) and t.dim() else 0
+
+    def array(self, t, dtype, shape=None):
+        """Address of a contiguous tensor of this type and shape (None: of one dimension and not
+        empty), or None."""
+        if not (isinstance(t, self.Tensor) and t.dtype is dtype and t.device == self.device and t.is_contiguous()):
+            return None
+        if (t.dim() != 1 or t.shape[0] < 1) if shape is None else t.shape != shape:
+            return None
+        return t.data_ptr()
+
+
 def check_chunk_args(cfg, device, q, k, v, cu_seqlens, out=None, accepted=None, slot_index=None):
     """dmc_chunk_attend (with out) and dmc_chunk_append: packed k, v [T, Hkv, d] and, for attention,
     q, out [T, Hq, d]; otherwise q [T, Hq] or [T, Hq, *] (only element 0 is read); cu_seqlens int32
@@ -603,10 +650,13 @@ class DMCChunk:
         self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
         self._ws_bytes = n
 
-    def _tokens(self, k):
-        if k.shape[0] > self.max_tokens:
-            _fail(f"{k.shape[0]} tokens, the workspace holds {self.max_tokens}")
-        return k.shape[0]
+        self._call = _PackedCall(cache.dtype, cache.device, cache.cfg.head_dim, 4 if cache.cfg.dtype == DMC_FP32 else 2)
+        self._cu_shape = (cache.cfg.batch + 1,)
+
+    def _tokens(self, T):
+        if T > self.max_tokens:
+            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
+        return T
 
     def attend(self, layer, q, k, v, cu_seqlens, out=None, stream=None):
         """Attention of packed new tokens q [T, Hq, d], k, v [T, Hkv, d] over the layer's cache and
@@ -614,21 +664,38 @@ class DMCChunk:
         stays as it is.  Returns out [T, Hq, d]; rows outside every chunk stay as they are."""
         if out is None:
             out = torch_empty_like(q)
-        check_chunk_args(self.cache.cfg, self.cache.device, q, k, v, cu_seqlens, out)
-        check(lib.dmc_chunk_attend(self.cache.handle, layer, _ptr(q), _strides(q), _ptr(k), _strides(k),
-                                   _ptr(v), _strides(v), _ptr(cu_seqlens), self._tokens(k),
-                                   self.max_chunk, _ptr(out), _strides(out), self._ws, self._ws_bytes,
-                                   _stream(stream)))
+        call, cfg = self._call, self.cache.cfg
+        T = call.rows(k)
+        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
+        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),)) if T > 0 else None
+        cu = call.array(cu_seqlens, call.i32, self._cu_shape)
+        if args is None or cu is None:
+            check_chunk_args(cfg, self.cache.device, q, k, v, cu_seqlens, out)
+            args, cu = _packed_args(q, k, v, out), cu_seqlens.data_ptr()
+        (qp, kp, vp, op), st = args
+        check(lib.dmc_chunk_attend(self.cache.handle, layer, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
+                                   self._tokens(T), self.max_chunk, op, byref(st, 48), self._ws,
+                                   self._ws_bytes, _stream(stream)))
         return out
 
     def append(self, layer, k, v, q, cu_seqlens, accepted=None, slot_index=None, stream=None):
         """Append the chunk (of row b only its first accepted[b] tokens) to the layer's cache; only
         q[..., 0] is read.  slot_index [T, Hkv] receives each token's slot, -1 if not appended."""
-        check_chunk_args(self.cache.cfg, self.cache.device, q, k, v, cu_seqlens, None, accepted, slot_index)
-        check(lib.dmc_chunk_append(self.cache.handle, layer, _ptr(k), _strides(k), _ptr(v), _strides(v),
-                                   _ptr(q), _strides(q), _ptr(cu_seqlens), _ptr(accepted),
-                                   self._tokens(k), self.max_chunk, _ptr(slot_index), self._ws,
-                                   self._ws_bytes, _stream(stream)))
+        call, cfg = self._call, self.cache.cfg
+        T = call.rows(k)
+        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
+        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ()) if T > 0 else None
+        cu = call.array(cu_seqlens, call.i32, self._cu_shape)
+        acc = None if accepted is None else call.array(accepted, call.i32, (cfg.batch,))
+        slots = None if slot_index is None else call.array(slot_index, call.i32, (T, Hkv))
+        if args is None or cu is None or (acc is None) != (accepted is None) or (slots is None) != (slot_index is None):
+            check_chunk_args(cfg, self.cache.device, q, k, v, cu_seqlens, None, accepted, slot_index)
+            args, cu = _packed_args(q, k, v), cu_seqlens.data_ptr()
+            acc, slots = _ptr(accepted), _ptr(slot_index)
+        (qp, kp, vp), st = args
+        check(lib.dmc_chunk_append(self.cache.handle, layer, kp, byref(st, 16), vp, byref(st, 32), qp, st, cu, acc,
+                                   self._tokens(T), self.max_chunk, slots, self._ws, self._ws_bytes,
+                                   _stream(stream)))
 
 
 def torch_empty_like(t):
@@ -692,8 +759,10 @@ def make_causal_config(num_q_heads, num_kv_heads, head_dim, dtype="bf16") -> Cau
                         DMC_FP32 if dtype in ("fp32", "float32") else DMC_BF16)
 
 
-def _strides(t):
-    return (c_int64 * 2)(t.stride(0), t.stride(1))
+def _packed_args(*tensors):
+    """Addresses and strides of packed tensors that have passed the full check."""
+    strides = [x for t in tensors for x in t.stride()[:2]]
+    return [t.data_ptr() for t in tensors], (c_int64 * len(strides))(*strides)
 
 
 class DMCCausal:
@@ -703,11 +772,14 @@ class DMCCausal:
     def __init__(self, cfg: CausalConfig, max_tokens, device="cuda"):
         import torch
         self.cfg = cfg
-        n = lib.dmc_causal_workspace_bytes(ctypes.byref(cfg), max_tokens)
+        self._cfg_ref = byref(cfg)
+        n = lib.dmc_causal_workspace_bytes(self._cfg_ref, max_tokens)
         if n == 0:
             raise DMCError(DMC_ERR_INVALID_ARG, last_error())
         self.max_tokens = max_tokens
         self.device = _cuda_device(device)
+        fp32 = cfg.dtype == DMC_FP32
+        self._call = _PackedCall(torch.float32 if fp32 else torch.bfloat16, self.device, cfg.head_dim, 4 if fp32 else 2)
         self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
         self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
         self._ws_bytes = n
@@ -721,10 +793,17 @@ class DMCCausal:
             out = torch_empty_like(q)
         if lse is None:
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse)
-        check(lib.dmc_causal_forward(ctypes.byref(self.cfg), _ptr(q), _strides(q), _ptr(k), _strides(k),
-                                     _ptr(v), _strides(v), _ptr(cu_seqlens), cu_seqlens.numel() - 1,
-                                     q.shape[0], _ptr(out), _strides(out), _ptr(lse), _stream(stream)))
+        call = self._call
+        T = call.rows(q)
+        Hq, Hkv = self.cfg.num_q_heads, self.cfg.num_kv_heads
+        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),)) if T > 0 else None
+        lp, cu = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32)
+        if args is None or lp is None or cu is None:
+            check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse)
+            args, lp, cu = _packed_args(q, k, v, out), lse.data_ptr(), cu_seqlens.data_ptr()
+        (qp, kp, vp, op), st = args
+        check(lib.dmc_causal_forward(self._cfg_ref, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
+                                     cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, _stream(stream)))
         return out, lse
 
     def backward(self, q, k, v, cu_seqlens, out, lse, dout, dq=None, dk=None, dv=None, stream=None):
@@ -732,13 +811,21 @@ class DMCCausal:
         dq = torch_empty_like(q) if dq is None else dq
         dk = torch_empty_like(k) if dk is None else dk
         dv = torch_empty_like(v) if dv is None else dv
-        check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse, dout, dq, dk, dv)
-        if q.shape[0] > self.max_tokens:
-            _fail(f"{q.shape[0]} tokens, the workspace holds {self.max_tokens}")
-        check(lib.dmc_causal_backward(ctypes.byref(self.cfg), _ptr(q), _strides(q), _ptr(k), _strides(k),
-                                      _ptr(v), _strides(v), _ptr(cu_seqlens), cu_seqlens.numel() - 1,
-                                      q.shape[0], _ptr(out), _strides(out), _ptr(lse), _ptr(dout),
-                                      _strides(dout), _ptr(dq), _strides(dq), _ptr(dk), _strides(dk),
-                                      _ptr(dv), _strides(dv), self._ws, self._ws_bytes,
-                                      _stream(stream)))
+        call = self._call
+        T = call.rows(q)
+        Hq, Hkv = self.cfg.num_q_heads, self.cfg.num_kv_heads
+        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv), (out, Hq), (dout, Hq)),
+                            ((dq, Hq), (dk, Hkv), (dv, Hkv))) if T > 0 else None
+        lp, cu = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32)
+        if args is None or lp is None or cu is None:
+            check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse, dout, dq, dk, dv)
+            args = _packed_args(q, k, v, out, dout, dq, dk, dv)
+            lp, cu = lse.data_ptr(), cu_seqlens.data_ptr()
+        if T > self.max_tokens:
+            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
+        (qp, kp, vp, op, dop, dqp, dkp, dvp), st = args
+        check(lib.dmc_causal_backward(self._cfg_ref, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
+                                      cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, dop, byref(st, 64),
+                                      dqp, byref(st, 80), dkp, byref(st, 96), dvp, byref(st, 112), self._ws,
+                                      self._ws_bytes, _stream(stream)))
         return dq, dk, dv

@@ -139,3 +139,30 @@ def test_config_struct_matches_header():
     body = re.search(r"typedef struct dmc_causal_config \{(.*?)\} dmc_causal_config;", text, re.S)
     names = re.findall(r"^\s*int32_t\s+([a-z_]+);", body.group(1), re.M)
     assert names == [f[0] for f in P.CausalConfig._fields_]
+
+
+def test_one_pass_checks_agree_with_the_full_ones():
+    """_PackedCall accepts what check_causal_args accepts (on its device) and returns its addresses;
+    whatever it declines goes to the full check."""
+    call = Bd._PackedCall(BF, torch.device("cpu"), D, 2)
+
+    def quick(a):
+        ins = [(a["q"], HQ), (a["k"], HKV), (a["v"], HKV), (a["out"], HQ), (a["dout"], HQ)]
+        return call.tensors(T, ins, [(a["dq"], HQ), (a["dk"], HKV), (a["dv"], HKV)])
+    a = _args()
+    ptrs, st = quick(a)
+    assert ptrs[0] == a["q"].data_ptr() and ptrs[-1] == a["dv"].data_ptr()
+    assert list(st) == [HQ * D, D, HKV * D, D, HKV * D, D] + [HQ * D, D] * 3 + [HKV * D, D] * 2
+    x = torch.zeros(T, HQ + 2 * HKV, D, dtype=BF)
+    a["q"], a["k"], a["v"] = x[:, :HQ], x[:, HQ:HQ + HKV], x[:, HQ + HKV:]
+    assert quick(a) is not None
+    for name, bad in (("q", torch.zeros(T, HQ, D)), ("k", torch.zeros(T, HQ, D, dtype=BF)),
+                      ("v", torch.zeros(T, HKV, D + 4, dtype=BF)[..., :D]), ("dq", a["q"]), ("dk", a["v"]),
+                      ("dout", torch.zeros(T, D, HQ, dtype=BF).transpose(1, 2)), ("dv", a["dk"]), ("out", None),
+                      ("k", torch.zeros(T * HKV * D + 8, dtype=BF)[1:1 + T * HKV * D].view(T, HKV, D))):
+        assert quick(dict(a, **{name: bad})) is None, name
+    assert call.array(a["lse"], call.f32, (T, HQ)) == a["lse"].data_ptr()
+    assert call.array(a["lse"], call.f32, (HQ, T)) is None and call.array(a["lse"], call.i32, (T, HQ)) is None
+    assert call.array(a["lse"].t(), call.f32, (HQ, T)) is None and call.array(3, call.f32, ()) is None
+    assert call.array(a["cu_seqlens"], call.i32) and call.array(a["lse"], call.f32) is None
+    assert call.array(a["cu_seqlens"][:0], call.i32) is None and call.rows([1, 2]) == 0
