@@ -875,8 +875,28 @@ static dmc_status check_packed_counts(int32_t num_seqs, int32_t total) {
   return DMC_OK;
 }
 
-static size_t causal_workspace(const dmc_causal_config &c, int32_t total) {
+static size_t causal_stats_bytes(const dmc_causal_config &c, int32_t total) {
   return align_up(size_t(c.num_q_heads) * (size_t(total) + 32) * 8, 256);
+}
+// Bytes of the parts of dK (and of dV) of up to `total` tokens: what the fewest
+// compute-unit-filling parts of any number of sequences take.
+static size_t causal_part_bytes(const dmc_causal_config &c, int32_t total, int parts) {
+  return parts > 1 ? align_up(size_t(parts) * total * c.num_kv_heads * c.head_dim * 4, 256) : 0;
+}
+constexpr int kWorkspaceUnits = 256;   // compute units that the parts are planned for
+static int causal_parts(const dmc_causal_config &c, int32_t seqs, int32_t total) {
+  return dmc::causal_key_parts(c.dtype == DMC_FP32 ? 4 : 2, c.num_q_heads, c.num_kv_heads, seqs, total, kWorkspaceUnits);
+}
+static size_t causal_workspace(const dmc_causal_config &c, int32_t total) {
+  // fewer tokens may be cut into more parts, but parts x tiles stays below 4 units'
+  // worth, with 128 tokens in a tile (and 16 parts of what one tile holds)
+  size_t most = 0;
+  for (int parts = 2; parts <= dmc::kMaxKeyParts; ++parts) {
+    const int64_t tiles = int64_t(4) * kWorkspaceUnits / (int64_t(parts) * c.num_kv_heads);   // (of one head)
+    const int64_t tokens = std::min<int64_t>(total, tiles * 128);
+    if (tokens > 0) most = std::max(most, causal_part_bytes(c, static_cast<int32_t>(tokens), parts));
+  }
+  return causal_stats_bytes(c, total) + (c.dtype == DMC_BF16 ? 2 * most : 0);
 }
 
 static void copy_strides(int64_t (&dst)[2], const int64_t *src) {
@@ -891,6 +911,8 @@ static void causal_params(const dmc_causal_config &c, const int32_t *cu, int32_t
   p->hq = c.num_q_heads;
   p->hkv = c.num_kv_heads;
   p->stat_stride = int64_t(total) + 32;
+  p->compute_units = kWorkspaceUnits;
+  p->parts = 1;
   p->scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(c.head_dim)));
 }
 
@@ -990,7 +1012,11 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, cons
   p.dq = dq;
   p.dk = dk;
   p.dv = dv;
-  p.stats = static_cast<float *>(ws);
+  p.parts = causal_parts(*cfg, num_seqs, total);
+  char *w = static_cast<char *>(ws);
+  p.stats = reinterpret_cast<float *>(w);
+  p.part_k = reinterpret_cast<float *>(w + causal_stats_bytes(*cfg, total));
+  p.part_v = reinterpret_cast<float *>(w + causal_stats_bytes(*cfg, total) + causal_part_bytes(*cfg, total, p.parts));
   copy_strides(p.qs, q_strides);
   copy_strides(p.ks, k_strides);
   copy_strides(p.vs, v_strides);

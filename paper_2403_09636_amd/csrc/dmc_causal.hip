@@ -17,6 +17,7 @@
 // tiles start at the sequence's first token, so that a wave's 32 columns meet
 // the diagonal in exactly one block.  Rows past a sequence's end are its last
 // row again (in bounds whatever lies behind) with weight 0.
+#include <algorithm>
 #include <type_traits>
 
 #include "dmc_mfma.h"
@@ -28,34 +29,99 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kTileShift = 7, kTile = 1 << kTileShift;     // bf16: tokens per workgroup
 constexpr int kTileShift32 = 5, kTile32 = 1 << kTileShift32;   // fp32
 
-// Head and tile index of a workgroup.  Heads are dealt to the XCDs (workgroup
-// i runs on XCD i mod 8) in runs where their count allows, so that a kv head's
-// keys and values stay in one L2; tiles in descending order, a sequence's
-// heaviest first.
-__device__ __forceinline__ void tile_of_block(const CausalParams &p, int ntiles, bool descending, int &head, int &idx) {
+// Head (of `heads`) and rank among the tiles of a workgroup.  Heads are dealt to
+// the XCDs (workgroup i runs on XCD i mod 8) in runs where their count allows, so
+// that a kv head's keys and values stay in one L2.
+__device__ __forceinline__ void head_of_block(int heads, int &head, int &rank) {
   const int bid = blockIdx.x;
-  int rank;
-  if ((p.hq & 7) == 0) {
-    const int per = p.hq >> 3, r = bid >> 3;
+  if ((heads & 7) == 0) {
+    const int per = heads >> 3, r = bid >> 3;
     rank = r / per;
     head = (bid & 7) * per + r - rank * per;
   } else {
-    rank = bid / p.hq;
-    head = bid - rank * p.hq;
+    rank = bid / heads;
+    head = bid - rank * heads;
   }
-  idx = descending ? ntiles - 1 - rank : rank;
 }
-// The same for tiles of keys: heads are kv heads, tiles in ascending order.
-__device__ __forceinline__ void key_tile_of_block(const CausalParams &p, int &head, int &idx) {
-  const int bid = blockIdx.x;
-  if ((p.hkv & 7) == 0) {
-    const int per = p.hkv >> 3, r = bid >> 3;
-    idx = r / per;
-    head = (bid & 7) * per + r - idx * per;
-  } else {
-    idx = bid / p.hkv;
-    head = bid - idx * p.hkv;
+
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row_sum<32>(x);
+  return x + __shfl_xor(x, 32, 64);
+}
+
+// The tile of a rank in descending order of length: tile k (from 1) of a query
+// kernel's sequence takes k tiles' worth of blocks, in a key kernel (REVERSED)
+// the k-th from its end does; heavy tiles that start last leave most of the chip
+// idle.  With N(l) tiles of length l or more, found by bisection over l: the length
+// of rank r is the largest l with N(l) > r, and the rank counts from N(l + 1) over
+// the sequences that have such a tile.
+constexpr int kSortSeqs = 256;   // sequences a wave holds the lengths of, four to a lane
+template <bool REVERSED>
+__device__ __forceinline__ PackedTile sorted_tile(const int32_t *cu, int seqs, int total, int rank, int shift) {
+  constexpr int kPer = kSortSeqs / 64;
+  const int lane = threadIdx.x & 63;
+  int start[kPer], tiles[kPer], n[kPer];
+  int most = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int b = j * 64 + lane;
+    const bool here = b < seqs;
+    start[j] = clamp_token(cu[here ? b : 0], total);
+    const int end = clamp_token(cu[here ? b + 1 : 0], total);
+    n[j] = here && end > start[j] ? end - start[j] : 0;
+    tiles[j] = (n[j] + (1 << shift) - 1) >> shift;
+    most = max(most, tiles[j]);
   }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
+  // (counts below 2^24: exact in floats)
+  auto at_least = [&](int l) {
+    int x = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x += max(tiles[j] - l + 1, 0);
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(wave_sum(static_cast<float>(x))));
+  };
+  PackedTile t{0, 0, 0, -1};
+  int lo = 1, hi = __builtin_amdgcn_readfirstlane(most) + 1;   // N(lo) > rank >= N(hi), if at all
+  if (at_least(1) <= rank) return t;
+  int above = 0;   // N(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1, c = at_least(mid);
+    if (c > rank) {
+      lo = mid;
+    } else {
+      hi = mid;
+      above = c;
+    }
+  }
+  int k = rank - above;   // among the sequences with a tile of length lo
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const unsigned long long has = __ballot(tiles[j] >= lo);
+    const int c = __popcll(has);
+    if (t.tile < 0 && k < c) {
+      const bool mine = ((has >> lane) & 1) && __popcll(has & ((1ull << lane) - 1)) == k;
+      const int src = 63 - __clzll(static_cast<long long>(__ballot(mine)));
+      t.seq = j * 64 + src;
+      t.start = __builtin_amdgcn_readlane(start[j], src);
+      t.n = __builtin_amdgcn_readlane(n[j], src);
+      t.tile = REVERSED ? __builtin_amdgcn_readlane(tiles[j], src) - lo : lo - 1;
+    }
+    k -= c;
+  }
+  t.seq = __builtin_amdgcn_readfirstlane(t.seq);
+  t.start = __builtin_amdgcn_readfirstlane(t.start);
+  t.n = __builtin_amdgcn_readfirstlane(t.n);
+  t.tile = __builtin_amdgcn_readfirstlane(t.tile);
+  return t;
+}
+
+// A workgroup's tile: by rank in descending length where the launch asks for it,
+// else in the order of the sequences (last ones first for queries).
+template <bool REVERSED>
+__device__ __forceinline__ PackedTile tile_of_rank(const CausalParams &p, int rank, int ntiles, int shift) {
+  if (p.sorted) return sorted_tile<REVERSED>(p.cu, p.seqs, p.total, rank, shift);
+  return packed_tile(p.cu, p.seqs, p.total, REVERSED ? rank : ntiles - 1 - rank, shift);
 }
 
 // Row `token`, head `h` of a strided tensor of ES-byte elements.
@@ -91,9 +157,9 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
     else if constexpr (S == 2) return ring2;
     else return ring3;
   };
-  int h, idx;
-  tile_of_block(p, ntiles, true, h, idx);
-  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift);
+  int h, rank;
+  head_of_block(p.hq, h, rank);
+  const PackedTile pt = tile_of_rank<false>(p, rank, ntiles, kTileShift);
   const int n = pt.n;
   if (pt.tile < 0 || pt.tile * kTile >= n) return;
 
@@ -307,11 +373,11 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
         for (int rr = 0; rr < 16; ++rr)
           if (score_row(rr) > tr) sv[rr] = neg_inf();
       }
-      // dP^T = V . dO^T, with P = exp2(S - L) formed between its products and
-      // the transposed keys read, then dS^T = P^T (dP^T - D).
+      // dP^T = V . dO^T, with P = exp2(S - L) formed between its products, then
+      // dS^T = P^T (dP^T - D).
       f32x16_t dp = f32x16_t{};
       float pe[16];
-      uint4 kt[NTL][2];
+      uint4 kt[KS];   // transposed keys
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         if (ks + 3 < KS) vr[(ks + 3) & 3] = *reinterpret_cast<const uint4 *>(vd + kaddr[ks + 3]);
@@ -322,17 +388,13 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
           pe[i] = fast_exp2(fmaf(sv[i], sl2, -Lc));
           computed_here(pe[i]);
         }
-        kt[ks >> 1][ks & 1] = tr_operand<RB>(kd, traddr[ks >> 1], ks & 1);
+        kt[ks] = tr_operand<RB>(kd, traddr[ks >> 1], ks & 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (diagonal) {   // (a masked row's dP may be anything)
 #pragma unroll
         for (int rr = 0; rr < 16; ++rr)
           if (score_row(rr) > tr) dp[rr] = Dc;
-#pragma unroll
-        for (int i = 0; i < NTL; ++i)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(kt[i][kk]);
       }
       uint4 sb[2];
 #pragma unroll
@@ -345,10 +407,12 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
         }
         sb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
       }
+      if (diagonal) {
 #pragma unroll
-      for (int i = 0; i < NTL; ++i)
+        for (int j = 0; j < 2 * NTL; ++j) left_out |= leave_out_nonfinite(kt[j]);
+      }
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(kt[i][kk], sb[kk], acc[i]);
+      for (int j = 0; j < 2 * NTL; ++j) acc[j >> 1] = mfma_32x32x16(kt[j], sb[j & 1], acc[j >> 1]);
     };
     for (int kb = 0; kb < nblk; kb += kSt) {
       step(std::integral_constant<int, 0>{}, kb);
@@ -409,9 +473,9 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
     else if constexpr (S == 1) return ring1;
     else return ring2;
   };
-  int g, idx;
-  key_tile_of_block(p, g, idx);
-  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift);
+  int g, rank;
+  head_of_block(p.hkv, g, rank);
+  const PackedTile pt = tile_of_rank<true>(p, rank, 0, kTileShift);
   const int n = pt.n;
   if (pt.tile < 0 || pt.tile * kTile >= n) return;
 
@@ -436,8 +500,9 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
     }
   }
 
-  const int qb0 = pt.tile * (kTile / 32), qb1 = (n + 31) >> 5;   // row blocks that see the tile
-  const int per_head = qb1 - qb0, nblk = G * per_head;
+  // Row blocks that see the tile, of every head in turn; this workgroup's part of them.
+  const int qb0 = pt.tile * (kTile / 32), qb1 = (n + 31) >> 5, per_head = qb1 - qb0;
+  const int part = blockIdx.y, lo = G * per_head * part / p.parts, nblk = G * per_head * (part + 1) / p.parts - lo;
   const uint32_t qst = static_cast<uint32_t>(p.qs[0] * 2), dst_ = static_cast<uint32_t>(p.dos[0] * 2);
   uint32_t qrow[DPW], qchunk[DPW];
 #pragma unroll
@@ -451,12 +516,12 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
   // rows' L, lanes 32..63 their D (rows past the sequence: the next one's, or
   // the workspace's padding, not used).
   const uint32_t soff = uint32_t(col) * 8 + uint32_t(hb) * 4;
-  int ih = g * G, iq = qb0;   // next block to issue: head, row block
+  int ih = g * G + lo / per_head, iq = qb0 + lo % per_head, left = nblk;   // next block to issue: head, row block
   // Every call issues 2 DPW + 1 transfers per wave; those past the last block
   // are switched off.
   auto issue = [&](auto st_c) {
-    const bool on = ih < g * G + G;
-    const int hh = on ? ih : g * G;
+    const bool on = left-- > 0;
+    const int hh = min(ih, g * G + G - 1);
     unsigned char *dst = slot(st_c);
     const char *qp = uniform_ptr(row_at<2>(p.q, p.qs, pt.start + iq * 32, hh));
     const char *dp = uniform_ptr(row_at<2>(p.dout, p.dos, pt.start + iq * 32, hh));
@@ -470,7 +535,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
       dma16_s(cdst + BLK, dp, row * dst_ + qchunk[i], on);
     }
     dma_so<kCachePolicyDefault, 4>(dst + 2 * BLK + wave * 256, sp, soff, on);
-    if (on && ++iq == qb1) {
+    if (++iq == qb1) {
       iq = qb0;
       ++ih;
     }
@@ -486,7 +551,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
 #pragma unroll
   for (int i = 0; i < NTL; ++i) acc[i] = f32x16_t{};
   bool left_out = false;
-  int cq = qb0;   // row block of the next step
+  int cq = iq;   // row block of the next step
 
   auto step = [&](auto stage_c, int kb) {
     constexpr int ST = decltype(stage_c)::value;
@@ -521,11 +586,10 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
       __builtin_amdgcn_sched_barrier(0);
     }
     float pe[16];
-    uint4 xt[NTL][2];   // transposed rows of the last product: dO (dV), Q (dK)
-    const char *xd = PART == 1 ? dd : qd;
+    const char *xd = PART == 1 ? dd : qd;   // rows of the last product: dO (dV), Q (dK)
+    uint4 xt[4];                            // them transposed, read three products ahead
     f32x16_t dp = f32x16_t{};
     if constexpr (PART == 2) {
-      statistics(sl + 32, Dr);
       uint4 dr[4];
 #pragma unroll
       for (int i = 0; i < 3; ++i) dr[i] = *reinterpret_cast<const uint4 *>(dd + raddr[i]);
@@ -540,14 +604,13 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
           pe[i] = fast_exp2(fmaf(sc[i], sl2, -Lr[i]));
           computed_here(pe[i]);
         }
-        xt[ks >> 1][ks & 1] = tr_operand<RB>(xd, traddr[ks >> 1], ks & 1);
+        if (ks == KS - 4) statistics(sl + 32, Dr);
+        if (ks >= KS - 3) xt[ks - (KS - 3)] = tr_operand<RB>(xd, traddr[(ks - (KS - 3)) >> 1], (ks - (KS - 3)) & 1);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < NTL; ++i)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) xt[i][kk] = tr_operand<RB>(xd, traddr[i], kk);
+      for (int j = 0; j < 3; ++j) xt[j] = tr_operand<RB>(xd, traddr[j >> 1], j & 1);
 #pragma unroll
       for (int i = 0; i < 16; ++i) pe[i] = fast_exp2(fmaf(sc[i], sl2, -Lr[i]));
     }
@@ -560,10 +623,6 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
         pe[rr] = vis ? pe[rr] : 0.0f;
         if constexpr (PART == 2) dp[rr] = vis ? dp[rr] - Dr[rr] : 0.0f;
       }
-#pragma unroll
-      for (int i = 0; i < NTL; ++i)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(xt[i][kk]);
     } else if constexpr (PART == 2) {
 #pragma unroll
       for (int rr = 0; rr < 16; ++rr) dp[rr] -= Dr[rr];
@@ -580,10 +639,16 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
       }
       wb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    auto product = [&](auto masked_c) {
 #pragma unroll
-    for (int i = 0; i < NTL; ++i)
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(xt[i][kk], wb[kk], acc[i]);
+      for (int j = 0; j < 2 * NTL; ++j) {
+        if (j + 3 < 2 * NTL) xt[(j + 3) & 3] = tr_operand<RB>(xd, traddr[(j + 3) >> 1], (j + 3) & 1);
+        if constexpr (decltype(masked_c)::value) left_out |= leave_out_nonfinite(xt[j & 3]);
+        acc[j >> 1] = mfma_32x32x16(xt[j & 3], wb[j & 1], acc[j >> 1]);
+      }
+    };
+    if (masked) product(std::true_type{});
+    else product(std::false_type{});
   };
 
   issue(std::integral_constant<int, 0>{});
@@ -597,20 +662,30 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
   }
   if (__any(left_out)) {   // the masked blocks of every head again
     const void *base = PART == 1 ? p.dout : p.q;
-    for (int hh = g * G; hh < g * G + G; ++hh)
-      for (int qb = qb0; qb < qb1; ++qb) {
-        const int rb = qb * 32;
-        if (rb < s0 || (rb != s0 && rb + 32 <= n)) continue;
-        add_nonfinite<D, PART == 2>(
+    for (int i = lo; i < lo + nblk; ++i) {
+      const int hh = g * G + i / per_head, rb = (qb0 + i % per_head) * 32;
+      if (rb < s0 || (rb != s0 && rb + 32 <= n)) continue;
+      add_nonfinite<D, PART == 2>(
             acc,
-            [&](int i, int e) {
-              return row4(row_at<2>(base, PART == 1 ? p.dos : p.qs, pt.start + min(rb + i, n - 1), hh), e);
-            },
-            [&](int i) { return kv_ok && rb + i >= js && rb + i < n; }, hb);
-      }
+          [&](int r, int e) {
+            return row4(row_at<2>(base, PART == 1 ? p.dos : p.qs, pt.start + min(rb + r, n - 1), hh), e);
+          },
+          [&](int r) { return kv_ok && rb + r >= js && rb + r < n; }, hb);
+    }
   }
   if (!kv_ok) return;
   const float scale = PART == 1 ? 1.0f : sl2 / kLog2e;
+  if (p.parts > 1) {   // this part's share, in fp32
+    float *rec = (PART == 1 ? p.part_v : p.part_k) + ((int64_t(part) * p.total + pt.start + js) * p.hkv + g) * D;
+#pragma unroll
+    for (int i = 0; i < NTL; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4 *>(rec + 32 * i + 8 * j + 4 * hb) =
+            make_float4(acc[i][4 * j] * scale, acc[i][4 * j + 1] * scale, acc[i][4 * j + 2] * scale,
+                        acc[i][4 * j + 3] * scale);
+    return;
+  }
   char *orow = const_cast<char *>(PART == 1 ? row_at<2>(p.dv, p.dvs, pt.start + js, g)
                                             : row_at<2>(p.dk, p.dks, pt.start + js, g));
 #pragma unroll
@@ -621,6 +696,31 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
       const uint32_t hi = cvt_pk_bf16(acc[i][4 * j + 2] * scale, acc[i][4 * j + 3] * scale);
       *reinterpret_cast<uint2 *>(orow + (32 * i + 8 * j + 4 * hb) * 2) = make_uint2(lo, hi);
     }
+}
+
+// The parts of dK and dV put together, in their order: one thread per 4 elements of
+// a row of a kv head, for the tokens inside the sequences.
+template <int D>
+__global__ __launch_bounds__(kThreads) void causal_parts_kernel(CausalParams p) {
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int first = clamp_token(p.cu[0], p.total), end = clamp_token(p.cu[p.seqs], p.total);
+  const int64_t row = i / (D / 4);
+  const int e = static_cast<int>(i - row * (D / 4)) * 4;
+  const int64_t token = row / p.hkv;
+  const int g = static_cast<int>(row - token * p.hkv);
+  if (token < first || token >= end) return;
+  const int64_t step = int64_t(p.total) * p.hkv * D;
+  float4 k = make_float4(0, 0, 0, 0), v = k;
+  for (int part = 0; part < p.parts; ++part) {
+    const float4 a = *reinterpret_cast<const float4 *>(p.part_k + part * step + row * D + e);
+    const float4 b = *reinterpret_cast<const float4 *>(p.part_v + part * step + row * D + e);
+    k.x += a.x; k.y += a.y; k.z += a.z; k.w += a.w;
+    v.x += b.x; v.y += b.y; v.z += b.z; v.w += b.w;
+  }
+  *reinterpret_cast<uint2 *>(const_cast<char *>(row_at<2>(p.dk, p.dks, token, g)) + e * 2) =
+      make_uint2(cvt_pk_bf16(k.x, k.y), cvt_pk_bf16(k.z, k.w));
+  *reinterpret_cast<uint2 *>(const_cast<char *>(row_at<2>(p.dv, p.dvs, token, g)) + e * 2) =
+      make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
 }
 
 // ---------------------------------------------------------------------------
@@ -636,9 +736,9 @@ __global__ __launch_bounds__(kThreads) void causal_query_f32_kernel(CausalParams
   constexpr int NT = F::NT;
   __shared__ __align__(16) float s_acc[F::kArea];
   __shared__ float s_m[kWaves * 32], s_l[kWaves * 32];
-  int h, idx;
-  tile_of_block(p, ntiles, true, h, idx);
-  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift32);
+  int h, rank;
+  head_of_block(p.hq, h, rank);
+  const PackedTile pt = tile_of_rank<false>(p, rank, ntiles, kTileShift32);
   const int n = pt.n, a = pt.tile * kTile32;
   if (pt.tile < 0 || a >= n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hb = lane >> 5;
@@ -765,9 +865,9 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
   constexpr int NT = F::NT;
   constexpr bool DV = PART != 2, DK = PART != 1;
   __shared__ __align__(16) float s_acc[F::kArea];
-  int g, idx;
-  key_tile_of_block(p, g, idx);
-  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, idx, kTileShift32);
+  int g, rank;
+  head_of_block(p.hkv, g, rank);
+  const PackedTile pt = tile_of_rank<true>(p, rank, 0, kTileShift32);
   const int n = pt.n, s0 = pt.tile * kTile32;
   if (pt.tile < 0 || s0 >= n) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hb = lane >> 5;
@@ -875,12 +975,28 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
   }
 }
 
+// Whether tiles go out in descending length: where there are more of them than run
+// at once, two workgroups per compute unit (finding a rank's tile takes about a
+// microsecond).  Query tiles only where an XCD's share of the keys and values fits
+// its 4 MB L2: sequences then run side by side rather than one after another.  us,
+// in the order of the sequences -> by length: backward, 6 sequences up to 4096
+// tokens, 32/8 heads, dV 718 -> 616, dK 911 -> 766; forward of 16 x 500 tokens,
+// 8 heads, d = 64, 20.7 -> 16.3, but of 4 x 4096, 32 heads, 582 -> 611.
+bool sort_tiles(const CausalParams &p, int64_t workgroups) {
+  return p.seqs <= kSortSeqs && workgroups > 2 * p.compute_units;
+}
+bool sort_queries(const CausalParams &p, int64_t workgroups, int row_bytes) {
+  const int64_t heads = (p.hkv + 7) / 8;
+  return sort_tiles(p, workgroups) && heads * p.total * 2 * row_bytes <= (4 << 20);
+}
+
 template <int D>
-hipError_t causal_forward(int elem_bytes, const CausalParams &p, hipStream_t s) {
+hipError_t causal_forward(int elem_bytes, CausalParams p, hipStream_t s) {
   const int shift = elem_bytes == 2 ? kTileShift : kTileShift32;
   const int ntiles = (p.total >> shift) + p.seqs;
   const int64_t blocks = int64_t(ntiles) * p.hq;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  p.sorted = sort_queries(p, blocks, D * elem_bytes);
   if (elem_bytes == 2)
     hipLaunchKernelGGL((causal_query_kernel<D, 0>), dim3(unsigned(blocks)), dim3(kThreads), 0, s, p, ntiles);
   else
@@ -889,17 +1005,24 @@ hipError_t causal_forward(int elem_bytes, const CausalParams &p, hipStream_t s) 
 }
 
 template <int D>
-hipError_t causal_backward(int elem_bytes, const CausalParams &p, hipStream_t s) {
+hipError_t causal_backward(int elem_bytes, CausalParams p, hipStream_t s) {
   const int shift = elem_bytes == 2 ? kTileShift : kTileShift32;
   const int ntiles = (p.total >> shift) + p.seqs;
   if (int64_t(ntiles) * p.hq > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const dim3 queries(unsigned(ntiles) * p.hq), keys(unsigned(ntiles) * p.hkv), threads(kThreads);
+  const dim3 queries(unsigned(ntiles) * p.hq), threads(kThreads);
+  const dim3 keys(unsigned(ntiles) * p.hkv, p.parts);
+  p.sorted = sort_queries(p, queries.x, D * elem_bytes);
   if (elem_bytes == 2) {
     hipLaunchKernelGGL((causal_query_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
+    p.sorted = sort_tiles(p, int64_t(keys.x) * keys.y);
     hipLaunchKernelGGL((causal_key_kernel<D, 1>), keys, threads, 0, s, p);
     hipLaunchKernelGGL((causal_key_kernel<D, 2>), keys, threads, 0, s, p);
+    if (p.parts > 1)
+      hipLaunchKernelGGL((causal_parts_kernel<D>), dim3(unsigned((int64_t(p.total) * p.hkv * (D / 4) + kThreads - 1) / kThreads)),
+                         threads, 0, s, p);
   } else {
     hipLaunchKernelGGL((causal_query_f32_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
+    p.sorted = sort_tiles(p, keys.x);
     if constexpr (D == 64) {
       hipLaunchKernelGGL((causal_key_f32_kernel<D, 0>), keys, threads, 0, s, p);
     } else {
@@ -911,6 +1034,13 @@ hipError_t causal_backward(int elem_bytes, const CausalParams &p, hipStream_t s)
 }
 
 }  // namespace
+
+int causal_key_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total, int compute_units) {
+  if (elem_bytes != 2 || seqs < 1) return 1;
+  const int64_t tiles = (total >> kTileShift) + 1, chain = (hq / hkv) * (total / seqs / 32);
+  const int64_t parts = std::min<int64_t>(4 * compute_units / (tiles * hkv), chain / 8);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, kMaxKeyParts)));
+}
 
 hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s) {
   return head_dim == 128 ? causal_forward<128>(elem_bytes, p, s) : causal_forward<64>(elem_bytes, p, s);

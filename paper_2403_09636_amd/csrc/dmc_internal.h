@@ -270,9 +270,17 @@ struct CausalParams {
   const int32_t *cu;             // [seqs + 1]
   float *stats;                  // workspace: [hq][stat_stride][2], per row log2-sum-exp, sum(dout * out)
   int64_t stat_stride;           // total + 32
+  float *part_k, *part_v;        // workspace, with several parts: [parts][total][hkv][d] of dK and dV
   float scale_log2;              // log2(e) / sqrt(d)
-  int32_t seqs, total, hq, hkv;
+  int32_t seqs, total, hq, hkv, compute_units;
+  int32_t parts;                 // parts that a key tile's rows are cut into
+  bool sorted;                   // tiles by descending length (set per launch)
 };
+// Parts of the key kernels' rows: where their tiles are too few for the chip, a
+// tile's (head, row block) list is shared out to several workgroups, eight blocks
+// or more each by the average sequence, whose sums meet in a last pass.
+constexpr int kMaxKeyParts = 16;
+int causal_key_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total, int compute_units);
 hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 hipError_t launch_causal_backward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 

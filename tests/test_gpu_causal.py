@@ -268,3 +268,20 @@ def test_boundaries_out_of_range(torch_cuda):
     att.forward(q.cuda(), k.cuda(), v.cuda(), cu, out=out, lse=lse)
     att.backward(q.cuda(), k.cuda(), v.cuda(), cu, out, lse, dout.cuda())
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d", [
+    # enough tiles to go out by length (more than two per compute unit), and key tiles cut into parts
+    ([130, 257, 1, 0, 640, 128, 129, 300], 64, 32, 64), ([700], 8, 1, 128), ([300, 280], 6, 2, 64),
+    ([40] * 100 + [500] + [0] * 3 + [7] * 90, 16, 8, 64)])
+def test_orders_and_parts(torch_cuda, lens, hq, hkv, d):
+    """Launch orders and partial sums of key tiles: against float64 on sampled heads, all rows."""
+    import paper_2403_09636_amd as P
+    q, k, v, dout = make(lens, hq, hkv, d, "bf16")
+    got = run(P, q, k, v, dout, lens)
+    G = hq // hkv
+    for g in sorted({0, hkv // 2, hkv - 1}):
+        heads = slice(g * G, g * G + G)
+        want = causal(q[:, heads], k[:, g:g + 1], v[:, g:g + 1], lens, dout[:, heads])
+        for name, x in got.items():
+            check(x[:, g:g + 1] if name in ("dk", "dv") else x[:, heads], want[name], f"{name} of kv head {g}")
