@@ -1037,8 +1037,8 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, cons
 
 // Workspace of the chunk calls: byte offsets of its sections (256-byte aligned).
 struct ChunkLayout {
-  size_t state_k, state_v, closed_k, closed_v, before, starts, carry, visible, piece_base, pieces, record_base, old_len,
-      old_z, partials, total;
+  size_t state_k, state_v, closed_k, closed_v, before, starts, carry, visible, unit_order, piece_base, pieces, record_base,
+      old_len, old_z, partials, total;
 };
 
 // Attention pieces beyond one per column tile, and the fewest 32-row blocks of
@@ -1069,7 +1069,8 @@ static ChunkLayout chunk_layout(const dmc_cache *c, int32_t total) {
   L.starts = take(H * blocks64 * 4);
   L.carry = take(H * blocks64 * dmc::carry_stride(cfg.head_dim) * 4);
   L.visible = take(U * 4);
-  L.piece_base = take((U + 1) * 4);
+  L.unit_order = take((U + 7) / 8 * 8 * 4);
+  L.piece_base = take(((U + 7) / 8 + 1) * 8 * 4);
   L.pieces = take(U * 4);
   L.record_base = take(U * 4);
   L.old_len = take(U * 4);
@@ -1148,6 +1149,7 @@ static dmc_status chunk_params(const dmc_cache *c, int32_t layer, const void *k,
   p.starts = reinterpret_cast<int32_t *>(w + W.starts);
   p.carry = reinterpret_cast<float *>(w + W.carry);
   p.visible = reinterpret_cast<int32_t *>(w + W.visible);
+  p.unit_order = reinterpret_cast<int32_t *>(w + W.unit_order);
   p.piece_base = reinterpret_cast<int32_t *>(w + W.piece_base);
   p.pieces = reinterpret_cast<int32_t *>(w + W.pieces);
   p.record_base = reinterpret_cast<int32_t *>(w + W.record_base);

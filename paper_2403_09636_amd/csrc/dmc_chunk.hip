@@ -419,16 +419,30 @@ __device__ __forceinline__ UnitPlan unit_plan(const ChunkParams &p, int u) {
   return x;
 }
 
+// Units are dealt to the XCDs (each with its own L2, so that a unit's tiles share
+// its slots there) in descending order of their blocks, back and forth: rows and
+// heads differ by orders of magnitude (a ragged batch of prompts, heads of other
+// compression).  The order comes from a counting sort by cost, eight buckets to a
+// factor of two.
+constexpr int kCostBuckets = 64 * 8;
+__device__ __forceinline__ int cost_bucket(float cost) {   // (most expensive first)
+  const int e = static_cast<int>(__float_as_uint(cost + 1.0f) >> 20) - (127 << 3);
+  return kCostBuckets - 1 - min(e, kCostBuckets - 1);
+}
+
 __device__ void plan_pieces(const ChunkParams &p) {
   __shared__ long long s_total[kWaves];
-  __shared__ int s_count[kWaves], s_split[kWaves];
+  __shared__ int s_split[kWaves], s_bucket[kCostBuckets], s_sum[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (p.units + kThreads - 1) / kThreads;
   const int i0 = min(tid * per, p.units), i1 = min(i0 + per, p.units);
+  for (int i = tid; i < kCostBuckets; i += kThreads) s_bucket[i] = 0;
+  __syncthreads();
   long long total = 0;
   for (int u = i0; u < i1; ++u) {
     const UnitPlan x = unit_plan(p, u);
     total += static_cast<long long>(x.tiles) * x.blocks;
+    atomicAdd(&s_bucket[cost_bucket(static_cast<float>(x.tiles) * x.blocks)], 1);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
@@ -447,43 +461,72 @@ __device__ void plan_pieces(const ChunkParams &p) {
     const long long want = (total + p.piece_budget - 1) / p.piece_budget;
     size = static_cast<int>(want > p.piece_min ? min(want, 1ll << 30) : p.piece_min);
   }
-  // Units of several pieces have floor(blocks / size) >= 2 of them per tile, so
-  // that their pieces, which have a record each, are at most the budget.
-  int mine = 0, split = 0;
+  // Bucket sizes -> first positions (two to a thread).
+  static_assert(kCostBuckets == 2 * kThreads, "two buckets a thread");
+  const int c0 = s_bucket[2 * tid], c1 = s_bucket[2 * tid + 1];
+  int ends = c0 + c1;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(ends, o, 64);
+    if (lane >= o) ends += t;
+  }
+  if (lane == 63) s_sum[wave] = ends;
+  // Pieces per tile.  Units of several have floor(blocks / size) >= 2 of them per
+  // tile, so that their pieces, which have a record each, are at most the budget.
+  int split = 0;
   for (int u = i0; u < i1; ++u) {
     const UnitPlan x = unit_plan(p, u);
     const int np = max(1, x.blocks / size);
     p.pieces[u] = np;
-    mine += x.tiles * np;
     split += np > 1 ? x.tiles * np : 0;
   }
-  int incl = mine, incs = split;
+  int incs = split;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(incl, o, 64), ts = __shfl_up(incs, o, 64);
-    if (lane >= o) {
-      incl += t;
-      incs += ts;
-    }
+    const int ts = __shfl_up(incs, o, 64);
+    if (lane >= o) incs += ts;
   }
-  if (lane == 63) {
-    s_count[wave] = incl;
-    s_split[wave] = incs;
-  }
+  if (lane == 63) s_split[wave] = incs;
   __syncthreads();
-  int run = incl - mine, rec = incs - split;
+  int first = ends - c0 - c1, rec = incs - split;
   for (int w = 0; w < wave; ++w) {
-    run += s_count[w];
+    first += s_sum[w];
     rec += s_split[w];
   }
+  s_bucket[2 * tid] = first;
+  s_bucket[2 * tid + 1] = first + c0;
+  __syncthreads();
+  const int row = (p.units + 7) >> 3;   // units of an XCD
   for (int u = i0; u < i1; ++u) {
-    const int np = p.pieces[u], n = unit_plan(p, u).tiles * np;
-    p.piece_base[u] = run;
+    const UnitPlan x = unit_plan(p, u);
+    const int at = atomicAdd(&s_bucket[cost_bucket(static_cast<float>(x.tiles) * x.blocks)], 1);
+    const int k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7, np = p.pieces[u];
+    p.unit_order[xcd * row + k] = u;
+    p.piece_base[xcd * (row + 1) + k + 1] = x.tiles * np;
     p.record_base[u] = rec;
-    run += n;
-    rec += np > 1 ? n : 0;
+    rec += np > 1 ? x.tiles * np : 0;
   }
-  if (tid == kThreads - 1) p.piece_base[p.units] = run;
+  if (tid < 8 * row - p.units) {   // places without a unit, in the last line
+    const int at = p.units + tid, k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7;
+    p.unit_order[xcd * row + k] = 0;
+    p.piece_base[xcd * (row + 1) + k + 1] = 0;
+  }
+  __syncthreads();   // (counts of all units written, by this workgroup)
+  for (int xcd = wave; xcd < 8; xcd += kWaves) {   // counts -> pieces before
+    int32_t *base = p.piece_base + xcd * (row + 1);
+    int run = 0;
+    for (int i = 0; i < row; i += 64) {
+      int incl = i + lane < row ? base[i + lane + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += t;
+      }
+      if (i + lane < row) base[i + lane + 1] = run + incl;
+      run += __shfl(incl, 63, 64);
+    }
+    if (lane == 0) base[0] = 0;
+  }
 }
 
 // A workgroup's piece of a tile.
@@ -494,20 +537,33 @@ struct Piece {
 };
 __device__ __forceinline__ bool find_piece(const ChunkParams &p, Piece &x) {
   const int lane = threadIdx.x & 63;
-  const int count = p.piece_base[p.units];
-  if (static_cast<int>(blockIdx.x) >= count) return false;
-  // consecutive pieces on one XCD (they share the unit's slots, or the closed states)
-  const int lin = blockIdx.x, q = count >> 3, r = count & 7, xc = lin & 7, j = lin >> 3;
-  const int idx = xc < r ? xc * (q + 1) + j : r * (q + 1) + (xc - r) * q + j;
-  int lo = 0, n = p.units;   // the last unit with piece_base <= idx
+  const int row = (p.units + 7) >> 3, slots = gridDim.x >> 3;
+  int xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;   // (workgroup i runs on XCD i mod 8)
+  const int mine = lane < 8 ? p.piece_base[lane * (row + 1) + row] : 0;   // pieces of XCD `lane`
+  const int count = __builtin_amdgcn_readlane(mine, xcd);
+  if (idx >= count) {   // a place left over: a piece of an XCD that has more than its places
+    int spare = idx - count;
+    for (int i = 0; i < xcd; ++i) spare += max(slots - __builtin_amdgcn_readlane(mine, i), 0);
+    for (xcd = 0; xcd < 8; ++xcd) {
+      const int over = max(__builtin_amdgcn_readlane(mine, xcd) - slots, 0);
+      if (spare < over) break;
+      spare -= over;
+    }
+    if (xcd == 8) return false;
+    idx = slots + spare;
+  }
+  const int32_t *base = p.piece_base + xcd * (row + 1);
+  int lo = 0, n = row;   // the last of its units with pieces before <= idx
   while (n > 1) {
     const int step = (n + 63) >> 6, i = lo + lane * step;
-    const bool le = lane == 0 || (i < lo + n && p.piece_base[i] <= idx);
+    const bool le = lane == 0 || (i < lo + n && base[i] <= idx);
     const int k = 63 - __clzll(static_cast<long long>(__ballot(le)));
     const int end = lo + n;
     lo += k * step;
     n = min(step, end - lo);
   }
+  const int rel = idx - __builtin_amdgcn_readfirstlane(base[lo]);
+  lo = __builtin_amdgcn_readfirstlane(p.unit_order[xcd * row + lo]);
   x.u = __builtin_amdgcn_readfirstlane(lo);
   x.b = x.u / p.hkv;
   x.g = x.u - x.b * p.hkv;
@@ -515,7 +571,6 @@ __device__ __forceinline__ bool find_piece(const ChunkParams &p, Piece &x) {
   x.start = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b], p.total));
   const int end = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b + 1], p.total));
   x.n = min(max(end - x.start, 0), p.max_chunk);
-  const int rel = idx - __builtin_amdgcn_readfirstlane(p.piece_base[x.u]);
   const int tiles = (x.n + (1 << p.tile_shift) - 1) >> p.tile_shift;
   x.record = __builtin_amdgcn_readfirstlane(p.record_base[x.u]) + rel;
   const int t = rel / x.parts;
@@ -1266,7 +1321,7 @@ hipError_t chunk_attend(const ChunkParams &p, bool vt, bool wide, hipStream_t s)
   hipError_t e = vt ? chunk_states<ES, D, (ES == 2 && G >= 4)>(p, s) : chunk_states<ES, D, false>(p, s);
   if (e != hipSuccess) return e;
   const unsigned tiles = (p.total >> p.tile_shift) + p.rows;
-  const unsigned pieces = tiles * p.hkv + p.piece_budget;
+  const unsigned pieces = (tiles * p.hkv + p.piece_budget + 7) / 8 * 8;
   if constexpr (ES == 2) {
     if (vt) {
       if constexpr (G >= 4) attend_bf16<D, G, true, true>(p, wide, pieces, s);
