@@ -1069,7 +1069,7 @@ static ChunkLayout chunk_layout(const dmc_cache *c, int32_t total) {
   L.starts = take(H * blocks64 * 4);
   L.carry = take(H * blocks64 * dmc::carry_stride(cfg.head_dim) * 4);
   L.visible = take(U * 4);
-  L.unit_order = take((U + 7) / 8 * 8 * 4);
+  L.unit_order = take((U + 7) / 8 * 8 * 8 * 4);
   L.piece_base = take(((U + 7) / 8 + 1) * 8 * 4);
   L.pieces = take(U * 4);
   L.record_base = take(U * 4);

@@ -323,9 +323,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
       }
       if (diagonal) {
 #pragma unroll
-        for (int i = 0; i < NTL; ++i)
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk) left_out |= leave_out_nonfinite(va[i][kk]);
+        for (int i = 0; i < NTL; ++i) left_out |= leave_out_nonfinite(va[i]);
       }
 #pragma unroll
       for (int i = 0; i < NTL; ++i)
@@ -407,10 +405,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
         }
         sb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      if (diagonal) {
-#pragma unroll
-        for (int j = 0; j < 2 * NTL; ++j) left_out |= leave_out_nonfinite(kt[j]);
-      }
+      if (diagonal) left_out |= leave_out_nonfinite(kt);
 #pragma unroll
       for (int j = 0; j < 2 * NTL; ++j) acc[j >> 1] = mfma_32x32x16(kt[j], sb[j & 1], acc[j >> 1]);
     };

@@ -406,6 +406,7 @@ __global__ __launch_bounds__(kThreads) void chunk_grow_kernel(ChunkParams p) {
 // more than tiles + budget pieces.
 // ---------------------------------------------------------------------------
 struct UnitPlan {
+  int start, n;        // the row's first token and tokens
   int tiles, blocks;   // column tiles; 32-row blocks of the whole list
 };
 __device__ __forceinline__ UnitPlan unit_plan(const ChunkParams &p, int u) {
@@ -413,6 +414,8 @@ __device__ __forceinline__ UnitPlan unit_plan(const ChunkParams &p, int u) {
   const int s0 = clamp_token(p.cu[b], p.total), s1 = clamp_token(p.cu[b + 1], p.total);
   const int n = min(max(s1 - s0, 0), p.max_chunk);
   UnitPlan x;
+  x.start = s0;
+  x.n = n;
   x.tiles = (n + (1 << p.tile_shift) - 1) >> p.tile_shift;
   // (the chunk's share at most every token a slot; half of it on average over the tiles)
   x.blocks = ((p.len[u] + 31) >> 5) + ((n + 63) >> 6);
@@ -501,14 +504,18 @@ __device__ void plan_pieces(const ChunkParams &p) {
     const UnitPlan x = unit_plan(p, u);
     const int at = atomicAdd(&s_bucket[cost_bucket(static_cast<float>(x.tiles) * x.blocks)], 1);
     const int k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7, np = p.pieces[u];
-    p.unit_order[xcd * row + k] = u;
+    int32_t *info = p.unit_order + (int64_t(xcd) * row + k) * 8;
+    *reinterpret_cast<int4 *>(info) = make_int4(u, np, rec, x.start);
+    info[4] = x.n;
     p.piece_base[xcd * (row + 1) + k + 1] = x.tiles * np;
     p.record_base[u] = rec;
     rec += np > 1 ? x.tiles * np : 0;
   }
   if (tid < 8 * row - p.units) {   // places without a unit, in the last line
     const int at = p.units + tid, k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7;
-    p.unit_order[xcd * row + k] = 0;
+    int32_t *info = p.unit_order + (int64_t(xcd) * row + k) * 8;   // (no pieces: never looked up)
+    *reinterpret_cast<int4 *>(info) = make_int4(0, 1, 0, 0);
+    info[4] = 0;
     p.piece_base[xcd * (row + 1) + k + 1] = 0;
   }
   __syncthreads();   // (counts of all units written, by this workgroup)
@@ -539,7 +546,9 @@ __device__ __forceinline__ bool find_piece(const ChunkParams &p, Piece &x) {
   const int lane = threadIdx.x & 63;
   const int row = (p.units + 7) >> 3, slots = gridDim.x >> 3;
   int xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;   // (workgroup i runs on XCD i mod 8)
-  const int mine = lane < 8 ? p.piece_base[lane * (row + 1) + row] : 0;   // pieces of XCD `lane`
+  const int mine = p.piece_base[(lane & 7) * (row + 1) + row];   // pieces of XCD `lane`
+  const int step0 = (row + 63) >> 6, at0 = min(lane * step0, row);
+  int before = p.piece_base[xcd * (row + 1) + at0];   // (ahead of what decides whether it is needed)
   const int count = __builtin_amdgcn_readlane(mine, xcd);
   if (idx >= count) {   // a place left over: a piece of an XCD that has more than its places
     int spare = idx - count;
@@ -551,28 +560,33 @@ __device__ __forceinline__ bool find_piece(const ChunkParams &p, Piece &x) {
     }
     if (xcd == 8) return false;
     idx = slots + spare;
+    before = p.piece_base[xcd * (row + 1) + at0];
   }
   const int32_t *base = p.piece_base + xcd * (row + 1);
-  int lo = 0, n = row;   // the last of its units with pieces before <= idx
-  while (n > 1) {
-    const int step = (n + 63) >> 6, i = lo + lane * step;
-    const bool le = lane == 0 || (i < lo + n && base[i] <= idx);
+  int lo = 0, n = row, step = step0;   // the last of its units with pieces before <= idx
+  while (true) {
+    const bool le = lane == 0 || (lane * step < n && before <= idx);
     const int k = 63 - __clzll(static_cast<long long>(__ballot(le)));
     const int end = lo + n;
     lo += k * step;
     n = min(step, end - lo);
+    before = __builtin_amdgcn_readlane(before, k);
+    if (n <= 1) break;
+    step = (n + 63) >> 6;
+    before = base[lo + min(lane * step, n - 1)];
   }
-  const int rel = idx - __builtin_amdgcn_readfirstlane(base[lo]);
-  lo = __builtin_amdgcn_readfirstlane(p.unit_order[xcd * row + lo]);
-  x.u = __builtin_amdgcn_readfirstlane(lo);
+  // (visibly uniform: every branch on them would otherwise be made per lane)
+  const int rel = __builtin_amdgcn_readfirstlane(idx - before);
+  const int32_t *info = p.unit_order + __builtin_amdgcn_readfirstlane(xcd * row + lo) * int64_t(8);
+  const int4 i4 = *reinterpret_cast<const int4 *>(info);
+  x.n = __builtin_amdgcn_readfirstlane(info[4]);
+  x.u = __builtin_amdgcn_readfirstlane(i4.x);
   x.b = x.u / p.hkv;
   x.g = x.u - x.b * p.hkv;
-  x.parts = __builtin_amdgcn_readfirstlane(p.pieces[x.u]);
-  x.start = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b], p.total));
-  const int end = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b + 1], p.total));
-  x.n = min(max(end - x.start, 0), p.max_chunk);
+  x.parts = __builtin_amdgcn_readfirstlane(i4.y);
+  x.record = __builtin_amdgcn_readfirstlane(i4.z) + rel;
+  x.start = __builtin_amdgcn_readfirstlane(i4.w);
   const int tiles = (x.n + (1 << p.tile_shift) - 1) >> p.tile_shift;
-  x.record = __builtin_amdgcn_readfirstlane(p.record_base[x.u]) + rel;
   const int t = rel / x.parts;
   x.part = rel - t * x.parts;
   x.tile = tiles - 1 - t;   // latest tokens (most states) first
@@ -657,21 +671,21 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
   const uint4 zero4 = make_uint4(0, 0, 0, 0);
   const float sl2 = p.scale_log2;
 
-  // Q^T operand (q[0] is not part of the score).
   uint4 qop[KS];
-  {
-    const char *qr = static_cast<const char *>(p.q) + (token * p.qs[0] + (x.g * G + head) * p.qs[1]) * 2;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qop[ks] = colv ? ld16(qr + ks * 32 + hb * 16) : zero4;
-    if (hb == 0) qop[0].x &= 0xffff0000u;
-  }
   // (the lowest finite value: a wave that has seen nothing must not outweigh any score)
   float m = lowest(), ls = 0.0f;
   f32x16_t acc[NTL];
 #pragma unroll
   for (int i = 0; i < NTL; ++i) acc[i] = f32x16_t{};
-  // The column's own state, in the tile's last piece (by the narrow wave with the fewest blocks).
-  if (x.part == x.parts - 1 && (WIDE || wave == ((b1 - b0) & (kWaves - 1)))) {
+  // Queries and own states of the columns, once the first blocks are on their way.
+  auto load_columns = [&]() {
+    // Q^T operand (q[0] is not part of the score).
+    const char *qr = static_cast<const char *>(p.q) + (token * p.qs[0] + (x.g * G + head) * p.qs[1]) * 2;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qop[ks] = colv ? ld16(qr + ks * 32 + hb * 16) : zero4;
+    if (hb == 0) qop[0].x &= 0xffff0000u;
+    // The column's own state, in the tile's last piece (by the narrow wave with the fewest blocks).
+    if (x.part != x.parts - 1 || !(WIDE || wave == ((b1 - b0) & (kWaves - 1)))) return;
     const int64_t row = (int64_t(x.g) * p.total + token) * RB;
     float d = 0.0f;
 #pragma unroll
@@ -697,7 +711,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
           acc[i][4 * j + 3] = bf16_hi(w.y);
         }
     }
-  }
+  };
 
   // Where a block lies.  Cached: BIG pages hold it whole; of smaller pages, a run
   // of rows (8 or more, so that a transfer of 1 KB lies in one) each.
@@ -754,21 +768,26 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
   auto clean_values = [&](uint4 (&va)[NTL][2], int kb) {
     const bool cached = kb < nbc;
     const int end = (cached ? vis : top) - (cached ? kb : kb - nbc) * 32;
+    if (end < 32) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const int keep = end - (16 * kk + 8 * hb);
-      uint32_t msk[4];
+      for (int kk = 0; kk < 2; ++kk) {
+        const int keep = end - (16 * kk + 8 * hb);
+        uint32_t msk[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        msk[q] = (2 * q < keep ? 0x0000ffffu : 0u) | (2 * q + 1 < keep ? 0xffff0000u : 0u);
+        for (int q = 0; q < 4; ++q)
+          msk[q] = (2 * q < keep ? 0x0000ffffu : 0u) | (2 * q + 1 < keep ? 0xffff0000u : 0u);
 #pragma unroll
-      for (int i = 0; i < NTL; ++i) {
-        va[i][kk].x &= msk[0];
-        va[i][kk].y &= msk[1];
-        va[i][kk].z &= msk[2];
-        va[i][kk].w &= msk[3];
-        if (!cached) left_out |= leave_out_nonfinite(va[i][kk]);
+        for (int i = 0; i < NTL; ++i) {
+          va[i][kk].x &= msk[0];
+          va[i][kk].y &= msk[1];
+          va[i][kk].z &= msk[2];
+          va[i][kk].w &= msk[3];
+        }
       }
+    }
+    if (!cached) {
+#pragma unroll
+      for (int i = 0; i < NTL; ++i) left_out |= leave_out_nonfinite(va[i]);
     }
   };
   uint32_t traddr[NTL][2], vtaddr[2];
@@ -850,6 +869,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
     issue(b0, std::integral_constant<int, 0>{});
     issue(b0 + 1, std::integral_constant<int, 1>{});
     issue(b0 + 2, std::integral_constant<int, 2>{});
+    load_columns();
     f32x16_t scn = f32x16_t{};
     wait_vmcnt<(kSt - 2) * 2 * DPW>();   // block b0 has landed
     ring_barrier();
@@ -909,6 +929,10 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
   } else {
     // A block's keys: row pi(col), 16-byte slices 2 ks + hb; of pages smaller than
     // a block each lane its row's page.  Slots past the visible ones read the last.
+    int page = 0;   // of the block that is issued next (BIG), looked up one block ahead
+    auto look_up = [&](int kb) {
+      if (BIG) page = kb < min(nbc, b1) ? page_index(kb * 32) : 0;
+    };
     auto load_keys = [&](int kb, uint4 (&k)[KS]) {
       const bool cached = kb < nbc;
       const int first = (cached ? kb : kb - nbc) * 32;
@@ -916,7 +940,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       if (!cached) {
         row = kclosed + int64_t(first + krow) * RB;
       } else if constexpr (BIG) {
-        row = p.pool + int64_t(page_index(first)) * p.page_bytes + int64_t((first & (P - 1)) + krow) * RB;
+        row = p.pool + int64_t(page) * p.page_bytes + int64_t((first & (P - 1)) + krow) * RB;
       } else {
         const int s = min(first + krow, vis - 1);
         row = p.pool + int64_t(p.ptab[table + (s >> p.log2p)]) * p.page_bytes + int64_t(s & (P - 1)) * RB;
@@ -943,8 +967,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       if (BIG || !cached) {
         const char *vp = vclosed + int64_t(first) * RB;
         if (cached) {
-          const char *page = p.pool + int64_t(page_index(first)) * p.page_bytes;
-          vp = page + int64_t(P) * RB + (VT ? 0 : int64_t(first & (P - 1)) * RB);
+          vp = p.pool + int64_t(page) * p.page_bytes + int64_t(P) * RB + (VT ? 0 : int64_t(first & (P - 1)) * RB);
         }
         vp = uniform_ptr(vp);
 #pragma unroll
@@ -968,6 +991,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       if (more) {
         issue_values(next, std::integral_constant<int, ST ^ 1>{});
         load_keys(next, kv[ST ^ 1]);
+        look_up(next + kWaves);
       }
       f32x16_t sc = f32x16_t{};
 #pragma unroll
@@ -977,9 +1001,10 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       weights(sc, kb, sv, masked);
 #pragma unroll
       for (int i = 0; i < 16; ++i) ev[i] = fast_exp2(fmaf(sv[i], sl2, -m));
-      uint4 pb[2], va[NTL][2];
+      uint4 pb[2];
       operands(ev, pb);
       const char *vd = reinterpret_cast<const char *>(slot(stage_c)) + wave * BLK;
+      uint4 va[NTL][2];
 #pragma unroll
       for (int i = 0; i < NTL; ++i)
 #pragma unroll
@@ -992,8 +1017,13 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       kb = next;
     };
     if (kb < b1) {
+      look_up(kb);
       issue_values(kb, std::integral_constant<int, 0>{});
       load_keys(kb, kv[0]);
+      look_up(kb + kWaves);
+    }
+    load_columns();
+    if (kb < b1) {
       while (true) {
         step(std::integral_constant<int, 0>{}, kb + kWaves < b1);
         if (kb >= b1) break;

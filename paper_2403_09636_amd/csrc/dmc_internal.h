@@ -309,7 +309,8 @@ struct ChunkParams {
   int32_t *starts;               // [hkv][blocks64]: segment starts per 64-token block
   float *carry;                  // [hkv][blocks64][carry_stride]: the open segment's sums at a block's end
   int32_t *visible;              // [U]: cached slots that the chunk attends to (attend)
-  int32_t *unit_order;           // [8][ceil(U / 8)]: units of every XCD (attend)
+  int32_t *unit_order;           // [8][ceil(U / 8)][8]: units of every XCD: unit, pieces per tile, partial records
+                                 // before it, the row's first token and tokens (attend)
   int32_t *piece_base;           // [8][ceil(U / 8) + 1]: pieces before them on their XCD (attend)
   int32_t *pieces;               // [U]: pieces per tile of the unit's columns (attend)
   int32_t *record_base;          // [U]: partial records before the unit's (attend)

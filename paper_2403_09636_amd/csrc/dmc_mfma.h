@@ -253,6 +253,14 @@ __device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) <
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
   return ((w & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u);
 }
+// NaN if any of the eight is not finite, else 0, added to acc.
+__device__ __forceinline__ float nonfinite(const uint4 &x, float acc) {
+  const bf16x2_t zero = __builtin_bit_cast(bf16x2_t, 0u);
+  acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.x), zero, acc, false);
+  acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.y), zero, acc, false);
+  acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.z), zero, acc, false);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x.w), zero, acc, false);
+}
 // A value operand of a block whose rows some columns do not see: their weight
 // is 0, but 0 times an infinity or NaN would reach them through the product.
 // Such elements are left out (set to 0) and reported, to be added after the
@@ -264,6 +272,19 @@ __device__ __forceinline__ bool leave_out_nonfinite(uint4 &x) {
   x.z &= m2;
   x.w &= m3;
   return (m0 & m1 & m2 & m3) != 0xffffffffu;
+}
+// The same for N operands, which are nearly always all finite (one product each
+// to find out).
+template <int N>
+__device__ __forceinline__ bool leave_out_nonfinite(uint4 (&x)[N]) {
+  float acc = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) acc = nonfinite(x[i], acc);
+  if (!__any(acc != 0.0f)) return false;   // (NaN compares unequal)
+  bool out = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) out |= leave_out_nonfinite(x[i]);
+  return out;
 }
 // Adds the infinities and NaN of a block's 32 bf16 rows to the columns that see
 // them (sees(i): this lane's column sees row i; load4(i, e): the packed elements
