@@ -1042,13 +1042,21 @@ struct ChunkLayout {
 };
 
 // Attention pieces beyond one per column tile, and the fewest 32-row blocks of
-// one.  Four per compute unit; none once the tiles themselves are eight per
+// one.  Three per compute unit; none once the tiles themselves are eight per
 // compute unit.
 static int32_t chunk_piece_budget(const dmc_cache *c, int32_t total, int shift) {
   const int64_t tiles = int64_t(total >> shift) * c->cfg.num_kv_heads;
-  return tiles >= int64_t(8) * c->cu_count ? 0 : 4 * c->cu_count;
+  return tiles >= int64_t(8) * c->cu_count ? 0 : 3 * c->cu_count;
 }
 constexpr int32_t kChunkPieceMin = 8;
+// Few units of one 32-column tile each: a fixed number of places per unit, as many
+// as are all resident (two per compute unit) and its capacity can use; 0 for
+// others, whose pieces are planned by their lengths.
+static int32_t chunk_fixed_parts(const dmc_cache *c, int32_t max_chunk, int64_t most_blocks) {
+  if (int64_t(max_chunk) * c->lay.group > 32 || c->lay.units > 64) return 0;
+  const int64_t parts = std::min<int64_t>(2 * c->cu_count / c->lay.units, most_blocks / kChunkPieceMin);
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
+}
 
 static ChunkLayout chunk_layout(const dmc_cache *c, int32_t total) {
   const dmc_cache_config &cfg = c->cfg;
@@ -1198,7 +1206,10 @@ dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q
   copy_strides(p.os, out_strides);
   const bool wide = dmc::chunk_wide(elem_bytes(c), cache->lay.group, max_chunk);
   p.tile_shift = dmc::chunk_tile_shift(cache->lay.group, wide);
-  p.piece_budget = chunk_piece_budget(cache, total, p.tile_shift);
+  // (units whose capacity makes less than two pieces are never cut)
+  const int64_t most_blocks = (int64_t(c.max_slots_per_seq) + 31) / 32 + (int64_t(max_chunk) + 63) / 64;
+  p.piece_budget = most_blocks < 2 * kChunkPieceMin ? 0 : chunk_piece_budget(cache, total, p.tile_shift);
+  p.fixed_parts = chunk_fixed_parts(cache, max_chunk, most_blocks);
   DeviceGuard g(cache->device);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");
   hipError_t e = dmc::launch_chunk_attend(elem_bytes(c), c.head_dim, cache->lay.group, cache->lay.v_trans, wide, p,

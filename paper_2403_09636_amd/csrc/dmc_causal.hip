@@ -405,7 +405,10 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
         }
         sb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      if (diagonal) left_out |= leave_out_nonfinite(kt);
+      if (diagonal) {   // (one by one: the check of all at once spills fifty registers here)
+#pragma unroll
+        for (int j = 0; j < 2 * NTL; ++j) left_out |= leave_out_nonfinite(kt[j]);
+      }
 #pragma unroll
       for (int j = 0; j < 2 * NTL; ++j) acc[j >> 1] = mfma_32x32x16(kt[j], sb[j & 1], acc[j >> 1]);
     };
@@ -897,10 +900,8 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
   at(min(wave, nblk - 1), hh, rb);
   F::load_row(qr, q_at(hh, rb + col), hb);
   bool out_v = false, out_k = false;
-#pragma unroll 1
-  for (int i = wave; i < nblk; i += kWaves) {
-    at(i, hh, rb);
-    const bool masked = rb == s0 || rb + 32 > n;
+  auto block = [&](int i, auto masked_c, bool masked) {
+    constexpr bool MASKED = decltype(masked_c)::value;
     if constexpr (DK) F::load_row(dor, do_at(hh, rb + col), hb);   // lands while the scores run
     typename F::Cols qc, oc;
     auto q_row = [&](int r) { return q_at(hh, rb + r); };
@@ -930,12 +931,21 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int row = rb + F::row(r, hb);
-      const bool vis = row >= js && row < n;
+      const bool vis = !MASKED || (row >= js && row < n);
       pv[r] = vis ? fast_exp2(sc[r] * p.scale_log2 - Lr[r]) : 0.0f;
       if constexpr (DK) ds[r] = vis ? pv[r] * (dp[r] - Dr[r]) : 0.0f;
     }
-    if constexpr (DV) out_v |= F::template add_rows<true>(dv, oc, do_row, pv, lane, masked);
-    if constexpr (DK) out_k |= F::template add_rows<true>(dk, qc, q_row, ds, lane, masked);
+    if constexpr (DV) out_v |= F::template add_rows<MASKED>(dv, oc, do_row, pv, lane, masked);
+    if constexpr (DK) out_k |= F::template add_rows<MASKED>(dk, qc, q_row, ds, lane, masked);
+  };
+#pragma unroll 1
+  for (int i = wave; i < nblk; i += kWaves) {
+    at(i, hh, rb);
+    const bool masked = rb == s0 || rb + 32 > n;
+    // (PART 2: the masked sums in a body of their own -- beside the others they spilled two
+    // hundred registers, 644 -> 270 us for 3 sequences up to 1000 tokens, 8/2 heads)
+    if (PART != 2 || masked) block(i, std::true_type{}, masked);
+    else block(i, std::false_type{}, false);
   }
   if (__any(out_v || out_k)) {
     for (int i = wave; i < nblk; i += kWaves) {

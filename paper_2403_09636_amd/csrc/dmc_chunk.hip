@@ -22,7 +22,8 @@ namespace dmc {
 namespace {
 
 constexpr int kBlockShift = 6, kBlock = 1 << kBlockShift;   // tokens of a workgroup of the state kernels
-constexpr int kWaveTokens = kBlock / kWaves;
+constexpr int kStateThreads = 512, kStateWaves = kStateThreads / 64;
+constexpr int kWaveTokens = kBlock / kStateWaves;
 
 // The E elements of a row at `p` as floats (one access).
 template <int ES, int E>
@@ -95,7 +96,7 @@ __device__ __forceinline__ char *page_of(const ChunkParams &p, int u, int s) {
   return p.pool + int64_t(p.ptab[int64_t(u) * p.maxpages + (s >> p.log2p)]) * p.page_bytes;
 }
 
-// One workgroup = one 64-token block of one unit: wave w takes tokens 16 w .. + 16,
+// One workgroup = one 64-token block of one unit: wave w takes tokens 8 w .. + 8,
 // lanes 0..31 the key's elements, lanes 32..63 the value's.  The wave's rows are
 // loaded once into registers; the segment's sums before each wave come from the
 // waves before it (LDS), before the block from the block records, before the row
@@ -133,12 +134,12 @@ __device__ __forceinline__ bool grow_unit(const ChunkParams &p, int u, int l, in
 }
 
 template <int ES, int D, bool VT, int MODE>
-__global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
+__global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams p) {
   constexpr int E = D / 32, RB = D * ES;
   constexpr bool kAppend = MODE == APPEND || MODE == ONE;
   __shared__ float s_omega[kBlock];
-  __shared__ float s_sum[kWaves][64 * E];   // a wave's sums of its open segment
-  __shared__ float s_sumz[kWaves];
+  __shared__ float s_sum[kStateWaves][64 * E];   // a wave's sums of its open segment
+  __shared__ float s_sumz[kStateWaves];
   __shared__ unsigned long long s_mask;
   __shared__ int s_next, s_first, s_prior, s_base, s_end;
   if constexpr (MODE == ATTEND) {
@@ -146,6 +147,12 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
       if (blockIdx.y == 0) plan_pieces(p);
       return;
     }
+  }
+  if (MODE != SUMS && blockIdx.x == 0 && blockIdx.y == 0) {   // boundaries out of range or decreasing
+    bool bad = false;
+    for (int b = threadIdx.x; b < p.rows; b += kStateThreads)
+      bad |= p.cu[b] < 0 || p.cu[b + 1] > p.total || p.cu[b + 1] < p.cu[b];
+    if (bad) atomicOr(&p.ctrl->flags, FLAG_BAD_LENGTH);
   }
   const int g = blockIdx.y;
   const PackedTile pt = packed_tile(p.cu, p.rows, p.total, blockIdx.x, kBlockShift);
@@ -159,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
   c.first = pt.tile * kBlock;
   c.index = blockIdx.x;
   if (kAppend && p.slot_index) {   // tokens that are not appended
-    for (int t = c.first + tid; t < min(c.first + kBlock, pt.n); t += kThreads)
+    for (int t = c.first + tid; t < min(c.first + kBlock, pt.n); t += kStateThreads)
       if (t >= c.n) p.slot_index[int64_t(c.start + t) * p.hkv + g] = -1;
   }
   if (c.first >= c.n) return;
@@ -182,6 +189,17 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
 #pragma unroll
   for (int i = 0; i < kWaveTokens; ++i)
     x[i].load(rows + int64_t(c.first + min(w0 + i, cnt - 1)) * rst);
+  Elems<ES, E> open_slot;   // the cached open slot, for the row's first block
+  if (pt.tile == 0 && l > 0) {
+    const char *page = page_of(p, c.u, l - 1);
+    const int P = 1 << p.log2p, r = (l - 1) & (P - 1);
+    if (VT && hb) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) open_slot.f[e] = load_elem<2>(page + int64_t(P) * RB, int64_t(el + e) * P + r);
+    } else {
+      open_slot.load(page + (int64_t(hb ? P : 0) + r) * RB + el * ES);
+    }
+  }
   if (wave == 0) {
     const bool here = lane < cnt;
     const int t = c.first + min(lane, cnt - 1);
@@ -262,19 +280,9 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
     }
     if (pt.tile == 0) {   // the cached open slot (an empty unit's first token opens one)
       if (l > 0) {
-        Elems<ES, E> s;
-        const char *page = page_of(p, c.u, l - 1);
-        const int P = 1 << p.log2p, r = (l - 1) & (P - 1);
-        if (VT && hb) {
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            s.f[e] = load_elem<2>(page + int64_t(P) * RB, int64_t(el + e) * P + r);
-        } else {
-          s.load(page + (int64_t(hb ? P : 0) + r) * RB + el * ES);
-        }
         z += zold;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(zold, s.f[e], o[e]);
+        for (int e = 0; e < E; ++e) o[e] = fmaf(zold, open_slot.f[e], o[e]);
       }
       return;
     }
@@ -298,9 +306,9 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.0f;
     if (pt.tile == 0) {
-      open_before(kWaves, o, z);
+      open_before(kStateWaves, o, z);
     } else {
-      for (int j = kWaves - 1; j >= 0; --j) {
+      for (int j = kStateWaves - 1; j >= 0; --j) {
         z += s_sumz[j];
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] += s_sum[j][lane * E + e];
@@ -314,6 +322,10 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
     return;
   }
   if (wcnt == 0) return;
+  // Pages of the wave's slots (its tokens' lie side by side), one to a lane.
+  const int slot0 = l - 1 + s_prior + __popcll(mask & ((1ull << w0) - 1)), page0 = max(slot0, 0) >> p.log2p;
+  int pages = 0;
+  if (kAppend && lane < 4) pages = p.ptab[int64_t(c.u) * p.maxpages + min(page0 + lane, p.maxpages - 1)];
   open_before(wave, sum, zs);
   const int P = 1 << p.log2p;
   const int64_t out_row = (int64_t(g) * p.total + c.start + c.first) * D + el;
@@ -325,7 +337,8 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
     const float w = s_omega[t];
     zs = (keep ? zs : 0.0f) + w;
     Elems<ES, E> s;
-    const float inv = 1.0f / zs;
+    // (bf16: the reciprocal's last bit is far below the state's rounding)
+    const float inv = ES == 2 ? __builtin_amdgcn_rcpf(zs) : 1.0f / zs;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       sum[e] = fmaf(w, x[i].f[e], keep ? sum[e] : 0.0f);
@@ -354,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void chunk_states_kernel(ChunkParams p) {
       const int slot = l - 1 + seg;
       if (lane == 0 && p.slot_index) p.slot_index[int64_t(c.start + c.first + t) * p.hkv + g] = slot;
       if ((closed || last) && slot >= 0 && slot < s_end) {   // (always, for boundaries that do not decrease)
-        char *page = page_of(p, c.u, slot);
+        char *page = p.pool + int64_t(__shfl(pages, (slot >> p.log2p) - page0, 64)) * p.page_bytes;
         const int r = slot & (P - 1);
         if (VT && hb) {
 #pragma unroll
@@ -403,7 +416,9 @@ __global__ __launch_bounds__(kThreads) void chunk_grow_kernel(ChunkParams p) {
 // into pieces of that list where units are few or long, which meet in a combine
 // pass; one workgroup per piece.  The lengths are on the device, so the plan is
 // made there: a piece is about total / budget blocks, so that there are never
-// more than tiles + budget pieces.
+// more than tiles + budget pieces.  Few units of one narrow tile each get a fixed
+// number of places instead (fixed_parts), which takes no plan and fewer loads that
+// wait for each other.
 // ---------------------------------------------------------------------------
 struct UnitPlan {
   int start, n;        // the row's first token and tokens
@@ -434,40 +449,38 @@ __device__ __forceinline__ int cost_bucket(float cost) {   // (most expensive fi
 }
 
 __device__ void plan_pieces(const ChunkParams &p) {
-  __shared__ long long s_total[kWaves];
-  __shared__ int s_split[kWaves], s_bucket[kCostBuckets], s_sum[kWaves];
+  __shared__ long long s_total[kStateWaves];
+  __shared__ int s_split[kStateWaves], s_bucket[kCostBuckets], s_sum[kStateWaves], s_pieces[8 * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.units + kThreads - 1) / kThreads;
+  const int per = (p.units + kStateThreads - 1) / kStateThreads;
   const int i0 = min(tid * per, p.units), i1 = min(i0 + per, p.units);
-  for (int i = tid; i < kCostBuckets; i += kThreads) s_bucket[i] = 0;
+  UnitPlan own{};   // the thread's first unit (its only one, of up to 512)
+  if (i0 < i1) own = unit_plan(p, i0);
+  auto plan_of = [&](int u) { return u == i0 ? own : unit_plan(p, u); };
+  for (int i = tid; i < kCostBuckets; i += kStateThreads) s_bucket[i] = 0;
   __syncthreads();
   long long total = 0;
   for (int u = i0; u < i1; ++u) {
-    const UnitPlan x = unit_plan(p, u);
+    const UnitPlan x = plan_of(u);
     total += static_cast<long long>(x.tiles) * x.blocks;
     atomicAdd(&s_bucket[cost_bucket(static_cast<float>(x.tiles) * x.blocks)], 1);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
   if (lane == 0) s_total[wave] = total;
-  // boundaries out of range or decreasing raise the flag
-  bool bad = false;
-  for (int b = tid; b < p.rows; b += kThreads)
-    bad |= p.cu[b] < 0 || p.cu[b + 1] > p.total || p.cu[b + 1] < p.cu[b];
-  if (bad) atomicOr(&p.ctrl->flags, FLAG_BAD_LENGTH);
   __syncthreads();
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) total += s_total[w];
+  for (int w = 0; w < kStateWaves; ++w) total += s_total[w];
   int size = 1 << 30;
   if (p.piece_budget > 0) {
     const long long want = (total + p.piece_budget - 1) / p.piece_budget;
     size = static_cast<int>(want > p.piece_min ? min(want, 1ll << 30) : p.piece_min);
   }
-  // Bucket sizes -> first positions (two to a thread).
-  static_assert(kCostBuckets == 2 * kThreads, "two buckets a thread");
-  const int c0 = s_bucket[2 * tid], c1 = s_bucket[2 * tid + 1];
-  int ends = c0 + c1;
+  // Bucket sizes -> first positions.
+  static_assert(kCostBuckets == kStateThreads, "a bucket to a thread");
+  const int here = s_bucket[tid];
+  int ends = here;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int t = __shfl_up(ends, o, 64);
@@ -478,9 +491,9 @@ __device__ void plan_pieces(const ChunkParams &p) {
   // tile, so that their pieces, which have a record each, are at most the budget.
   int split = 0;
   for (int u = i0; u < i1; ++u) {
-    const UnitPlan x = unit_plan(p, u);
+    const UnitPlan x = plan_of(u);
     const int np = max(1, x.blocks / size);
-    p.pieces[u] = np;
+    p.pieces[u] = np;   // (for the combine pass)
     split += np > 1 ? x.tiles * np : 0;
   }
   int incs = split;
@@ -491,23 +504,23 @@ __device__ void plan_pieces(const ChunkParams &p) {
   }
   if (lane == 63) s_split[wave] = incs;
   __syncthreads();
-  int first = ends - c0 - c1, rec = incs - split;
+  int first = ends - here, rec = incs - split;
   for (int w = 0; w < wave; ++w) {
     first += s_sum[w];
     rec += s_split[w];
   }
-  s_bucket[2 * tid] = first;
-  s_bucket[2 * tid + 1] = first + c0;
+  s_bucket[tid] = first;
   __syncthreads();
   const int row = (p.units + 7) >> 3;   // units of an XCD
   for (int u = i0; u < i1; ++u) {
-    const UnitPlan x = unit_plan(p, u);
+    const UnitPlan x = plan_of(u);
     const int at = atomicAdd(&s_bucket[cost_bucket(static_cast<float>(x.tiles) * x.blocks)], 1);
-    const int k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7, np = p.pieces[u];
+    const int k = at >> 3, xcd = k & 1 ? 7 - (at & 7) : at & 7, np = max(1, x.blocks / size);
     int32_t *info = p.unit_order + (int64_t(xcd) * row + k) * 8;
     *reinterpret_cast<int4 *>(info) = make_int4(u, np, rec, x.start);
     info[4] = x.n;
-    p.piece_base[xcd * (row + 1) + k + 1] = x.tiles * np;
+    if (row < 64) s_pieces[xcd * 64 + k] = x.tiles * np;
+    else p.piece_base[xcd * (row + 1) + k + 1] = x.tiles * np;
     p.record_base[u] = rec;
     rec += np > 1 ? x.tiles * np : 0;
   }
@@ -516,14 +529,15 @@ __device__ void plan_pieces(const ChunkParams &p) {
     int32_t *info = p.unit_order + (int64_t(xcd) * row + k) * 8;   // (no pieces: never looked up)
     *reinterpret_cast<int4 *>(info) = make_int4(0, 1, 0, 0);
     info[4] = 0;
-    p.piece_base[xcd * (row + 1) + k + 1] = 0;
+    if (row < 64) s_pieces[xcd * 64 + k] = 0;
+    else p.piece_base[xcd * (row + 1) + k + 1] = 0;
   }
   __syncthreads();   // (counts of all units written, by this workgroup)
-  for (int xcd = wave; xcd < 8; xcd += kWaves) {   // counts -> pieces before
+  for (int xcd = wave; xcd < 8; xcd += kStateWaves) {   // counts -> pieces before
     int32_t *base = p.piece_base + xcd * (row + 1);
     int run = 0;
     for (int i = 0; i < row; i += 64) {
-      int incl = i + lane < row ? base[i + lane + 1] : 0;
+      int incl = i + lane >= row ? 0 : row < 64 ? s_pieces[xcd * 64 + lane] : base[i + lane + 1];
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int t = __shfl_up(incl, o, 64);
@@ -544,6 +558,19 @@ struct Piece {
 };
 __device__ __forceinline__ bool find_piece(const ChunkParams &p, Piece &x) {
   const int lane = threadIdx.x & 63;
+  if (p.fixed_parts > 0) {
+    x.u = blockIdx.x / p.fixed_parts;
+    x.part = blockIdx.x - x.u * p.fixed_parts;
+    x.parts = p.fixed_parts;
+    x.record = blockIdx.x;
+    x.b = x.u / p.hkv;
+    x.g = x.u - x.b * p.hkv;
+    x.tile = 0;
+    x.start = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b], p.total));
+    const int end = __builtin_amdgcn_readfirstlane(clamp_token(p.cu[x.b + 1], p.total));
+    x.n = min(max(end - x.start, 0), p.max_chunk);
+    return x.n > 0;
+  }
   const int row = (p.units + 7) >> 3, slots = gridDim.x >> 3;
   int xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;   // (workgroup i runs on XCD i mod 8)
   const int mine = p.piece_base[(lane & 7) * (row + 1) + row];   // pieces of XCD `lane`
@@ -602,6 +629,12 @@ __device__ __forceinline__ int closed_before(const ChunkParams &p, const Piece &
 }
 __device__ __forceinline__ int visible_slots(const ChunkParams &p, int u) {
   return __builtin_amdgcn_readfirstlane(min(max(p.visible[u], 0), p.len[u]));
+}
+
+// Pieces of a unit's one tile where every unit has fixed_parts places: as many as
+// give each piece_min of its nb blocks, or one.
+__device__ __forceinline__ int fixed_parts_of(const ChunkParams &p, int nb) {
+  return max(1, min(p.fixed_parts, nb / p.piece_min));
 }
 
 // A page-table entry by a scalar load (uniform address; written by earlier launches).
@@ -666,6 +699,10 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
   const int lim_lo = cnt == T ? __builtin_amdgcn_readfirstlane(closed_before(p, x, a)) : 0;   // every column
   const int vis = visible_slots(p, x.u);
   const int nbc = (vis + 31) >> 5, nb = nbc + ((top + 31) >> 5);
+  if (p.fixed_parts > 0) {
+    x.parts = fixed_parts_of(p, nb);
+    if (x.part >= x.parts) return;
+  }
   const int b0 = static_cast<int>(int64_t(nb) * x.part / x.parts);
   const int b1 = static_cast<int>(int64_t(nb) * (x.part + 1) / x.parts);   // this piece's blocks
   const uint4 zero4 = make_uint4(0, 0, 0, 0);
@@ -1139,6 +1176,10 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams 
   const int lim_lo = cnt == T ? __builtin_amdgcn_readfirstlane(closed_before(p, x, a)) : 0;
   const int vis = visible_slots(p, x.u);
   const int nbc = (vis + 31) >> 5, nb = nbc + ((top + 31) >> 5);
+  if (p.fixed_parts > 0) {
+    x.parts = fixed_parts_of(p, nb);
+    if (x.part >= x.parts) return;
+  }
   const int b0 = static_cast<int>(int64_t(nb) * x.part / x.parts);
   const int b1 = static_cast<int>(int64_t(nb) * (x.part + 1) / x.parts);
 
@@ -1282,11 +1323,11 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams 
 }
 
 // The pieces of a tile put together: o = sum_i 2^(m_i - M) acc_i / sum_i
-// 2^(m_i - M) l_i.  One wave per column, lanes own D / 64 elements; records are
-// read four at a time.  Tiles of one piece have been written already.
+// 2^(m_i - M) l_i.  One wave per column, lanes own D / 64 elements; bound by latency:
+// records are read sixteen at a time.  Tiles of one piece have been written already.
 template <int ES, int D, int G, int COLS>
 __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) {
-  constexpr int E = D / 64, REC = D + 4, R = 4;
+  constexpr int E = D / 64, REC = D + 4, R = 16;
   const int g = blockIdx.y, lane = threadIdx.x & 63;
   const int c = blockIdx.z * kWaves + (threadIdx.x >> 6);
   const PackedTile pt = packed_tile(p.cu, p.rows, p.total, blockIdx.x, p.tile_shift);
@@ -1294,33 +1335,57 @@ __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) 
   const int t = (pt.tile << p.tile_shift) + c / G;
   if (pt.tile < 0 || t >= n) return;
   const int u = pt.seq * p.hkv + g;
-  const int parts = __builtin_amdgcn_readfirstlane(p.pieces[u]);
+  int parts, first;
+  if (p.fixed_parts > 0) {
+    const Piece x{u, pt.seq, g, pt.start, n, 0, 0, 0, 0};
+    const int nb = ((visible_slots(p, u) + 31) >> 5) + ((closed_before(p, x, n - 1) + 31) >> 5);
+    parts = fixed_parts_of(p, nb);
+    first = u * p.fixed_parts;
+  } else {
+    const int tiles = (n + (1 << p.tile_shift) - 1) >> p.tile_shift;
+    parts = p.pieces[u];
+    first = p.record_base[u] + (tiles - 1 - pt.tile) * parts;
+  }
+  parts = __builtin_amdgcn_readfirstlane(parts);
+  first = __builtin_amdgcn_readfirstlane(first);
   if (parts == 1) return;
-  const int tiles = (n + (1 << p.tile_shift) - 1) >> p.tile_shift;
-  const int first = __builtin_amdgcn_readfirstlane(p.record_base[u]) + (tiles - 1 - pt.tile) * parts;
   const float *rec = p.partials + (int64_t(first) * COLS + c) * REC;
   float M = lowest(), L = 0.0f, A[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) A[e] = 0.0f;
+  auto of_lane = [](float y, int j) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), j));
+  };
   for (int i0 = 0; i0 < parts; i0 += R) {
-    float mi[R], li[R], a[R][E];
+    // lane i < R reads record i's maximum and sum; every load of a batch in one round trip
+    const float *mine = rec + int64_t(min(i0 + (lane & (R - 1)), parts - 1)) * COLS * REC;
+    float mi = mine[0], li = mine[1], a[R][E];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      const float *r = rec + int64_t(min(i0 + j, parts - 1)) * COLS * REC;
-      mi[j] = r[0];
-      li[j] = r[1];
+      const float *r = rec + int64_t(min(i0 + j, parts - 1)) * COLS * REC + 4 + lane * E;
 #pragma unroll
-      for (int e = 0; e < E; ++e) a[j][e] = r[4 + lane * E + e];
+      for (int e = 0; e < E; ++e) a[j][e] = r[e];
     }
+    if (i0 + (lane & (R - 1)) >= parts) {   // (the last record again: without weight)
+      mi = lowest();
+      li = 0.0f;
+    }
+    float mn = M;
+#pragma unroll
+    for (int j = 0; j < R; ++j) mn = fmaxf(mn, of_lane(mi, j));
+    const float f = fast_exp2(M - mn), w = i0 + (lane & (R - 1)) < parts ? fast_exp2(mi - mn) : 0.0f;
+    M = mn;
+    L *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) A[e] *= f;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      if (i0 + j >= parts) break;
-      const float mn = fmaxf(M, mi[j]);
-      const float f = fast_exp2(M - mn), w = fast_exp2(mi[j] - mn);
-      M = mn;
-      L = L * f + w * li[j];
+      const float wj = of_lane(w, j);
+      if (i0 + j < parts) {
+        L = fmaf(wj, of_lane(li, j), L);
 #pragma unroll
-      for (int e = 0; e < E; ++e) A[e] = A[e] * f + w * a[j][e];
+        for (int e = 0; e < E; ++e) A[e] = fmaf(wj, a[j][e], A[e]);
+      }
     }
   }
   const float inv = 1.0f / L;
@@ -1333,8 +1398,9 @@ __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) 
 template <int ES, int D, bool VT>
 hipError_t chunk_states(const ChunkParams &p, hipStream_t s) {
   if (p.max_chunk > kBlock)
-    hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, SUMS>), dim3(p.blocks64, p.hkv), dim3(kThreads), 0, s, p);
-  hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, ATTEND>), dim3(p.blocks64 + 1, p.hkv), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, SUMS>), dim3(p.blocks64, p.hkv), dim3(kStateThreads), 0, s, p);
+  const int plan = p.fixed_parts > 0 ? 0 : 1;   // the workgroup that plans
+  hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, ATTEND>), dim3(p.blocks64 + plan, p.hkv), dim3(kStateThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -1351,7 +1417,8 @@ hipError_t chunk_attend(const ChunkParams &p, bool vt, bool wide, hipStream_t s)
   hipError_t e = vt ? chunk_states<ES, D, (ES == 2 && G >= 4)>(p, s) : chunk_states<ES, D, false>(p, s);
   if (e != hipSuccess) return e;
   const unsigned tiles = (p.total >> p.tile_shift) + p.rows;
-  const unsigned pieces = (tiles * p.hkv + p.piece_budget + 7) / 8 * 8;
+  const unsigned pieces = p.fixed_parts > 0 ? unsigned(p.units) * p.fixed_parts
+                                            : (tiles * p.hkv + p.piece_budget + 7) / 8 * 8;
   if constexpr (ES == 2) {
     if (vt) {
       if constexpr (G >= 4) attend_bf16<D, G, true, true>(p, wide, pieces, s);
@@ -1364,7 +1431,7 @@ hipError_t chunk_attend(const ChunkParams &p, bool vt, bool wide, hipStream_t s)
     hipLaunchKernelGGL((chunk_attend_f32_kernel<D, G>), dim3(pieces), dim3(kThreads), 0, s, p);
   }
   e = hipGetLastError();
-  if (e != hipSuccess || p.piece_budget == 0) return e;
+  if (e != hipSuccess || p.piece_budget == 0 || p.fixed_parts == 1) return e;
   if (wide)
     hipLaunchKernelGGL((chunk_combine_kernel<ES, D, G, 128>), dim3(tiles, p.hkv, 128 / kWaves), dim3(kThreads), 0, s, p);
   else
@@ -1385,12 +1452,12 @@ hipError_t attend_by_group(int group, const ChunkParams &p, bool vt, bool wide, 
 
 template <int ES, int D, bool VT>
 hipError_t chunk_append(const ChunkParams &p, hipStream_t s) {
-  const dim3 grid(p.blocks64, p.hkv), threads(kThreads);
+  const dim3 grid(p.blocks64, p.hkv), threads(kStateThreads);
   if (p.max_chunk <= kBlock) {
     hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, ONE>), grid, threads, 0, s, p);
   } else {
     hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, SUMS>), grid, threads, 0, s, p);
-    hipLaunchKernelGGL(chunk_grow_kernel, dim3((p.units + kWaves - 1) / kWaves), threads, 0, s, p);
+    hipLaunchKernelGGL(chunk_grow_kernel, dim3((p.units + kWaves - 1) / kWaves), dim3(kThreads), 0, s, p);
     hipLaunchKernelGGL((chunk_states_kernel<ES, D, VT, APPEND>), grid, threads, 0, s, p);
   }
   return hipGetLastError();

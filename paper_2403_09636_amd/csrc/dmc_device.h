@@ -240,6 +240,18 @@ struct PackedTile {
 // The sequence and tile of tile index idx, by the whole wave (64 candidates a step).
 __device__ __forceinline__ PackedTile packed_tile(const int32_t *cu, int seqs, int total, int idx, int shift) {
   const int lane = threadIdx.x & 63;
+  if (seqs < 64) {   // every boundary in one load
+    const int start = clamp_token(cu[min(lane, seqs)], total);
+    const bool le = lane == 0 || (lane < seqs && (start >> shift) + lane <= idx);
+    const int k = 63 - __clzll(static_cast<long long>(__ballot(le)));
+    PackedTile t;
+    t.seq = k;
+    t.start = __builtin_amdgcn_readlane(start, k);
+    const int end = __builtin_amdgcn_readlane(start, k + 1);
+    t.n = end > t.start ? end - t.start : 0;
+    t.tile = idx - ((t.start >> shift) + k);
+    return t;
+  }
   int lo = 0, n = seqs;   // the answer lies in [lo, lo + n)
   while (n > 1) {
     const int step = (n + 63) >> 6, i = lo + lane * step;

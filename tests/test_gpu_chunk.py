@@ -376,3 +376,33 @@ def test_refusals(torch_cuda):
         assert call(False, **kw) == 1 and msg in Bd.last_error()
     torch.cuda.synchronize()
     assert c.cache.lengths(0).tolist() == [[5, 6], [7, 0]]
+
+
+def test_append_alone_flags_boundaries(torch_cuda):
+    for cu in ([0, 12, 5], [-1, 4, 9], [0, 4, 99]):
+        c = Case(4, 2, 64, "bf16", [[20, 20], [9, 9]], max_chunk=16)
+        q, k, v = c.tokens([20])
+        c.chunk.append(0, k, v, q, torch.tensor(cu, dtype=torch.int32, device="cuda"))
+        assert c.cache.status() == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("chunk", [3, 30])
+def test_many_units_are_planned(torch_cuda, dtype, chunk):
+    """More than 64 units (pieces planned by their lengths), ragged, some empty, some far longer; sampled rows."""
+    rng = np.random.default_rng(1)
+    B, hkv = 40, 2
+    slots = rng.integers(0, 60, (B, hkv))
+    slots[3] = (1500, 4)
+    slots[17] = 0
+    lens = [int(x) for x in rng.integers(0, chunk + 1, B)]
+    lens[3], lens[17] = chunk, chunk
+    c = Case(4, hkv, 64, dtype, slots, max_tokens=sum(lens), max_chunk=chunk, extra=64)
+    q, k, v = c.tokens(lens, 2.0)
+    out = f64(c.chunk.attend(0, q, k, v, cu_of(lens).cuda()))
+    c.ref.units = [c.ref.units[b] for b in (3, 17, 30)]
+    lo = np.concatenate([[0], np.cumsum(lens)])
+    rows = np.concatenate([np.arange(lo[b], lo[b + 1]) for b in (3, 17, 30)])
+    want, bound, _ = c.ref.chunk(*(f64(t)[rows] for t in (q, k, v)), [lens[b] for b in (3, 17, 30)])
+    assert (np.abs(out[rows] - want) <= bound).all()
+    c.cache.check()
