@@ -432,22 +432,25 @@ typedef struct dmc_causal_config {
   int32_t dtype;             /* dmc_dtype of q, k, v, out and the gradients */
 } dmc_causal_config;
 
-/* Bytes of workspace of dmc_causal_backward for up to total_tokens tokens (the
- * rows' statistics); 0 if invalid (see dmc_last_error). */
+/* Bytes of workspace of both calls for up to total_tokens tokens (the rows'
+ * statistics, and partial sums where few tiles are shared out to more
+ * workgroups); 0 if invalid (see dmc_last_error). */
 size_t dmc_causal_workspace_bytes(const dmc_causal_config *cfg, int32_t total_tokens);
 
-/* Forward: out_dev [total, Hq, d] and lse_dev. */
+/* Forward: out_dev [total, Hq, d] and lse_dev.  workspace_dev: caller-owned device
+ * memory, 256-byte aligned; it carries nothing between calls, and calls that may
+ * overlap need one each. */
 dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q_dev,
                               const int64_t q_strides[2], const void *k_dev,
                               const int64_t k_strides[2], const void *v_dev,
                               const int64_t v_strides[2], const int32_t *cu_seqlens_dev,
                               int32_t num_seqs, int32_t total_tokens, void *out_dev,
-                              const int64_t out_strides[2], float *lse_dev, dmc_stream_t stream);
+                              const int64_t out_strides[2], float *lse_dev,
+                              void *workspace_dev, size_t workspace_bytes, dmc_stream_t stream);
 
 /* Backward: gradients of sum(out * dout) with respect to q, k and v (summed
  * over the query heads of a kv head's group), given the forward's inputs, out
- * and lse.  workspace_dev: caller-owned device memory, 256-byte aligned; it
- * carries nothing between calls, and calls that may overlap need one each. */
+ * and lse.  workspace_dev as for the forward. */
 dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q_dev,
                                const int64_t q_strides[2], const void *k_dev,
                                const int64_t k_strides[2], const void *v_dev,

@@ -113,7 +113,7 @@ def _load():
     lib.dmc_causal_workspace_bytes.argtypes = [POINTER(CausalConfig), c_int32]
     lib.dmc_causal_workspace_bytes.restype = c_size_t
     lib.dmc_causal_forward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
-                                       *packed, c_void_p, c_void_p]
+                                       *packed, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.dmc_causal_backward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
                                         *packed, c_void_p, *packed * 4, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
@@ -767,7 +767,7 @@ def _packed_args(*tensors):
 
 class DMCCausal:
     """Plain causal attention of packed sequences (forward + backward), for layers without
-    compression; the backward's workspace, for up to max_tokens tokens, is one torch allocation."""
+    compression; the workspace, for up to max_tokens tokens, is one torch allocation."""
 
     def __init__(self, cfg: CausalConfig, max_tokens, device="cuda"):
         import torch
@@ -801,9 +801,12 @@ class DMCCausal:
         if args is None or lp is None or cu is None:
             check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse)
             args, lp, cu = _packed_args(q, k, v, out), lse.data_ptr(), cu_seqlens.data_ptr()
+        if T > self.max_tokens:
+            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
         (qp, kp, vp, op), st = args
         check(lib.dmc_causal_forward(self._cfg_ref, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
-                                     cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, _stream(stream)))
+                                     cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, self._ws,
+                                     self._ws_bytes, _stream(stream)))
         return out, lse
 
     def backward(self, q, k, v, cu_seqlens, out, lse, dout, dq=None, dk=None, dv=None, stream=None):

@@ -878,25 +878,28 @@ static dmc_status check_packed_counts(int32_t num_seqs, int32_t total) {
 static size_t causal_stats_bytes(const dmc_causal_config &c, int32_t total) {
   return align_up(size_t(c.num_q_heads) * (size_t(total) + 32) * 8, 256);
 }
-// Bytes of the parts of dK (and of dV) of up to `total` tokens: what the fewest
-// compute-unit-filling parts of any number of sequences take.
-static size_t causal_part_bytes(const dmc_causal_config &c, int32_t total, int parts) {
-  return parts > 1 ? align_up(size_t(parts) * total * c.num_kv_heads * c.head_dim * 4, 256) : 0;
+// Bytes of `parts` parts of `heads` rows of `floats` for each of `total` tokens.
+static size_t causal_part_bytes(int32_t total, int parts, int heads, int floats) {
+  return parts > 1 ? align_up(size_t(parts) * total * heads * floats * 4, 256) : 0;
 }
-constexpr int kWorkspaceUnits = 256;   // compute units that the parts are planned for
-static int causal_parts(const dmc_causal_config &c, int32_t seqs, int32_t total) {
-  return dmc::causal_key_parts(c.dtype == DMC_FP32 ? 4 : 2, c.num_q_heads, c.num_kv_heads, seqs, total, kWorkspaceUnits);
+// The most of that for up to `total` tokens in any number of sequences: fewer tokens
+// may be cut into more parts, but parts times tiles stay within `places`.
+static size_t causal_most_part_bytes(int32_t total, int max_parts, int places, int tile, int heads, int floats) {
+  size_t most = 0;
+  for (int parts = 2; parts <= max_parts; ++parts) {
+    const int64_t tokens = std::min<int64_t>(total, places / (int64_t(parts) * heads) * tile);
+    if (tokens > 0) most = std::max(most, causal_part_bytes(static_cast<int32_t>(tokens), parts, heads, floats));
+  }
+  return most;
 }
 static size_t causal_workspace(const dmc_causal_config &c, int32_t total) {
-  // fewer tokens may be cut into more parts, but parts x tiles stays below 4 units'
-  // worth, with 128 tokens in a tile (and 16 parts of what one tile holds)
-  size_t most = 0;
-  for (int parts = 2; parts <= dmc::kMaxKeyParts; ++parts) {
-    const int64_t tiles = int64_t(4) * kWorkspaceUnits / (int64_t(parts) * c.num_kv_heads);   // (of one head)
-    const int64_t tokens = std::min<int64_t>(total, tiles * 128);
-    if (tokens > 0) most = std::max(most, causal_part_bytes(c, static_cast<int32_t>(tokens), parts));
-  }
-  return causal_stats_bytes(c, total) + (c.dtype == DMC_BF16 ? 2 * most : 0);
+  const bool bf16 = c.dtype == DMC_BF16;
+  return causal_stats_bytes(c, total) +
+         2 * causal_most_part_bytes(total, dmc::kMaxKeyParts, dmc::kPartPlaces, bf16 ? 128 : 32, c.num_kv_heads,
+                                    c.head_dim) +
+         (bf16 ? causal_most_part_bytes(total, dmc::kMaxQueryParts, dmc::kQueryPartPlaces, 128, c.num_q_heads,
+                                        c.head_dim + 4)
+               : 0);
 }
 
 static void copy_strides(int64_t (&dst)[2], const int64_t *src) {
@@ -904,16 +907,35 @@ static void copy_strides(int64_t (&dst)[2], const int64_t *src) {
   dst[1] = src[1];
 }
 
-static void causal_params(const dmc_causal_config &c, const int32_t *cu, int32_t seqs, int32_t total, dmc::CausalParams *p) {
+static void causal_params(const dmc_causal_config &c, const int32_t *cu, int32_t seqs, int32_t total, void *ws,
+                          dmc::CausalParams *p) {
   p->cu = cu;
   p->seqs = seqs;
   p->total = total;
   p->hq = c.num_q_heads;
   p->hkv = c.num_kv_heads;
   p->stat_stride = int64_t(total) + 32;
-  p->compute_units = kWorkspaceUnits;
-  p->parts = 1;
   p->scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(c.head_dim)));
+  const dmc::CausalParts parts = dmc::causal_parts(c.dtype == DMC_FP32 ? 4 : 2, c.num_q_heads, c.num_kv_heads, seqs, total);
+  p->parts = parts.keys;
+  p->query_parts = parts.queries;
+  char *w = static_cast<char *>(ws);
+  const size_t keys = causal_part_bytes(total, parts.keys, c.num_kv_heads, c.head_dim);
+  p->stats = reinterpret_cast<float *>(w);
+  w += causal_stats_bytes(c, total);
+  p->part_k = reinterpret_cast<float *>(w);
+  p->part_v = reinterpret_cast<float *>(w + keys);
+  p->part_q = reinterpret_cast<float *>(w + 2 * keys);
+}
+
+// Checks of the workspace of a causal call.
+static dmc_status check_causal_workspace(const dmc_causal_config &c, int32_t total, const void *ws, size_t bytes) {
+  if (!ws) return fail(DMC_ERR_INVALID_ARG, "workspace must be non-NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u)
+    return fail(DMC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (bytes < causal_workspace(c, total))
+    return fail(DMC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", bytes, causal_workspace(c, total));
+  return DMC_OK;
 }
 
 // Whether a launch with one workgroup per head and tile (of at least 32 tokens) fits a grid.
@@ -931,7 +953,7 @@ dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q, const
                               const void *k, const int64_t k_strides[2], const void *v,
                               const int64_t v_strides[2], const int32_t *cu, int32_t num_seqs,
                               int32_t total, void *out, const int64_t out_strides[2], float *lse,
-                              dmc_stream_t stream) {
+                              void *ws, size_t bytes, dmc_stream_t stream) {
   dmc_status st = validate_causal(cfg);
   if (st == DMC_OK) st = check_packed_counts(num_seqs, total);
   if (st != DMC_OK) return st;
@@ -946,10 +968,12 @@ dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q, const
     if (st != DMC_OK) return st;
   }
   if (!cu || !lse) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens and lse must be non-NULL");
+  st = check_causal_workspace(*cfg, total, ws, bytes);
+  if (st != DMC_OK) return st;
   if (!causal_grid_fits(*cfg, num_seqs, total))
     return fail(DMC_ERR_UNSUPPORTED, "too many tokens and sequences for one launch");
   dmc::CausalParams p{};
-  causal_params(*cfg, cu, num_seqs, total, &p);
+  causal_params(*cfg, cu, num_seqs, total, ws, &p);
   p.q = q;
   p.k = k;
   p.v = v;
@@ -960,7 +984,7 @@ dmc_status dmc_causal_forward(const dmc_causal_config *cfg, const void *q, const
   copy_strides(p.vs, v_strides);
   copy_strides(p.os, out_strides);
   int dev = 0;
-  st = memory_device(out, "out", &dev);
+  st = memory_device(ws, "the workspace", &dev);
   if (st != DMC_OK) return st;
   DeviceGuard g(dev);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the tensors' device");
@@ -994,15 +1018,13 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, cons
     st = check_packed(t, total, cfg->head_dim, es);
     if (st != DMC_OK) return st;
   }
-  if (!cu || !lse || !ws) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens, lse and workspace must be non-NULL");
-  if (reinterpret_cast<uintptr_t>(ws) & 255u)
-    return fail(DMC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  if (bytes < causal_workspace(*cfg, total))
-    return fail(DMC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", bytes, causal_workspace(*cfg, total));
+  if (!cu || !lse) return fail(DMC_ERR_INVALID_ARG, "cu_seqlens and lse must be non-NULL");
+  st = check_causal_workspace(*cfg, total, ws, bytes);
+  if (st != DMC_OK) return st;
   if (!causal_grid_fits(*cfg, num_seqs, total))
     return fail(DMC_ERR_UNSUPPORTED, "too many tokens and sequences for one launch");
   dmc::CausalParams p{};
-  causal_params(*cfg, cu, num_seqs, total, &p);
+  causal_params(*cfg, cu, num_seqs, total, ws, &p);
   p.q = q;
   p.k = k;
   p.v = v;
@@ -1012,11 +1034,6 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q, cons
   p.dq = dq;
   p.dk = dk;
   p.dv = dv;
-  p.parts = causal_parts(*cfg, num_seqs, total);
-  char *w = static_cast<char *>(ws);
-  p.stats = reinterpret_cast<float *>(w);
-  p.part_k = reinterpret_cast<float *>(w + causal_stats_bytes(*cfg, total));
-  p.part_v = reinterpret_cast<float *>(w + causal_stats_bytes(*cfg, total) + causal_part_bytes(*cfg, total, p.parts));
   copy_strides(p.qs, q_strides);
   copy_strides(p.ks, k_strides);
   copy_strides(p.vs, v_strides);

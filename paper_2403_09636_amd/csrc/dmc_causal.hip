@@ -124,6 +124,10 @@ __device__ __forceinline__ PackedTile tile_of_rank(const CausalParams &p, int ra
   return packed_tile(p.cu, p.seqs, p.total, REVERSED ? rank : ntiles - 1 - rank, shift);
 }
 
+// Parts that a query tile of `blocks` key blocks is cut into, four blocks or more
+// each (of up to `most`).
+__device__ __forceinline__ int tile_parts(int most, int blocks) { return max(1, min(most, blocks >> 2)); }
+
 // Row `token`, head `h` of a strided tensor of ES-byte elements.
 template <int ES>
 __device__ __forceinline__ const char *row_at(const void *base, const int64_t (&st)[2], int64_t token, int h) {
@@ -170,8 +174,11 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
   const int t = a + col;
   const bool colv = t < n;
   const int64_t token = pt.start + (colv ? t : 0);
-  const int nblk = (min(n, pt.tile * kTile + kTile) + 31) >> 5;
-  const int wave_hi = a < n ? min(a + 32, n) : 0;   // keys < wave_hi feed this wave
+  // The tile's key blocks; this workgroup's part of them.
+  const int all = (min(n, pt.tile * kTile + kTile) + 31) >> 5, parts = tile_parts(p.query_parts, all), share = blockIdx.y;
+  if (share >= parts) return;
+  const int blk0 = all * share / parts, nblk = all * (share + 1) / parts;
+  const int wave_hi = a < n ? min(min(a + 32, n), nblk * 32) : 0;   // keys < wave_hi feed this wave
   const int g = h / (p.hq / p.hkv);
   const uint4 zero4 = make_uint4(0, 0, 0, 0);
   const float sl2 = p.scale_log2;
@@ -197,7 +204,31 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
       }
       Dc = part + __shfl_xor(part, 32, 64);
       if (colv) Lc = p.lse[token * p.hq + h] * kLog2e;
-      if (colv && hb == 0) {   // for the key kernels
+      // D from the rounded outputs is off by up to 2^-8 |dO . o|, which shows in the
+      // gradients of rows of few keys (their outputs are as large as the values; over n
+      // keys they average out to n^-1/2 of it).  As the probabilities of a row add up
+      // to 1, sum dS is what D lacks: a sequence's first tile, at most four blocks,
+      // takes it from there first.
+      if (pt.tile == 0 && a < n) {
+        float lack = 0.0f;
+        const char *k0 = row_at<2>(p.k, p.ks, pt.start, g), *v0 = row_at<2>(p.v, p.vs, pt.start, g);
+#pragma unroll 1
+        for (int kb = 0; kb * 32 <= a; ++kb) {
+          const int64_t row = min(kb * 32 + score_slot(col), n - 1);
+          f32x16_t sc = f32x16_t{}, dp = f32x16_t{};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            sc = mfma_32x32x16(ld16(k0 + row * p.ks[0] * 2 + ks * 32 + hb * 16), qop[ks], sc);
+            dp = mfma_32x32x16(ld16(v0 + row * p.vs[0] * 2 + ks * 32 + hb * 16), dop[ks], dp);
+          }
+          const int tr = one_register(kb * 32 == a ? col - 8 * hb : 32);
+#pragma unroll
+          for (int rr = 0; rr < 16; ++rr)
+            lack += score_row(rr) <= tr ? fast_exp2(fmaf(sc[rr], sl2, -Lc)) * (dp[rr] - Dc) : 0.0f;
+        }
+        Dc += lack + __shfl_xor(lack, 32, 64);
+      }
+      if (colv && hb == 0 && share == 0) {   // for the key kernels
         *reinterpret_cast<float2 *>(p.stats + (h * p.stat_stride + token) * 2) = make_float2(Lc, Dc);
       }
     }
@@ -244,12 +275,12 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
   tr_offsets<D, MODE == 0 ? VSW : KSW>(lane, traddr);
   bool left_out = false;
 
-  issue(0, std::integral_constant<int, 0>{});
-  issue(1, std::integral_constant<int, 1>{});
-  issue(2, std::integral_constant<int, 2>{});
+  issue(blk0, std::integral_constant<int, 0>{});
+  issue(blk0 + 1, std::integral_constant<int, 1>{});
+  issue(blk0 + 2, std::integral_constant<int, 2>{});
   if constexpr (MODE == 0) {
     f32x16_t scn = f32x16_t{};
-    wait_vmcnt<(kSt - 2) * 2 * DPW>();   // block 0 has landed
+    wait_vmcnt<(kSt - 2) * 2 * DPW>();   // the first block has landed
     ring_barrier();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -332,7 +363,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
     };
     // Whole rounds of four steps (a step past the last block only keeps the
     // barriers and transfer counts in step).
-    for (int kb = 0; kb < nblk; kb += kSt) {
+    for (int kb = blk0; kb < nblk; kb += kSt) {
       step(std::integral_constant<int, 0>{}, kb);
       step(std::integral_constant<int, 1>{}, kb + 1);
       step(std::integral_constant<int, 2>{}, kb + 2);
@@ -412,7 +443,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
 #pragma unroll
       for (int j = 0; j < 2 * NTL; ++j) acc[j >> 1] = mfma_32x32x16(kt[j], sb[j & 1], acc[j >> 1]);
     };
-    for (int kb = 0; kb < nblk; kb += kSt) {
+    for (int kb = blk0; kb < nblk; kb += kSt) {
       step(std::integral_constant<int, 0>{}, kb);
       step(std::integral_constant<int, 1>{}, kb + 1);
       step(std::integral_constant<int, 2>{}, kb + 2);
@@ -429,6 +460,20 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
   // Lane holds dims 32 i + 8 j + 4 hb .. + 4 of its column.
   const float lt = ls + __shfl_xor(ls, 32, 64);
   if (!colv) return;
+  if (parts > 1) {   // this part's record: the sums, and in the forward the maximum and sum of the weights
+    float *rec = p.part_q + ((int64_t(share) * p.total + token) * p.hq + h) * (D + 4);
+    if (MODE == 0 && hb == 0) {
+      rec[0] = m;
+      rec[1] = lt;
+    }
+#pragma unroll
+    for (int i = 0; i < NTL; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4 *>(rec + 4 + 32 * i + 8 * j + 4 * hb) =
+            make_float4(acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]);
+    return;
+  }
   char *orow = const_cast<char *>(MODE == 0 ? row_at<2>(p.out, p.os, token, h) : row_at<2>(p.dq, p.dqs, token, h));
   float scale;
   if constexpr (MODE == 0) {
@@ -696,9 +741,58 @@ __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p)
     }
 }
 
+// The parts of a query row put together, in their order, one wave per row and head:
+// outputs (MODE 0: with the weights 2^(m - M) of their maxima, and the row's log
+// sum exp) or dQ.
+template <int D, int MODE>
+__global__ __launch_bounds__(kThreads) void causal_query_parts_kernel(CausalParams p, int ntiles) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int wid = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int h = wid % p.hq, row = wid / p.hq;   // (tile index, row of the tile)
+  const PackedTile pt = packed_tile(p.cu, p.seqs, p.total, row >> kTileShift, kTileShift);
+  const int t = pt.tile * kTile + (row & (kTile - 1));
+  if (row >= ntiles * kTile || pt.tile < 0 || t >= pt.n) return;
+  const int parts = tile_parts(p.query_parts, (min(pt.n, pt.tile * kTile + kTile) + 31) >> 5);
+  if (parts == 1) return;
+  const int64_t token = pt.start + t, step = int64_t(p.total) * p.hq * (D + 4);
+  const float *rec = p.part_q + (token * p.hq + h) * (D + 4);
+  float M = lowest(), L = 0.0f, A[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) A[e] = 0.0f;
+  float m[kMaxQueryParts], l[kMaxQueryParts], a[kMaxQueryParts][E];
+#pragma unroll
+  for (int i = 0; i < kMaxQueryParts; ++i) {   // (every load in flight; past the parts, the last one again)
+    const float *r = rec + min(i, parts - 1) * step;
+    m[i] = r[0];
+    l[i] = r[1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[i][e] = r[4 + lane * E + e];
+  }
+  if constexpr (MODE == 0) {
+#pragma unroll
+    for (int i = 0; i < kMaxQueryParts; ++i) M = fmaxf(M, m[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxQueryParts; ++i) {
+    if (i < parts) {
+      const float w = MODE == 0 ? fast_exp2(m[i] - M) : 1.0f;
+      L = fmaf(w, l[i], L);
+#pragma unroll
+      for (int e = 0; e < E; ++e) A[e] = fmaf(w, a[i][e], A[e]);
+    }
+  }
+  const float scale = MODE == 0 ? 1.0f / L : p.scale_log2 / kLog2e;
+#pragma unroll
+  for (int e = 0; e < E; ++e) A[e] *= scale;
+  const char *o = MODE == 0 ? row_at<2>(p.out, p.os, token, h) : row_at<2>(p.dq, p.dqs, token, h);
+  store_e<2, E>(const_cast<char *>(o) + lane * E * 2, A);
+  if (MODE == 0 && lane == 0) p.lse[token * p.hq + h] = (M + __log2f(L)) * kLn2;
+}
+
 // The parts of dK and dV put together, in their order: one thread per 4 elements of
 // a row of a kv head, for the tokens inside the sequences.
-template <int D>
+template <int ES, int D>
 __global__ __launch_bounds__(kThreads) void causal_parts_kernel(CausalParams p) {
   const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
   const int first = clamp_token(p.cu[0], p.total), end = clamp_token(p.cu[p.seqs], p.total);
@@ -715,10 +809,15 @@ __global__ __launch_bounds__(kThreads) void causal_parts_kernel(CausalParams p) 
     k.x += a.x; k.y += a.y; k.z += a.z; k.w += a.w;
     v.x += b.x; v.y += b.y; v.z += b.z; v.w += b.w;
   }
-  *reinterpret_cast<uint2 *>(const_cast<char *>(row_at<2>(p.dk, p.dks, token, g)) + e * 2) =
-      make_uint2(cvt_pk_bf16(k.x, k.y), cvt_pk_bf16(k.z, k.w));
-  *reinterpret_cast<uint2 *>(const_cast<char *>(row_at<2>(p.dv, p.dvs, token, g)) + e * 2) =
-      make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
+  char *dk = const_cast<char *>(row_at<ES>(p.dk, p.dks, token, g)) + e * ES;
+  char *dv = const_cast<char *>(row_at<ES>(p.dv, p.dvs, token, g)) + e * ES;
+  if constexpr (ES == 2) {
+    *reinterpret_cast<uint2 *>(dk) = make_uint2(cvt_pk_bf16(k.x, k.y), cvt_pk_bf16(k.z, k.w));
+    *reinterpret_cast<uint2 *>(dv) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
+  } else {
+    *reinterpret_cast<float4 *>(dk) = k;
+    *reinterpret_cast<float4 *>(dv) = v;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -872,7 +971,10 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
   const int G = p.hq / p.hkv;
   const int js = s0 + col;   // this lane's key
   const bool kv_ok = js < n;
-  const int qb0 = pt.tile, per_head = ((n + 31) >> 5) - qb0, nblk = G * per_head;   // the first of a head holds the diagonal
+  // Row blocks that see the tile, of every head in turn (the first of a head holds the
+  // diagonal); this workgroup's part of them.
+  const int qb0 = pt.tile, per_head = ((n + 31) >> 5) - qb0, part = blockIdx.y;
+  const int blk0 = G * per_head * part / p.parts, nblk = G * per_head * (part + 1) / p.parts;
 
   auto key_row = [&](const void *base, const int64_t (&st)[2], int c) -> const float * {
     return s0 + c < n ? reinterpret_cast<const float *>(row_at<4>(base, st, pt.start + s0 + c, g)) : nullptr;
@@ -897,7 +999,7 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
   auto q_at = [&](int hh, int r) { return reinterpret_cast<const float *>(row_at<4>(p.q, p.qs, pt.start + min(r, n - 1), hh)); };
   auto do_at = [&](int hh, int r) { return reinterpret_cast<const float *>(row_at<4>(p.dout, p.dos, pt.start + min(r, n - 1), hh)); };
   int hh, rb;
-  at(min(wave, nblk - 1), hh, rb);
+  at(min(blk0 + wave, G * per_head - 1), hh, rb);
   F::load_row(qr, q_at(hh, rb + col), hb);
   bool out_v = false, out_k = false;
   auto block = [&](int i, auto masked_c, bool masked) {
@@ -925,7 +1027,7 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
     f32x16_t dp = f32x16_t{};
     if constexpr (DK) dp = F::dots(dor, vst);
     int hn, rn;
-    at(min(i + kWaves, nblk - 1), hn, rn);
+    at(min(i + kWaves, G * per_head - 1), hn, rn);
     F::load_row(qr, q_at(hn, rn + col), hb);
     float pv[16], ds[16];
 #pragma unroll
@@ -939,7 +1041,7 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
     if constexpr (DK) out_k |= F::template add_rows<MASKED>(dk, qc, q_row, ds, lane, masked);
   };
 #pragma unroll 1
-  for (int i = wave; i < nblk; i += kWaves) {
+  for (int i = blk0 + wave; i < nblk; i += kWaves) {
     at(i, hh, rb);
     const bool masked = rb == s0 || rb + 32 > n;
     // (PART 2: the masked sums in a body of their own -- beside the others they spilled two
@@ -948,7 +1050,7 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
     else block(i, std::false_type{}, false);
   }
   if (__any(out_v || out_k)) {
-    for (int i = wave; i < nblk; i += kWaves) {
+    for (int i = blk0 + wave; i < nblk; i += kWaves) {
       at(i, hh, rb);
       if (!(rb == s0 || rb + 32 > n)) continue;
       auto sees = [&](int r) { return kv_ok && rb + r >= js && rb + r < n; };
@@ -956,19 +1058,21 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
       if constexpr (DK) F::add_nonfinite(dk, [&](int r) { return q_at(hh, rb + r); }, sees, lane);
     }
   }
-  auto emit = [&](void *out, const int64_t (&st)[2]) {   // the merged rows of the tile's keys
+  auto emit = [&](void *out, const int64_t (&st)[2], float *share) {   // the merged rows of the tile's keys
     __syncthreads();
     for (int i = tid; i < 32 * D / 4; i += kThreads) {
       const int c = i / (D / 4), e = i % (D / 4);
-      if (s0 + c < n)
-        *reinterpret_cast<typename F::f4_t *>(const_cast<char *>(row_at<4>(out, st, pt.start + s0 + c, g)) + 16 * e) =
-            F::sum(s_acc, c, e);
+      if (s0 + c >= n) continue;
+      const int64_t token = pt.start + s0 + c;
+      char *o = p.parts > 1 ? reinterpret_cast<char *>(share + ((int64_t(part) * p.total + token) * p.hkv + g) * D)
+                            : const_cast<char *>(row_at<4>(out, st, token, g));
+      *reinterpret_cast<typename F::f4_t *>(o + 16 * e) = F::sum(s_acc, c, e);
     }
   };
   __syncthreads();   // the staged rows' last use
   if constexpr (DV) {
     F::put(s_acc, wave, lane, dv);
-    emit(p.dv, p.dvs);
+    emit(p.dv, p.dvs, p.part_v);
     if constexpr (DK) __syncthreads();   // the merge area is reused
   }
   if constexpr (DK) {
@@ -976,7 +1080,7 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
 #pragma unroll
     for (int i = 0; i < NT; ++i) dk[i] *= scale;
     F::put(s_acc, wave, lane, dk);
-    emit(p.dk, p.dks);
+    emit(p.dk, p.dks, p.part_k);
   }
 }
 
@@ -988,11 +1092,18 @@ __global__ __launch_bounds__(kThreads) void causal_key_f32_kernel(CausalParams p
 // tokens, 32/8 heads, dV 718 -> 616, dK 911 -> 766; forward of 16 x 500 tokens,
 // 8 heads, d = 64, 20.7 -> 16.3, but of 4 x 4096, 32 heads, 582 -> 611.
 bool sort_tiles(const CausalParams &p, int64_t workgroups) {
-  return p.seqs <= kSortSeqs && workgroups > 2 * p.compute_units;
+  return p.seqs <= kSortSeqs && workgroups > kPartPlaces / 2;
 }
 bool sort_queries(const CausalParams &p, int64_t workgroups, int row_bytes) {
   const int64_t heads = (p.hkv + 7) / 8;
   return sort_tiles(p, workgroups) && heads * p.total * 2 * row_bytes <= (4 << 20);
+}
+
+template <int D, int MODE>
+void launch_query_parts(const CausalParams &p, int ntiles, hipStream_t s) {
+  if (p.query_parts > 1)
+    hipLaunchKernelGGL((causal_query_parts_kernel<D, MODE>),
+                       dim3(unsigned((int64_t(ntiles) * kTile * p.hq + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, p, ntiles);
 }
 
 template <int D>
@@ -1002,10 +1113,13 @@ hipError_t causal_forward(int elem_bytes, CausalParams p, hipStream_t s) {
   const int64_t blocks = int64_t(ntiles) * p.hq;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   p.sorted = sort_queries(p, blocks, D * elem_bytes);
-  if (elem_bytes == 2)
-    hipLaunchKernelGGL((causal_query_kernel<D, 0>), dim3(unsigned(blocks)), dim3(kThreads), 0, s, p, ntiles);
-  else
-    hipLaunchKernelGGL((causal_query_f32_kernel<D, 0>), dim3(unsigned(blocks)), dim3(kThreads), 0, s, p, ntiles);
+  const dim3 grid(unsigned(blocks), elem_bytes == 2 ? p.query_parts : 1), threads(kThreads);
+  if (elem_bytes == 2) {
+    hipLaunchKernelGGL((causal_query_kernel<D, 0>), grid, threads, 0, s, p, ntiles);
+    launch_query_parts<D, 0>(p, ntiles, s);
+  } else {
+    hipLaunchKernelGGL((causal_query_f32_kernel<D, 0>), grid, threads, 0, s, p, ntiles);
+  }
   return hipGetLastError();
 }
 
@@ -1014,37 +1128,43 @@ hipError_t causal_backward(int elem_bytes, CausalParams p, hipStream_t s) {
   const int shift = elem_bytes == 2 ? kTileShift : kTileShift32;
   const int ntiles = (p.total >> shift) + p.seqs;
   if (int64_t(ntiles) * p.hq > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const dim3 queries(unsigned(ntiles) * p.hq), threads(kThreads);
+  const dim3 queries(unsigned(ntiles) * p.hq, elem_bytes == 2 ? p.query_parts : 1), threads(kThreads);
   const dim3 keys(unsigned(ntiles) * p.hkv, p.parts);
+  const dim3 rows(unsigned((int64_t(p.total) * p.hkv * (D / 4) + kThreads - 1) / kThreads));
   p.sorted = sort_queries(p, queries.x, D * elem_bytes);
   if (elem_bytes == 2) {
     hipLaunchKernelGGL((causal_query_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
+    launch_query_parts<D, 1>(p, ntiles, s);
     p.sorted = sort_tiles(p, int64_t(keys.x) * keys.y);
     hipLaunchKernelGGL((causal_key_kernel<D, 1>), keys, threads, 0, s, p);
     hipLaunchKernelGGL((causal_key_kernel<D, 2>), keys, threads, 0, s, p);
-    if (p.parts > 1)
-      hipLaunchKernelGGL((causal_parts_kernel<D>), dim3(unsigned((int64_t(p.total) * p.hkv * (D / 4) + kThreads - 1) / kThreads)),
-                         threads, 0, s, p);
+    if (p.parts > 1) hipLaunchKernelGGL((causal_parts_kernel<2, D>), rows, threads, 0, s, p);
   } else {
     hipLaunchKernelGGL((causal_query_f32_kernel<D, 1>), queries, threads, 0, s, p, ntiles);
-    p.sorted = sort_tiles(p, keys.x);
+    p.sorted = sort_tiles(p, int64_t(keys.x) * keys.y);
     if constexpr (D == 64) {
       hipLaunchKernelGGL((causal_key_f32_kernel<D, 0>), keys, threads, 0, s, p);
     } else {
       hipLaunchKernelGGL((causal_key_f32_kernel<D, 1>), keys, threads, 0, s, p);
       hipLaunchKernelGGL((causal_key_f32_kernel<D, 2>), keys, threads, 0, s, p);
     }
+    if (p.parts > 1) hipLaunchKernelGGL((causal_parts_kernel<4, D>), rows, threads, 0, s, p);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-int causal_key_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total, int compute_units) {
-  if (elem_bytes != 2 || seqs < 1) return 1;
-  const int64_t tiles = (total >> kTileShift) + 1, chain = (hq / hkv) * (total / seqs / 32);
-  const int64_t parts = std::min<int64_t>(4 * compute_units / (tiles * hkv), chain / 8);
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(parts, kMaxKeyParts)));
+CausalParts causal_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total) {
+  CausalParts x{1, 1};
+  if (seqs < 1) return x;
+  const int64_t tiles = (total >> (elem_bytes == 2 ? kTileShift : kTileShift32)) + 1;   // of one head
+  const int64_t blocks = total / seqs / 32;                                              // of the average sequence
+  const int64_t keys = std::min<int64_t>(kPartPlaces / (tiles * hkv), (hq / hkv) * blocks / (elem_bytes == 2 ? 8 : 4));
+  const int64_t queries = std::min<int64_t>(kQueryPartPlaces / (tiles * hq), blocks / 8);
+  x.keys = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(keys, kMaxKeyParts)));
+  if (elem_bytes == 2) x.queries = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(queries, kMaxQueryParts)));
+  return x;
 }
 
 hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s) {

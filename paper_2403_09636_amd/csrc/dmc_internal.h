@@ -271,16 +271,26 @@ struct CausalParams {
   float *stats;                  // workspace: [hq][stat_stride][2], per row log2-sum-exp, sum(dout * out)
   int64_t stat_stride;           // total + 32
   float *part_k, *part_v;        // workspace, with several parts: [parts][total][hkv][d] of dK and dV
+  float *part_q;                 // workspace, likewise: [query_parts][total][hq][d + 4] of outputs or dQ
   float scale_log2;              // log2(e) / sqrt(d)
-  int32_t seqs, total, hq, hkv, compute_units;
+  int32_t seqs, total, hq, hkv;
   int32_t parts;                 // parts that a key tile's rows are cut into
+  int32_t query_parts;           // most parts that a query tile's keys are cut into
   bool sorted;                   // tiles by descending length (set per launch)
 };
-// Parts of the key kernels' rows: where their tiles are too few for the chip, a
-// tile's (head, row block) list is shared out to several workgroups, eight blocks
-// or more each by the average sequence, whose sums meet in a last pass.
-constexpr int kMaxKeyParts = 16;
-int causal_key_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total, int compute_units);
+// Where tiles are too few for the chip, a tile's blocks are shared out to several
+// workgroups whose sums meet in a last pass: a key tile's (head, row block) list,
+// eight blocks or more each by the average sequence (fp32, whose waves share a list:
+// four), in up to four workgroups for a compute unit in all; a query tile's key
+// blocks likewise, in up to two, as its parts' records are larger (at four, 3000 +
+// 2000 + 100 tokens of 8 heads lost, 73 -> 83 us).  us before -> after: backward,
+// fp32, 2 x 300 tokens, 8/1 heads, 329 -> 111; forward, bf16, 1000 tokens, 4/1 heads,
+// 26.5 -> 20.2.
+constexpr int kMaxKeyParts = 16, kMaxQueryParts = 8, kPartPlaces = 1024, kQueryPartPlaces = 512;
+struct CausalParts {
+  int keys, queries;
+};
+CausalParts causal_parts(int elem_bytes, int hq, int hkv, int seqs, int64_t total);
 hipError_t launch_causal_forward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 hipError_t launch_causal_backward(int elem_bytes, int head_dim, const CausalParams &p, hipStream_t s);
 

@@ -26,7 +26,8 @@ def causal(q, k, v, lens, dout=None):
       out    rounding u |o|, and P rounded to the type: u P |v|
       lse    e_S and f
       scores chains of d products: e_S = d 2^-24 |q|.|k| / sqrt(d), relative in P (twice: with lse's)
-      D      = dO . o with the rounded o: e_D = sum |dO| bound(o)
+      D      = dO . o with the rounded o: e_D = sum |dO| bound(o); a sequence's first 128 rows
+             sum P dP instead: e_D = (2 e_S + f) sum P (|dP| + |D|)
       dS     = P (dP - D): u |dS| (rounded to the type) + P e_D + e_S |dS|
       dq     = sum dS k: sum e_dS |k| + u |dq|;  dk likewise;  dv = sum P dO: sum u P |dO| + u |dv|
     """
@@ -65,6 +66,9 @@ def causal(q, k, v, lens, dout=None):
             D = (do * o).sum(1, keepdim=True)
             dS = P * (dp - D)
             eD = (do.abs() * (bo + f * o.abs())).sum(1, keepdim=True)
+            # (the first 128 rows take D from sum P dP, with unrounded probabilities)
+            eD[:128] = ((2 * es + f) * P * (dp.abs() + D.abs())).sum(1, keepdim=True)[:128] + (
+                f * do.abs() @ vh.abs().T * P).sum(1, keepdim=True)[:128]
             edp = f * (do.abs() @ vh.abs().T)
             eS = (u + 2 * es + f) * dS.abs() + P * (eD + edp)
             sc = 1 / math.sqrt(d)

@@ -87,7 +87,7 @@ def _call(backward, cfg=None, ptr=4096, ws=1 << 14, ws_bytes=1 << 30, total=T, s
     head = [ctypes.byref(cfg), *(x for n in ("q", "k", "v") for x in (p[n], st[n])), cu, seqs, total,
             p["out"], st["out"], lse]
     if not backward:
-        return Bd.lib.dmc_causal_forward(*head, None)
+        return Bd.lib.dmc_causal_forward(*head, ws, ws_bytes, None)
     return Bd.lib.dmc_causal_backward(*head, *(x for n in ("dout", "dq", "dk", "dv") for x in (p[n], st[n])),
                                       ws, ws_bytes, None)
 
@@ -118,9 +118,10 @@ def test_output_rows_that_overlap(strides):
 def test_workspace_refusals():
     n = Bd.lib.dmc_causal_workspace_bytes(ctypes.byref(P.make_causal_config(HQ, HKV, D)), T)
     assert n >= HQ * T * 8
-    assert _call(True, ws=None) == 1 and "workspace" in Bd.last_error()
-    assert _call(True, ws=4096 + 16) == 1 and "256-byte" in Bd.last_error()
-    assert _call(True, ws_bytes=n - 1) == 1 and "workspace has" in Bd.last_error()
+    for backward in (False, True):
+        assert _call(backward, ws=None) == 1 and "workspace" in Bd.last_error()
+        assert _call(backward, ws=4096 + 16) == 1 and "256-byte" in Bd.last_error()
+        assert _call(backward, ws_bytes=n - 1) == 1 and "workspace has" in Bd.last_error()
     assert Bd.lib.dmc_causal_workspace_bytes(ctypes.byref(P.make_causal_config(3, 2, 64)), T) == 0
     assert Bd.lib.dmc_causal_workspace_bytes(ctypes.byref(P.make_causal_config(4, 2, 64)), -1) == 0
 

@@ -273,11 +273,12 @@ def test_boundaries_out_of_range(torch_cuda):
 @pytest.mark.parametrize("lens,hq,hkv,d", [
     # enough tiles to go out by length (more than two per compute unit), and key tiles cut into parts
     ([130, 257, 1, 0, 640, 128, 129, 300], 64, 32, 64), ([700], 8, 1, 128), ([300, 280], 6, 2, 64),
-    ([40] * 100 + [500] + [0] * 3 + [7] * 90, 16, 8, 64)])
-def test_orders_and_parts(torch_cuda, lens, hq, hkv, d):
+    ([40] * 100 + [500] + [0] * 3 + [7] * 90, 16, 8, 64), ([1300, 3, 900], 2, 1, 128), ([700, 1], 4, 4, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_orders_and_parts(torch_cuda, dtype, lens, hq, hkv, d):
     """Launch orders and partial sums of key tiles: against float64 on sampled heads, all rows."""
     import paper_2403_09636_amd as P
-    q, k, v, dout = make(lens, hq, hkv, d, "bf16")
+    q, k, v, dout = make(lens, hq, hkv, d, dtype)
     got = run(P, q, k, v, dout, lens)
     G = hq // hkv
     for g in sorted({0, hkv // 2, hkv - 1}):
