@@ -736,7 +736,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
     if (colv) {
       m = d * sl2;
       if (m == neg_inf()) m = lowest();   // (by itself it still has weight 1)
-      ls = hb == 0 ? 1.0f : 0.0f;         // counted once per column
+      // counted once per column; a score of +infinity or NaN makes the row NaN, whatever else it sees
+      ls = hb == 0 ? (m < -neg_inf() ? 1.0f : __builtin_nanf("")) : 0.0f;
 #pragma unroll
       for (int i = 0; i < NTL; ++i)
 #pragma unroll

@@ -209,6 +209,24 @@ def test_non_finite_tokens(torch_cuda, dtype, bad, at):
         assert (out[at:40, :, 5] == math.inf).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("slots", [0, 50])
+@pytest.mark.parametrize("lens,most", [([6], 6), ([6], 40), ([40], 40), ([1], 40)])
+def test_a_token_whose_own_score_is_not_finite(torch_cuda, dtype, bad, slots, lens, most):
+    """A score of NaN or +infinity on the token's own state makes its whole row NaN, as a softmax does, also
+    where nothing else is visible; k and v are finite, so no other row changes."""
+    c = Case(8, 2, 64, dtype, [[slots] * 2], max_chunk=most)
+    q, k, v = c.tokens(lens, 2.0)
+    k[0, :, 1] = 1.0
+    want, bound, _ = c.ref.chunk(f64(q), f64(k), f64(v), lens)
+    # an empty cache: the first token's state is its own k, so that the score has the infinity's sign
+    q[0, :, 1] = bad
+    out = f64(c.chunk.attend(0, q, k, v, cu_of(lens).cuda()))
+    assert np.isnan(out[0]).all()
+    assert (np.abs(out - want)[1:] <= bound[1:]).all()
+
+
 def test_no_room(torch_cuda):
     """A unit without slots or pages for its chunk keeps its cache; others take theirs."""
     P = torch_cuda and __import__("paper_2403_09636_amd")
