@@ -1325,10 +1325,12 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams 
 
 // The pieces of a tile put together: o = sum_i 2^(m_i - M) acc_i / sum_i
 // 2^(m_i - M) l_i.  One wave per column, lanes own D / 64 elements; bound by latency:
-// records are read sixteen at a time.  Tiles of one piece have been written already.
+// records are read sixteen at a time, or four where there are no more (256 wide tiles
+// of two pieces: 21 us, 40 with sixteen loads for the two; 24 rows of 32 heads and 6
+// tokens: 4.8).  Tiles of one piece have been written already.
 template <int ES, int D, int G, int COLS>
 __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) {
-  constexpr int E = D / 64, REC = D + 4, R = 16;
+  constexpr int E = D / 64, REC = D + 4;
   const int g = blockIdx.y, lane = threadIdx.x & 63;
   const int c = blockIdx.z * kWaves + (threadIdx.x >> 6);
   const PackedTile pt = packed_tile(p.cu, p.rows, p.total, blockIdx.x, p.tile_shift);
@@ -1357,7 +1359,8 @@ __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) 
   auto of_lane = [](float y, int j) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), j));
   };
-  for (int i0 = 0; i0 < parts; i0 += R) {
+  auto batch = [&](int i0, auto r_c) {
+    constexpr int R = decltype(r_c)::value;
     // lane i < R reads record i's maximum and sum; every load of a batch in one round trip
     const float *mine = rec + int64_t(min(i0 + (lane & (R - 1)), parts - 1)) * COLS * REC;
     float mi = mine[0], li = mine[1], a[R][E];
@@ -1388,7 +1391,10 @@ __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) 
         for (int e = 0; e < E; ++e) A[e] = fmaf(wj, a[j][e], A[e]);
       }
     }
-  }
+  };
+  if (parts <= 4) batch(0, std::integral_constant<int, 4>{});
+  else
+    for (int i0 = 0; i0 < parts; i0 += 16) batch(i0, std::integral_constant<int, 16>{});
   const float inv = 1.0f / L;
 #pragma unroll
   for (int e = 0; e < E; ++e) A[e] *= inv;
@@ -1466,6 +1472,12 @@ hipError_t chunk_append(const ChunkParams &p, hipStream_t s) {
 
 }  // namespace
 
+// More than two narrow tiles of columns: wide.  us of the attention and its combine
+// pass (d 128), narrow / wide, by max_chunk * G:
+//                                   40        64        96        128       256
+//   16 rows, 32/8 heads, 8192      69/72     77/77    104/72      -        197/143
+//   16 rows, 16/16 heads, 4096     72/63     71/72     97/79    122/97     227/121
+//   2 rows, 32/8 heads, 2048       18/20     19/21     19/23     20/26      29/28
 bool chunk_wide(int elem_bytes, int group, int max_chunk) { return elem_bytes == 2 && max_chunk * int64_t(group) > 64; }
 
 int chunk_tile_shift(int group, bool wide) {
