@@ -1234,7 +1234,8 @@ dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q
   }
   p.out = out;
   copy_strides(p.os, out_strides);
-  const bool wide = dmc::chunk_wide(elem_bytes(c), cache->lay.group, max_chunk);
+  const bool wide = dmc::chunk_wide(elem_bytes(c), cache->lay.group, max_chunk,
+                                    int64_t(cache->lay.units) * c.max_slots_per_seq);
   p.tile_shift = dmc::chunk_tile_shift(cache->lay.group, wide);
   // (units whose capacity makes less than two pieces are never cut)
   const int64_t most_blocks = (int64_t(c.max_slots_per_seq) + 31) / 32 + (int64_t(max_chunk) + 63) / 64;

@@ -1472,13 +1472,19 @@ hipError_t chunk_append(const ChunkParams &p, hipStream_t s) {
 
 }  // namespace
 
-// More than two narrow tiles of columns: wide.  us of the attention and its combine
-// pass (d 128), narrow / wide, by max_chunk * G:
-//                                   40        64        96        128       256
-//   16 rows, 32/8 heads, 8192      69/72     77/77    104/72      -        197/143
-//   16 rows, 16/16 heads, 4096     72/63     71/72     97/79    122/97     227/121
-//   2 rows, 32/8 heads, 2048       18/20     19/21     19/23     20/26      29/28
-bool chunk_wide(int elem_bytes, int group, int max_chunk) { return elem_bytes == 2 && max_chunk * int64_t(group) > 64; }
+// Wide tiles read a cache once for four times as many columns, narrow ones leave
+// more workgroups for a small one.  us of the attention and its combine pass (32/8
+// heads, d 128), narrow / wide, by the layer's cached slots and max_chunk * G:
+//              16K       32K       64K     8 x 8K     512K
+//    40       18/20       -         -         -       69/62
+//    64       18/21     20/22     27/24     28/24     77/65
+//   128       20/25     28/28     39/32     39/31    107/85
+//   256       29/28       -         -         -      197/143
+// (Lengths are on the device: by what the caches can hold.  A cache that is nearly
+// empty loses the few us of its own column.)
+bool chunk_wide(int elem_bytes, int group, int max_chunk, int64_t slots) {
+  return elem_bytes == 2 && max_chunk * int64_t(group) > (slots >= (1 << 16) ? 32 : 128);
+}
 
 int chunk_tile_shift(int group, bool wide) {
   int shift = wide ? 7 : 5;

@@ -333,7 +333,7 @@ struct ChunkParams {
   int32_t fixed_parts;           // > 0: places for pieces of every unit, which has one narrow tile; no plan (attend)
 };
 // Tokens of a column tile of the attention (log2), and whether its workgroups take 128 columns or 32.
-bool chunk_wide(int elem_bytes, int group, int max_chunk);
+bool chunk_wide(int elem_bytes, int group, int max_chunk, int64_t slots);
 int chunk_tile_shift(int group, bool wide);
 hipError_t launch_chunk_attend(int elem_bytes, int head_dim, int group, bool vt, bool wide, const ChunkParams &p,
                                hipStream_t s);

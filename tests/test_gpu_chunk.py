@@ -129,6 +129,19 @@ def test_long_caches_in_pieces(torch_cuda, dtype, hq, hkv, chunk):
     c.attend(*c.tokens([chunk], 2.0), [chunk])
 
 
+@pytest.mark.parametrize("hq,hkv,chunk", [(8, 2, 12), (8, 2, 9), (8, 1, 16), (2, 2, 33)])
+def test_few_columns_on_large_caches(torch_cuda, hq, hkv, chunk):
+    """Room for 64K slots or more in the layer: more than 32 columns are one wide tile."""
+    lens = [chunk, 0, chunk - 1]
+    c = Case(hq, hkv, 64, "bf16", [[700] * hkv, [0] * hkv, [31] * hkv], extra=24000, max_chunk=chunk)
+    x = c.tokens(lens, 2.0)
+    c.attend(*x, lens)
+    c.append(*x, lens)
+    c.ref.restart(c.cache, c.layer)
+    c.attend(*c.tokens(lens, 2.0), lens)
+    c.cache.check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_accepted_tokens(torch_cuda, dtype):
     """Drafts of which a part is accepted, then decode steps and further chunks: one conversation."""
