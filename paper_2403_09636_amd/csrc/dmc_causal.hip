@@ -142,7 +142,9 @@ __device__ __forceinline__ const char *row_at(const void *base, const int64_t (&
 //   S^T[key][col] = K . Q^T;   O^T[dim][col] += V^T P^T;   dQ^T[dim][col] += K^T dS^T
 // Score row m is key pi(m) (bits 2 and 3 of m swapped), which makes a lane's
 // score registers the operand of the second product.  Forward: block kb's
-// exponentials run between the score products of block kb + 1.
+// exponentials run between the score products of block kb + 1.  Bound by the matrix
+// cores and the softmax beside them: 5 sequences up to 8192, 32 heads, d 128, forward
+// 1080 us (920 TFLOP/s); 6 up to 4096, 32/8 heads, forward 500 us, dq 660 us.
 // ---------------------------------------------------------------------------
 template <int D, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams p, int ntiles) {
@@ -499,6 +501,7 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
 // each holds half the accumulators and runs two waves per SIMD.
 //   S[row][key] = Q . K^T,  dP[row][key] = dO . V^T   (rows pi-permuted)
 //   dV^T[dim][key] += dO^T P,  dK^T[dim][key] += Q^T dS
+// 6 sequences up to 4096, 32/8 heads, d 128: dV 556-586 us, dK 748-777 us.
 template <int D, int PART>
 __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p) {
   static_assert(PART == 1 || PART == 2, "dV part or dK part");
@@ -825,7 +828,8 @@ __global__ __launch_bounds__(kThreads) void causal_parts_kernel(CausalParams p) 
 // columns of one head -- queries in the forward and dq, keys in the key kernel
 // -- whose four waves share the column operands and take every fourth 32-row
 // block of the other side straight from global memory; their results meet in
-// LDS.  Bound by the fp32 matrix rate and by the longest tile's chain of blocks.
+// LDS.  Bound by the fp32 matrix rate and by the longest tile's chain of blocks (4
+// sequences up to 640, 8/4 heads, d 64: forward 30 us, dq 51, dK and dV 74).
 // ---------------------------------------------------------------------------
 template <int D, int MODE>
 __global__ __launch_bounds__(kThreads) void causal_query_f32_kernel(CausalParams p, int ntiles) {

@@ -105,7 +105,9 @@ __device__ __forceinline__ char *page_of(const ChunkParams &p, int u, int s) {
 //   ATTEND  every state, closed states, counts; and the plan of the attention (one more workgroup)
 //   APPEND  closed states and the last one into the pages (pages allocated before)
 //   ONE     the same for rows of one block: allocates the pages itself
-// Bound by reading k, v and writing the states.
+// Bound by reading k, v and writing the states: 6 prompts up to 4096 tokens, 32
+// heads, d 128:, SUMS 70-100 us, ATTEND 138, APPEND 122; by the
+// round trips of one workgroup on a few tokens (24 rows of 6: 10 us, 1 row of 4: 6).
 enum { SUMS, ATTEND, APPEND, ONE };
 
 __device__ void plan_pieces(const ChunkParams &p);
@@ -651,10 +653,12 @@ __device__ __forceinline__ int page_entry(const int32_t *ptab, int64_t i) {
 //
 // WIDE (many query rows): four waves of 32 columns share the blocks, which come
 // into LDS by direct transfers (a ring of four, three ahead); bound by the
-// matrix cores and the softmax.  Narrow (few rows): one tile of 32 columns whose
+// matrix cores and the softmax (512 tokens of 4 rows, 64/8 heads, on 6000 slots: 481-507
+// us).  Narrow (few rows): one tile of 32 columns whose
 // waves take every fourth block, the keys straight into registers and the values
 // into a ring of two blocks of the wave's own, one block ahead; bound by memory
-// (two workgroups and 128 KB of requests per compute unit).
+// (two workgroups and 128 KB of requests per compute unit; 24 rows of 6 tokens, 32 heads,
+// up to 4096 slots: 87-89 us, 5.2 TB/s).
 //
 // BIG: pages of >= 32 slots (a block lies in one page); VT: value pages, and
 // the blocks of closed values, stored transposed.
@@ -1157,7 +1161,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
 // fp32, on v_mfma_f32_32x32x2_f32 (operand forms: F32): one tile of 32 columns,
 // whose four waves take every fourth block of its piece straight from the pages
 // and the closed states; their online-softmax states meet in LDS.  Bound by the
-// fp32 matrix rate, and by the chain of blocks of a wave.
+// fp32 matrix rate, and by the chain of blocks of a wave (5 rows of 77 tokens, 12/6
+// heads, d 64, on up to 1500 tokens' slots: 21 us).
 // ---------------------------------------------------------------------------
 template <int D, int G>
 __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams p) {
