@@ -437,3 +437,56 @@ def test_many_units_are_planned(torch_cuda, dtype, chunk):
     want, bound, _ = c.ref.chunk(*(f64(t)[rows] for t in (q, k, v)), [lens[b] for b in (3, 17, 30)])
     assert (np.abs(out[rows] - want) <= bound).all()
     c.cache.check()
+
+
+@pytest.mark.parametrize("dtype,hq,page", [("bf16", 4, 32), ("bf16", 16, 32), ("bf16", 8, 16), ("fp32", 8, 32)])
+def test_pages_beyond_4_gb(torch_cuda, dtype, hq, page):
+    """Another layer holds the pool's first 4 GB, so that this layer's pages lie past 32-bit offsets."""
+    d, units = 128, 8
+    slots = -(-2 ** 32 // (2 * d * (4 if dtype == "fp32" else 2)) // units) + page
+    pages = units * -(-slots // page) + 64
+    c = Case(hq, 4, d, dtype, [[0] * 4] * 2, page=page, extra=slots, num_pages=pages, layers=2, layer=1, max_tokens=64,
+             max_chunk=4)
+    full = torch.zeros((2, 4, slots, d), dtype=dtype_of(dtype), device="cuda")
+    c.cache.import_(0, full, full, torch.full((2, 4), slots, dtype=torch.int32, device="cuda"),
+                    torch.ones((2, 4), device="cuda"))
+    del full
+    assert c.cache.pages_used() * page * 2 * d * (4 if dtype == "fp32" else 2) > 2 ** 32
+    narrow, wide = c.chunk, c.P.DMCChunk(c.cache, 64, 40)
+    for chunk, lens in ((narrow, [4, 3]), (wide, [40, 17]), (wide, [1, 33]), (narrow, [2, 4])):
+        c.chunk = chunk
+        x = c.tokens(lens, 1.5)
+        c.attend(*x, lens)
+        c.append(*x, lens)
+        c.ref.restart(c.cache, c.layer)
+    c.cache.check()
+
+
+def test_two_handles_at_once(torch_cuda):
+    """Attention from two handles on two streams over one cache, and a handle whose bound on a row's
+    tokens is far above the call's."""
+    c = Case(8, 2, 64, "bf16", [[2000, 40], [300, 3], [0, 7]], max_tokens=64, max_chunk=8)
+    other = c.P.DMCChunk(c.cache, 64, 2 ** 31 - 1)
+    lens = [5, 8, 2]
+    x, cu = c.tokens(lens, 2.0), cu_of(lens).cuda()
+    want, bound, _ = c.ref.chunk(*(f64(t) for t in x), lens)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.zeros_like(x[0]) for _ in range(4)] for _ in sides]
+    torch.cuda.synchronize()
+    for i in range(4):
+        for side, chunk, out in zip(sides, (c.chunk, other), outs):
+            chunk.attend(0, *x, cu, out=out[i], stream=side)
+    torch.cuda.synchronize()
+    for out in outs:
+        assert (np.abs(f64(out[0]) - want) <= bound).all()
+        assert all(torch.equal(o, out[0]) for o in out)
+
+
+def test_closed_cache(torch_cuda):
+    c = Case(4, 2, 64, "bf16", [[5, 6]], max_tokens=16)
+    x = c.tokens([4])
+    c.cache.close()
+    for call in (lambda: c.chunk.attend(0, *x, cu_of([4]).cuda()), lambda: c.P.DMCChunk(c.cache, 16),
+                 lambda: c.chunk.append(0, x[1], x[2], x[0], cu_of([4]).cuda())):
+        with pytest.raises(c.P.DMCError, match="NULL"):
+            call()
