@@ -286,3 +286,31 @@ def test_orders_and_parts(torch_cuda, dtype, lens, hq, hkv, d):
         want = causal(q[:, heads], k[:, g:g + 1], v[:, g:g + 1], lens, dout[:, heads])
         for name, x in got.items():
             check(x[:, g:g + 1] if name in ("dk", "dv") else x[:, heads], want[name], f"{name} of kv head {g}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides_beyond_4_gb(torch_cuda, dtype):
+    """Tokens spread over more than 4 GB, inputs and outputs, give the bits of contiguous ones."""
+    import paper_2403_09636_amd as P
+    hq, hkv, d, T = 2, 1, 64, 40000
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    width = 120000 // dt.itemsize
+    buf = torch.empty((T, width), dtype=dt, device="cuda")
+    assert buf.numel() * dt.itemsize > 2 ** 32
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def place(at, heads):
+        return buf[:, at:at + heads * d].view(T, heads, d)
+    q, k, v, dout = (place(at, h) for at, h in ((0, hq), (1024, hkv), (2048, hkv), (4096, hq)))
+    for t in (q, k, v, dout):
+        t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+    cu = cu_of([700, 1, 499] + [400] * 97).cuda()
+    att = P.DMCCausal(P.make_causal_config(hq, hkv, d, dtype), T)
+    out, lse = att.forward(q, k, v, cu, out=place(8192, hq))
+    grads = att.backward(q, k, v, cu, out, lse, dout, dq=place(9216, hq), dk=place(10240, hkv), dv=place(11264, hkv))
+    qc, kc, vc, dc = (t.contiguous() for t in (q, k, v, dout))
+    want, wlse = att.forward(qc, kc, vc, cu)
+    assert torch.equal(out, want) and torch.equal(lse, wlse)
+    assert want.isfinite().all()
+    for a, b in zip(grads, att.backward(qc, kc, vc, cu, want, wlse, dc)):
+        assert torch.equal(a, b)
