@@ -1058,36 +1058,6 @@ struct ChunkLayout {
       old_len, old_z, partials, total;
 };
 
-// Attention pieces beyond one per column tile; none once the tiles themselves are
-// eight per compute unit.  us of the attention and its combine pass (bf16, d 128):
-//   narrow, per compute unit        2       3       4
-//     24 rows, 32 heads, <= 4096   99.4    93.9    95.5
-//     16 rows, 64/8 heads, 16384  116     112     120
-//   wide (a record is four times as large)   1       2       3
-//     16 rows, 32/8 heads, 8192, 24 tokens  122.0    72.2    85.2
-//     1 row, 32/8 heads, 16384, 512 tokens  137.2   108.4   126.7
-//     16 rows, 16/16 heads, 4096, 128        85.5    96.7   125.1
-static int32_t chunk_piece_budget(const dmc_cache *c, int32_t total, int shift, bool wide) {
-  const int64_t tiles = int64_t(total >> shift) * c->cfg.num_kv_heads;
-  return tiles >= int64_t(8) * c->cu_count ? 0 : (wide ? 2 : 3) * c->cu_count;
-}
-// The fewest 32-row blocks of a piece.  us of the attention and its combine pass:
-//                                              4      8      16
-//   1 row, 16/4 heads, 900 slots at CR mix    15.5   15.8   17.0
-//   fp32, 5 rows, 12/6 heads, 77 tokens       21.8   21.0   35.4 (attention alone)
-//   4 rows, 8 heads, one row of 9000 slots    41.6   28.8   21.2
-constexpr int32_t kChunkPieceMin = 8;
-// Few units of one 32-column tile each: a fixed number of places per unit, as many
-// as are all resident (two per compute unit) and its capacity can use; 0 for
-// others, whose pieces are planned by their lengths: with 64 units each gets 8 places
-// and more would leave them too few.  A call for 4 rows of 8 heads, one of 9000 slots:
-// 28 us, planned 37.
-static int32_t chunk_fixed_parts(const dmc_cache *c, int32_t max_chunk, int64_t most_blocks) {
-  if (int64_t(max_chunk) * c->lay.group > 32 || c->lay.units > 64) return 0;
-  const int64_t parts = std::min<int64_t>(2 * c->cu_count / c->lay.units, most_blocks / kChunkPieceMin);
-  return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(parts, 64)));
-}
-
 static ChunkLayout chunk_layout(const dmc_cache *c, int32_t total) {
   const dmc_cache_config &cfg = c->cfg;
   const size_t es = elem_bytes(cfg), d = cfg.head_dim, H = cfg.num_kv_heads, U = c->lay.units, B = cfg.batch;
@@ -1209,7 +1179,7 @@ static dmc_status chunk_params(const dmc_cache *c, int32_t layer, const void *k,
   p.decision_src = cfg.decision_src;
   p.blocks64 = total / 64 + cfg.batch;
   p.blocks32 = total / 32 + cfg.batch;
-  p.piece_min = kChunkPieceMin;
+  p.piece_min = dmc::kChunkPieceMin;
   return DMC_OK;
 }
 
@@ -1237,10 +1207,10 @@ dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q
   const bool wide = dmc::chunk_wide(elem_bytes(c), cache->lay.group, max_chunk,
                                     int64_t(cache->lay.units) * c.max_slots_per_seq);
   p.tile_shift = dmc::chunk_tile_shift(cache->lay.group, wide);
-  // (units whose capacity makes less than two pieces are never cut)
-  const int64_t most_blocks = (int64_t(c.max_slots_per_seq) + 31) / 32 + (int64_t(max_chunk) + 63) / 64;
-  p.piece_budget = most_blocks < 2 * kChunkPieceMin ? 0 : chunk_piece_budget(cache, total, p.tile_shift, wide);
-  p.fixed_parts = chunk_fixed_parts(cache, max_chunk, most_blocks);
+  const dmc::ChunkSplit split = dmc::chunk_split(cache->cu_count, c.batch, c.num_kv_heads, cache->lay.group, c.max_slots_per_seq,
+                                                 total, max_chunk, p.tile_shift, wide);
+  p.fixed_parts = split.fixed_parts;
+  p.piece_budget = split.piece_budget;
   DeviceGuard g(cache->device);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");
   hipError_t e = dmc::launch_chunk_attend(elem_bytes(c), c.head_dim, cache->lay.group, cache->lay.v_trans, wide, p,

@@ -1443,7 +1443,7 @@ hipError_t chunk_attend(const ChunkParams &p, bool vt, bool wide, hipStream_t s)
     hipLaunchKernelGGL((chunk_attend_f32_kernel<D, G>), dim3(pieces), dim3(kThreads), 0, s, p);
   }
   e = hipGetLastError();
-  if (e != hipSuccess || p.piece_budget == 0 || p.fixed_parts == 1) return e;
+  if (e != hipSuccess || (p.fixed_parts <= 1 && p.piece_budget == 0)) return e;   // every tile is whole
   if (wide)
     hipLaunchKernelGGL((chunk_combine_kernel<ES, D, G, 128>), dim3(tiles, p.hkv, 128 / kWaves), dim3(kThreads), 0, s, p);
   else

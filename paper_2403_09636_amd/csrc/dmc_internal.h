@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace dmc {
 
 __host__ __device__ constexpr inline size_t align_up(size_t x, size_t a) {
@@ -335,6 +337,45 @@ struct ChunkParams {
 // Tokens of a column tile of the attention (log2), and whether its workgroups take 128 columns or 32.
 bool chunk_wide(int elem_bytes, int group, int max_chunk, int64_t slots);
 int chunk_tile_shift(int group, bool wide);
+// How the attention's column tiles are cut into pieces, which leave records for the
+// combine pass: by a fixed number of places per unit, or by a plan with a budget of
+// pieces beyond one per tile (the other is 0 then).  Tiles are whole if neither is
+// more than one.
+struct ChunkSplit {
+  int32_t fixed_parts, piece_budget;
+};
+// The fewest 32-row blocks of a piece.  us of the attention and its combine pass:
+//                                              4      8      16
+//   1 row, 16/4 heads, 900 slots at CR mix    15.5   15.8   17.0
+//   fp32, 5 rows, 12/6 heads, 77 tokens       21.8   21.0   35.4 (attention alone)
+//   4 rows, 8 heads, one row of 9000 slots    41.6   28.8   21.2
+constexpr int32_t kChunkPieceMin = 8;
+// Few units of one 32-column tile each get as many places as are all resident (two
+// per compute unit) and their capacity can use: a call for 4 rows of 8 heads, one of
+// 9000 slots, takes 28 us, planned 37; with 64 units each gets 8 places and more would
+// leave them too few.  Others are planned, with no budget where units of this
+// capacity make less than two pieces, or once the tiles themselves are eight per
+// compute unit.  Tiles are those that the rows can fill: the tensors may be longer.
+// us of the attention and its combine pass by the budget (bf16, d 128):
+//   narrow, per compute unit        2       3       4
+//     24 rows, 32 heads, <= 4096   99.4    93.9    95.5
+//     16 rows, 64/8 heads, 16384  116     112     120
+//   wide (a record is four times as large)   1       2       3
+//     16 rows, 32/8 heads, 8192, 24 tokens  122.0    72.2    85.2
+//     1 row, 32/8 heads, 16384, 512 tokens  137.2   108.4   126.7
+//     16 rows, 16/16 heads, 4096, 128        85.5    96.7   125.1
+inline ChunkSplit chunk_split(int cu_count, int rows, int hkv, int group, int max_slots, int total, int max_chunk,
+                              int tile_shift, bool wide) {
+  const int64_t units = int64_t(rows) * hkv;
+  const int64_t blocks = (int64_t(max_slots) + 31) / 32 + (int64_t(max_chunk) + 63) / 64;   // of a unit, at most
+  if (int64_t(max_chunk) * group <= 32 && units <= 64) {
+    const int64_t parts = std::min<int64_t>(2 * cu_count / units, blocks / kChunkPieceMin);
+    return {static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(parts, 64))), 0};
+  }
+  const int64_t tiles = (std::min<int64_t>(total, int64_t(rows) * max_chunk) >> tile_shift) * hkv;
+  if (blocks < 2 * kChunkPieceMin || tiles >= int64_t(8) * cu_count) return {0, 0};
+  return {0, (wide ? 2 : 3) * cu_count};
+}
 hipError_t launch_chunk_attend(int elem_bytes, int head_dim, int group, bool vt, bool wide, const ChunkParams &p,
                                hipStream_t s);
 hipError_t launch_chunk_append(int elem_bytes, int head_dim, bool vt, const ChunkParams &p, hipStream_t s);
