@@ -224,7 +224,6 @@ __global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams
       const int grow = __popcll(mask);
       end = l + grow;
       if (!grow_unit(p, c.u, l, grow)) base = -1;
-      else if (lane == 0) p.len[c.u] = end;
     }
     if (lane == 0) {
       s_mask = mask;
@@ -249,6 +248,8 @@ __global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams
     if (p.slot_index && tid < cnt) p.slot_index[int64_t(c.start + c.first + tid) * p.hkv + g] = -1;
     return;
   }
+  // (every wave has read the old length before the barrier)
+  if (MODE == ONE && tid == 0) p.len[c.u] = s_end;
   // Sums of the wave's tokens since its last segment start.
   // (past the row's end: its last token again, used by nobody)
   const uint32_t wmask = static_cast<uint32_t>(mask >> w0) & ((1u << kWaveTokens) - 1);
