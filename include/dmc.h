@@ -391,7 +391,7 @@ dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q
  *     chunk went to, -1 for tokens that were not appended; other rows stay as
  *     they were.
  * A unit without room for its whole chunk (slots, pages) keeps its cache as it
- * was and raises the capacity flag. */
+ * was, takes no pages and raises the capacity flag. */
 dmc_status dmc_chunk_append(dmc_cache *cache, int32_t layer, const void *k_dev,
                             const int64_t k_strides[2], const void *v_dev,
                             const int64_t v_strides[2], const void *q_dev,

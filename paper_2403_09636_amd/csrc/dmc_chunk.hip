@@ -112,8 +112,36 @@ enum { SUMS, ATTEND, APPEND, ONE };
 
 __device__ void plan_pieces(const ChunkParams &p);
 
-// Pages for a unit that grows from l to l + grow slots: new pages from the bump
-// pointer into the page table (by one wave).  False when they do not exist.
+// n pages from the pool's bump pointer, all or none (by one lane): the first one, or -1.
+// At rest the pointer is at most the pool's end.  The unit whose addition takes it past
+// the end puts it back; until then nobody else can get pages, as every addition starts
+// past the end, so that what it puts back is still what has been handed out.  Units that
+// add meanwhile wait for that (their additions are undone with it) and look again, so
+// that a refused request never costs another unit its pages.
+// (Compare and swap serves one unit a round trip: of 24 rows of 32 heads, half or all of
+// which need a page, 0.8 and 1.8 ms for the launch of 6 tokens a row; this way 18 us.)
+__device__ __forceinline__ long long take_pages(const ChunkParams &p, int n) {
+  unsigned long long *used = &p.ctrl->pages_used;
+  const unsigned long long end = static_cast<unsigned long long>(p.num_pages), more = static_cast<unsigned long long>(n);
+  for (int polls = 0; polls < (1 << 16);) {   // (a bound; the wait is for the few instructions of a running wave)
+    const unsigned long long at = atomicAdd(used, more);
+    if (at + more <= end) return static_cast<long long>(at);
+    if (at <= end) {
+      atomicExch(used, at);
+      return -1;
+    }
+    unsigned long long now = at;
+    for (; now > end && polls < (1 << 16); ++polls) {
+      __builtin_amdgcn_s_sleep(1);
+      now = __hip_atomic_load(used, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (now + more > end) return -1;
+  }
+  return -1;
+}
+
+// Pages for a unit that grows from l to l + grow slots, into the page table (by one
+// wave).  False when they do not exist.
 __device__ __forceinline__ bool grow_unit(const ChunkParams &p, int u, int l, int grow) {
   const int lane = threadIdx.x & 63;
   if (grow > p.max_slots - l) {
@@ -123,10 +151,9 @@ __device__ __forceinline__ bool grow_unit(const ChunkParams &p, int u, int l, in
   const int P = 1 << p.log2p;
   const int have = (l + P - 1) >> p.log2p, need = (l + grow + P - 1) >> p.log2p;
   if (need == have) return true;
-  unsigned long long at = 0;
-  if (lane == 0) at = atomicAdd(&p.ctrl->pages_used, static_cast<unsigned long long>(need - have));
+  long long at = lane == 0 ? take_pages(p, need - have) : 0;
   at = __shfl(at, 0, 64);
-  if (at + (need - have) > static_cast<unsigned long long>(p.num_pages)) {
+  if (at < 0) {
     if (lane == 0) atomicOr(&p.ctrl->flags, FLAG_POOL_EXHAUSTED);
     return false;
   }

@@ -22,7 +22,7 @@ enum : int32_t {
 
 // Control block at the start of the control section.
 struct Control {
-  unsigned long long pages_used;  // bump allocator of the page pool
+  unsigned long long pages_used;  // bump allocator of the page pool: between launches at most its end
   long long alloc_base;           // first page of the last prefill / import allocation
   long long alloc_count;          // pages in it (0 after a failed allocation)
   int32_t flags;

@@ -669,7 +669,10 @@ __global__ __launch_bounds__((valu_decode_threads<ES, G>())) void decode_kernel(
           if (has_cur) p.z[u] = znew;
           (UNIT ? p.len_in : p.len_out)[u] = (has_cur && !alpha) ? l + 1 : l;
           if (p.slot_index) p.slot_index[u] = has_cur ? slot : -1;
-          if (flag) atomicOr(&p.ctrl->flags, flag);
+          if (flag) {
+            atomicOr(&p.ctrl->flags, flag);
+            if (flag == FLAG_POOL_EXHAUSTED) atomicAdd(&p.ctrl->pages_used, ~0ull);   // (-1: it rests at the pool's end)
+          }
           if constexpr (!UNIT) {
             const int r0 = off / span;                  // range holding the unit's first slot
             p.meta[2 * u] = r0 + u;                     // its first partial record
@@ -1373,7 +1376,10 @@ __global__ __launch_bounds__(kThreads, mfma_decode_wg_per_cu<D>()) void decode_m
           if (has_cur) p.z[u] = znew;
           (UNIT ? p.len_in : p.len_out)[u] = (has_cur && !alpha) ? l + 1 : l;
           if (p.slot_index) p.slot_index[u] = has_cur ? slot : -1;
-          if (flag) atomicOr(&p.ctrl->flags, flag);
+          if (flag) {
+            atomicOr(&p.ctrl->flags, flag);
+            if (flag == FLAG_POOL_EXHAUSTED) atomicAdd(&p.ctrl->pages_used, ~0ull);   // (-1: it rests at the pool's end)
+          }
           if constexpr (!UNIT) {
             const int r0 = whole ? r : pieces ? off : off / span;   // the unit's first range
             p.meta[2 * u] = r0 + u;
