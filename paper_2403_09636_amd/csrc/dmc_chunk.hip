@@ -52,17 +52,21 @@ struct Elems {
 };
 
 // Tokens of a row that count: at most max_chunk, and for an append the accepted
-// ones (out-of-range values raise the flag and are clamped).
-__device__ __forceinline__ int row_tokens(const ChunkParams &p, int b, int n, bool raise) {
-  bool bad = n > p.max_chunk;
+// ones (out-of-range values are clamped).
+__device__ __forceinline__ int row_tokens(const ChunkParams &p, int b, int n) {
   n = min(n, p.max_chunk);
-  if (p.accepted) {
-    const int x = p.accepted[b];
-    bad |= x < 0 || x > n;
-    n = min(max(x, 0), n);
-  }
-  if (bad && raise) atomicOr(&p.ctrl->flags, FLAG_BAD_LENGTH);
+  if (p.accepted) n = min(max(p.accepted[b], 0), n);
   return n;
+}
+// Whether a row's lengths are out of range: its boundaries (which may not decrease
+// either), its tokens, or how many of them are accepted.
+__device__ __forceinline__ bool bad_row(const ChunkParams &p, int b) {
+  const int s0 = p.cu[b], s1 = p.cu[b + 1];
+  bool bad = s0 < 0 || s1 > p.total || s1 < s0;
+  const int n = max(clamp_token(s1, p.total) - clamp_token(s0, p.total), 0);
+  bad |= n > p.max_chunk;
+  if (p.accepted) bad |= p.accepted[b] < 0 || p.accepted[b] > min(n, p.max_chunk);
+  return bad;
 }
 
 // One workgroup's 64-token block of one unit.
@@ -177,10 +181,9 @@ __global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams
       return;
     }
   }
-  if (MODE != SUMS && blockIdx.x == 0 && blockIdx.y == 0) {   // boundaries out of range or decreasing
+  if (MODE != SUMS && blockIdx.x == 0 && blockIdx.y == 0) {   // (every row, also those without tokens)
     bool bad = false;
-    for (int b = threadIdx.x; b < p.rows; b += kStateThreads)
-      bad |= p.cu[b] < 0 || p.cu[b + 1] > p.total || p.cu[b + 1] < p.cu[b];
+    for (int b = threadIdx.x; b < p.rows; b += kStateThreads) bad |= bad_row(p, b);
     if (bad) atomicOr(&p.ctrl->flags, FLAG_BAD_LENGTH);
   }
   const int g = blockIdx.y;
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams
   c.b = pt.seq;
   c.u = c.b * p.hkv + g;
   c.start = pt.start;
-  c.n = row_tokens(p, c.b, pt.n, pt.tile == 0 && g == 0 && tid == 0);
+  c.n = row_tokens(p, c.b, pt.n);
   c.first = pt.tile * kBlock;
   c.index = blockIdx.x;
   if (kAppend && p.slot_index) {   // tokens that are not appended
@@ -420,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void chunk_grow_kernel(ChunkParams p) {
   if (u >= p.units) return;
   const int b = u / p.hkv, g = u - b * p.hkv;
   const int s0 = clamp_token(p.cu[b], p.total), s1 = clamp_token(p.cu[b + 1], p.total);
-  const int n = row_tokens(p, b, max(s1 - s0, 0), false);
+  const int n = row_tokens(p, b, max(s1 - s0, 0));
   if (n == 0) return;
   const int blocks = (n + kBlock - 1) >> kBlockShift;
   const int64_t at = int64_t(g) * p.blocks64 + (s0 >> kBlockShift) + b;
