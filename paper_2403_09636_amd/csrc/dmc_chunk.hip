@@ -770,18 +770,20 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
     d += __shfl_xor(d, 32, 64);
     if (colv) {
       m = d * sl2;
-      if (m == neg_inf()) m = lowest();   // (by itself it still has weight 1)
-      // counted once per column; a score of +infinity or NaN makes the row NaN, whatever else it sees
-      ls = hb == 0 ? (m < -neg_inf() ? 1.0f : __builtin_nanf("")) : 0.0f;
+      // weight 1, relative to itself; 0 for a score of -infinity (NaN for the row if it sees nothing else), and
+      // a score of +infinity or NaN makes the row NaN, whatever else it sees
+      const float w = m == neg_inf() ? 0.0f : m < -neg_inf() ? 1.0f : __builtin_nanf("");
+      if (m == neg_inf()) m = lowest();
+      ls = hb == 0 ? w : 0.0f;   // (counted once per column)
 #pragma unroll
       for (int i = 0; i < NTL; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint2 w = *reinterpret_cast<const uint2 *>(p.state_v + row + (32 * i + 8 * j + 4 * hb) * 2);
-          acc[i][4 * j + 0] = bf16_lo(w.x);
-          acc[i][4 * j + 1] = bf16_hi(w.x);
-          acc[i][4 * j + 2] = bf16_lo(w.y);
-          acc[i][4 * j + 3] = bf16_hi(w.y);
+          const uint2 v = *reinterpret_cast<const uint2 *>(p.state_v + row + (32 * i + 8 * j + 4 * hb) * 2);
+          acc[i][4 * j + 0] = w * bf16_lo(v.x);
+          acc[i][4 * j + 1] = w * bf16_hi(v.x);
+          acc[i][4 * j + 2] = w * bf16_lo(v.y);
+          acc[i][4 * j + 3] = w * bf16_hi(v.y);
         }
     }
   };
@@ -1246,13 +1248,14 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams 
     d += __shfl_xor(d, 32, 64);
     if (colv) {
       m = d * p.scale_log2;
+      const float w = m == neg_inf() ? 0.0f : 1.0f;   // (-infinity: as in the bf16 kernel)
       if (m == neg_inf()) m = lowest();
-      ls = hb == 0 ? 1.0f : 0.0f;
+      ls = hb == 0 ? w : 0.0f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const typename F::col_t e = *reinterpret_cast<const typename F::col_t *>(vs + NT * F::row(r, hb));
 #pragma unroll
-        for (int i = 0; i < NT; ++i) acc[i][r] = e[i];
+        for (int i = 0; i < NT; ++i) acc[i][r] = w * e[i];
       }
     }
   }
