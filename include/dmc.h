@@ -389,7 +389,7 @@ dmc_status dmc_chunk_attend(const dmc_cache *cache, int32_t layer, const void *q
  *     invalid-argument flag and are clamped).  NULL = all of them.
  *   slot_index_dev: optional int32 [total_tokens, Hkv]: slot each token of a
  *     chunk went to, -1 for tokens that were not appended; other rows stay as
- *     they were.
+ *     they were.  It must not overlap an input.
  * A unit without room for its whole chunk (slots, pages) keeps its cache as it
  * was, takes no pages and raises the capacity flag. */
 dmc_status dmc_chunk_append(dmc_cache *cache, int32_t layer, const void *k_dev,

@@ -374,6 +374,43 @@ def _packed_overlap(x, y):
     return shift < xr or shift + yr > step
 
 
+def _touches(x, lo, hi):
+    """Whether a tensor [tokens, heads, d] has an element in the bytes lo .. hi - 1."""
+    x0, x1, _ = _spans(x)
+    if x.numel() == 0 or x0 >= hi or lo >= x1:
+        return False
+    es, row, step = x.element_size(), x.shape[2] * x.element_size(), x.stride(0) * x.element_size()
+    for h in range(x.shape[1]):
+        at = x0 + h * x.stride(1) * es   # rows at + t * step
+        if step == 0:
+            if at < hi and at + row > lo:
+                return True
+        else:
+            first = max(0, -(-(lo - row + 1 - at) // step))   # the first row that ends behind lo
+            if first < x.shape[0] and at + first * step < hi:
+                return True
+    return False
+
+
+def _shared(x, y):
+    """Whether two tensors share memory: packed ones (three dimensions) or contiguous arrays."""
+    if x.dim() != 3:
+        x, y = y, x
+    if x.dim() != 3:
+        return _overlap(x, y)
+    if y.dim() == 3:
+        return _packed_overlap(x, y)
+    return y.numel() > 0 and _touches(x, y.data_ptr(), y.data_ptr() + y.numel() * y.element_size())
+
+
+def _check_apart(written, read):
+    """No tensor that a call writes (name, tensor or None) shares memory with another one of it."""
+    for i, (name, x) in enumerate(written):
+        for other, y in (*read, *written[:i]):
+            if x is not None and y is not None and _shared(x, y):
+                _fail(f"{name} overlaps {other}")
+
+
 def _check_rows(name, t, dtype, tokens, heads, d):
     some = getattr(t, "shape", (1,))[:1] != (0,)   # (an empty tensor's strides mean nothing)
     _check(name, t, dtype, (tokens, heads, d), contiguous=False, last_dim_contiguous=some,
@@ -385,10 +422,7 @@ def _check_packed(inputs, outputs, dtype, d):
     strides multiples of 8 elements, 16-byte aligned; an output shares memory with no other one."""
     for name, t, tokens, heads in (*inputs, *outputs):
         _check_rows(name, t, dtype, tokens, heads, d)
-    for i, (name, t, _, _) in enumerate(outputs):
-        for other, x, _, _ in (*inputs, *outputs[:i]):
-            if _packed_overlap(t, x):
-                _fail(f"{name} overlaps {other}")
+    _check_apart([x[:2] for x in outputs], [x[:2] for x in inputs])
 
 
 def _check_cu(cu_seqlens, rows=None):
@@ -400,9 +434,9 @@ def _check_cu(cu_seqlens, rows=None):
 
 class _PackedCall:
     """The checks of a packed call's tensors in one pass, for calls whose GPU time is a few
-    microseconds: the conditions of _check_packed, tested without a message.  tensors() returns the
-    addresses of the tensors and their strides as one int64 array, or None if any condition fails (the
-    caller's full check then names it, or finds that nothing is wrong)."""
+    microseconds: the conditions of _check_packed and _check_apart, tested without a message.  tensors()
+    returns the addresses of the tensors and their strides as one int64 array, or None if any condition
+    fails (the caller's full check then names it, or finds that nothing is wrong)."""
 
     def __init__(self, dtype, device, d, es):
         import torch
@@ -410,10 +444,11 @@ class _PackedCall:
         self.dtype, self.device, self.d, self.es = dtype, device, d, es
         self.strides = {n: c_int64 * (2 * n) for n in range(1, 9)}
 
-    def tensors(self, T, inputs, outputs):
-        """inputs, outputs: (tensor, heads) each; outputs must lie apart from everything."""
+    def tensors(self, T, inputs, outputs, read=(), written=()):
+        """inputs, outputs: (tensor, heads) each; read, written: the byte ranges of the
+        call's arrays, as addresses.  What is written must lie apart from everything."""
         dtype, device, d, es, tensor = self.dtype, self.device, self.d, self.es, self.Tensor
-        ptrs, strides, spans = [], [], []
+        ptrs, strides, spans = [], [], [*read]
         for t, heads in (*inputs, *outputs):
             if not (isinstance(t, tensor) and t.dtype is dtype and t.shape == (T, heads, d) and t.device == device):
                 return None
@@ -424,8 +459,8 @@ class _PackedCall:
             ptrs.append(p)
             strides += (s0, s1)
             spans.append((p, p + ((T - 1) * s0 + (heads - 1) * s1 + d) * es))
-        n = len(inputs)
-        for i in range(n, len(spans)):
+        spans += written
+        for i in range(len(read) + len(inputs), len(spans)):
             lo, hi = spans[i]
             for a, b in spans[:i]:
                 if lo < b and a < hi:
@@ -466,6 +501,9 @@ def check_chunk_args(cfg, device, q, k, v, cu_seqlens, out=None, accepted=None, 
         _check("accepted", accepted, torch.int32, (cfg.batch,), align16=False)
     if slot_index is not None:
         _check("slot_index", slot_index, torch.int32, (T, Hkv), align16=False)
+        q0 = q.unsqueeze(-1) if q.dim() == 2 else q[..., :1]   # what is read of it
+        _check_apart([("slot_index", slot_index)], [("k", k), ("v", v), ("q", q0)])
+    _check_apart([("out", out), ("slot_index", slot_index)], [("cu_seqlens", cu_seqlens), ("accepted", accepted)])
     _on_device(device, q=q, k=k, v=v, cu_seqlens=cu_seqlens, out=out, accepted=accepted,
                slot_index=slot_index)
 
@@ -486,6 +524,12 @@ def check_causal_args(cfg, device, q, k, v, cu_seqlens, out, lse, dout=None, dq=
     _check_packed(inputs, outputs, dt, d)
     _check_cu(cu_seqlens)
     _check("lse", lse, torch.float32, (T, Hq), align16=False)
+    tensors, written = [x[:2] for x in inputs], [x[:2] for x in outputs]
+    if dout is None:
+        _check_apart([("lse", lse)], [*tensors, *written])
+        _check_apart([*written, ("lse", lse)], [("cu_seqlens", cu_seqlens)])
+    else:
+        _check_apart(written, [("lse", lse), ("cu_seqlens", cu_seqlens)])
     _on_device(device, cu_seqlens=cu_seqlens, lse=lse,
                **{name: t for name, t, _, _ in (*inputs, *outputs)})
 
@@ -667,9 +711,10 @@ class DMCChunk:
         call, cfg = self._call, self.cache.cfg
         T = call.rows(k)
         Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
-        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),)) if T > 0 else None
-        cu = call.array(cu_seqlens, call.i32, self._cu_shape)
-        if args is None or cu is None:
+        cu, args = call.array(cu_seqlens, call.i32, self._cu_shape), None
+        if cu is not None and T > 0:
+            args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),), ((cu, cu + 4 * cfg.batch + 4),))
+        if args is None:
             check_chunk_args(cfg, self.cache.device, q, k, v, cu_seqlens, out)
             args, cu = _packed_args(q, k, v, out), cu_seqlens.data_ptr()
         (qp, kp, vp, op), st = args
@@ -684,11 +729,17 @@ class DMCChunk:
         call, cfg = self._call, self.cache.cfg
         T = call.rows(k)
         Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
-        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ()) if T > 0 else None
-        cu = call.array(cu_seqlens, call.i32, self._cu_shape)
+        cu, args = call.array(cu_seqlens, call.i32, self._cu_shape), None
         acc = None if accepted is None else call.array(accepted, call.i32, (cfg.batch,))
         slots = None if slot_index is None else call.array(slot_index, call.i32, (T, Hkv))
-        if args is None or cu is None or (acc is None) != (accepted is None) or (slots is None) != (slot_index is None):
+        if cu is not None and (acc is None) == (accepted is None) and (slots is None) == (slot_index is None) and T > 0:
+            read, written = [(cu, cu + 4 * cfg.batch + 4)], ()
+            if acc is not None:
+                read.append((acc, acc + 4 * cfg.batch))
+            if slots is not None:
+                written = ((slots, slots + 4 * T * Hkv),)
+            args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), (), read, written)
+        if args is None:
             check_chunk_args(cfg, self.cache.device, q, k, v, cu_seqlens, None, accepted, slot_index)
             args, cu = _packed_args(q, k, v), cu_seqlens.data_ptr()
             acc, slots = _ptr(accepted), _ptr(slot_index)
@@ -796,9 +847,11 @@ class DMCCausal:
         call = self._call
         T = call.rows(q)
         Hq, Hkv = self.cfg.num_q_heads, self.cfg.num_kv_heads
-        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),)) if T > 0 else None
-        lp, cu = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32)
-        if args is None or lp is None or cu is None:
+        lp, cu, args = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32), None
+        if lp is not None and cu is not None and T > 0:
+            args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv)), ((out, Hq),),
+                                ((cu, cu + 4 * cu_seqlens.shape[0]),), ((lp, lp + 4 * T * Hq),))
+        if args is None:
             check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse)
             args, lp, cu = _packed_args(q, k, v, out), lse.data_ptr(), cu_seqlens.data_ptr()
         if T > self.max_tokens:
@@ -817,10 +870,12 @@ class DMCCausal:
         call = self._call
         T = call.rows(q)
         Hq, Hkv = self.cfg.num_q_heads, self.cfg.num_kv_heads
-        args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv), (out, Hq), (dout, Hq)),
-                            ((dq, Hq), (dk, Hkv), (dv, Hkv))) if T > 0 else None
-        lp, cu = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32)
-        if args is None or lp is None or cu is None:
+        lp, cu, args = call.array(lse, call.f32, (T, Hq)), call.array(cu_seqlens, call.i32), None
+        if lp is not None and cu is not None and T > 0:
+            args = call.tensors(T, ((q, Hq), (k, Hkv), (v, Hkv), (out, Hq), (dout, Hq)),
+                                ((dq, Hq), (dk, Hkv), (dv, Hkv)),
+                                ((cu, cu + 4 * cu_seqlens.shape[0]), (lp, lp + 4 * T * Hq)))
+        if args is None:
             check_causal_args(self.cfg, self.device, q, k, v, cu_seqlens, out, lse, dout, dq, dk, dv)
             args = _packed_args(q, k, v, out, dout, dq, dk, dv)
             lp, cu = lse.data_ptr(), cu_seqlens.data_ptr()
