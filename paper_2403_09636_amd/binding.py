@@ -534,12 +534,14 @@ def check_causal_args(cfg, device, q, k, v, cu_seqlens, out, lse, dout=None, dq=
                **{name: t for name, t, _, _ in (*inputs, *outputs)})
 
 
-def _stream(stream):
+def _stream(stream, device):
+    """The handle of a stream, or of the current one of the device that the call's tensors are on
+    (which need not be the current device)."""
     import torch
     if stream is not None:
         return stream.cuda_stream
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # no Stream object around the handle
-    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
 def _cuda_device(device):
@@ -572,7 +574,7 @@ class DMCCache:
         self._ws_bytes = nbytes
         handle = c_void_p()
         check(lib.dmc_cache_alloc(ctypes.byref(cfg), c_void_p(self._ws_ptr), nbytes,
-                                  _stream(stream), ctypes.byref(handle)))
+                                  _stream(stream, self.device), ctypes.byref(handle)))
         self.handle = handle
         self._decode_call = _DecodeCall(cfg, self.device)
 
@@ -594,7 +596,7 @@ class DMCCache:
             check_decode_args(self.cfg, self.device, q, k, v, out, slot_index)
             ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                     None if slot_index is None else slot_index.data_ptr())
-        check(step(self.handle, layer, *ptrs, _stream(stream)))
+        check(step(self.handle, layer, *ptrs, _stream(stream, self.device)))
         return out
 
     def decode_step(self, layer, q, k, v, out=None, slot_index=None, stream=None):
@@ -616,7 +618,7 @@ class DMCCache:
         vs = (c_int64 * 3)(v.stride(0), v.stride(1), v.stride(2))
         qs = (c_int64 * 3)(q.stride(0), q.stride(1), q.stride(2))
         check(lib.dmc_prefill_compress(self.handle, layer, _ptr(k), ks, _ptr(v), vs, _ptr(q), qs,
-                                       n, _ptr(prompt_lens), _ptr(slot_index), _stream(stream)))
+                                       n, _ptr(prompt_lens), _ptr(slot_index), _stream(stream, self.device)))
 
     def prefill_attend(self, layer, k, v, q, out=None, n=None, prompt_lens=None, slot_index=None,
                        stream=None):
@@ -635,7 +637,7 @@ class DMCCache:
         os_ = (c_int64 * 3)(out.stride(0), out.stride(1), out.stride(2))
         check(lib.dmc_prefill_attend(self.handle, layer, _ptr(k), ks, _ptr(v), vs, _ptr(q), qs, n,
                                      _ptr(prompt_lens), _ptr(out), os_, _ptr(slot_index),
-                                     _stream(stream)))
+                                     _stream(stream, self.device)))
         return out
 
     # -- accessors --------------------------------------------------------------
@@ -643,7 +645,7 @@ class DMCCache:
         import torch
         out = torch.empty((self.cfg.batch, self.cfg.num_kv_heads), dtype=torch.int32,
                           device=self.device)
-        check(lib.dmc_cache_lengths(self.handle, layer, _ptr(out), _stream(stream)))
+        check(lib.dmc_cache_lengths(self.handle, layer, _ptr(out), _stream(stream, self.device)))
         return out
 
     def export(self, layer, dense_slots=None, stream=None):
@@ -654,27 +656,27 @@ class DMCCache:
         V = torch.empty(shape, dtype=self.dtype, device=self.device)
         z = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
         check(lib.dmc_cache_export(self.handle, layer, _ptr(K), _ptr(V), dense_slots, _ptr(z),
-                                   _stream(stream)))
+                                   _stream(stream, self.device)))
         return K, V, z
 
     def import_(self, layer, K, V, lengths, z, stream=None):
         check_import_args(self.cfg, self.device, K, V, lengths, z)
         check(lib.dmc_cache_import(self.handle, layer, _ptr(K), _ptr(V), K.shape[2],
-                                   _ptr(lengths), _ptr(z), _stream(stream)))
+                                   _ptr(lengths), _ptr(z), _stream(stream, self.device)))
 
     def check(self, stream=None):
-        check(lib.dmc_cache_check(self.handle, _stream(stream)))
+        check(lib.dmc_cache_check(self.handle, _stream(stream, self.device)))
 
     def status(self, stream=None) -> int:
-        return lib.dmc_cache_check(self.handle, _stream(stream))
+        return lib.dmc_cache_check(self.handle, _stream(stream, self.device))
 
     def pages_used(self, stream=None) -> int:
         n = c_int64()
-        check(lib.dmc_cache_pages_used(self.handle, ctypes.byref(n), _stream(stream)))
+        check(lib.dmc_cache_pages_used(self.handle, ctypes.byref(n), _stream(stream, self.device)))
         return n.value
 
     def reset(self, stream=None):
-        check(lib.dmc_cache_reset(self.handle, _stream(stream)))
+        check(lib.dmc_cache_reset(self.handle, _stream(stream, self.device)))
 
 
 class DMCChunk:
@@ -720,7 +722,7 @@ class DMCChunk:
         (qp, kp, vp, op), st = args
         check(lib.dmc_chunk_attend(self.cache.handle, layer, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
                                    self._tokens(T), self.max_chunk, op, byref(st, 48), self._ws,
-                                   self._ws_bytes, _stream(stream)))
+                                   self._ws_bytes, _stream(stream, self.cache.device)))
         return out
 
     def append(self, layer, k, v, q, cu_seqlens, accepted=None, slot_index=None, stream=None):
@@ -746,7 +748,7 @@ class DMCChunk:
         (qp, kp, vp), st = args
         check(lib.dmc_chunk_append(self.cache.handle, layer, kp, byref(st, 16), vp, byref(st, 32), qp, st, cu, acc,
                                    self._tokens(T), self.max_chunk, slots, self._ws, self._ws_bytes,
-                                   _stream(stream)))
+                                   _stream(stream, self.cache.device)))
 
 
 def torch_empty_like(t):
@@ -785,7 +787,7 @@ class DMCTrainer:
                          (("out", out, "q"), ("alpha", alpha, "tok")))
         check(lib.dmc_train_forward(ctypes.byref(self.cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(noise),
                                     _ptr(out), _ptr(alpha), self._ws, self._ws_bytes,
-                                    _stream(stream)))
+                                    _stream(stream, self.device)))
         return out
 
     def backward(self, q, k, v, noise, out, dout, dalpha=None, dq=None, dk=None, dv=None,
@@ -800,7 +802,7 @@ class DMCTrainer:
         check(lib.dmc_train_backward(ctypes.byref(self.cfg), _ptr(q), _ptr(k), _ptr(v),
                                      _ptr(noise), _ptr(out), _ptr(dout), _ptr(dalpha), _ptr(dq),
                                      _ptr(dk), _ptr(dv), self._ws, self._ws_bytes,
-                                     _stream(stream)))
+                                     _stream(stream, self.device)))
         return dq, dk, dv
 
 
@@ -859,7 +861,7 @@ class DMCCausal:
         (qp, kp, vp, op), st = args
         check(lib.dmc_causal_forward(self._cfg_ref, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
                                      cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, self._ws,
-                                     self._ws_bytes, _stream(stream)))
+                                     self._ws_bytes, _stream(stream, self.device)))
         return out, lse
 
     def backward(self, q, k, v, cu_seqlens, out, lse, dout, dq=None, dk=None, dv=None, stream=None):
@@ -885,5 +887,5 @@ class DMCCausal:
         check(lib.dmc_causal_backward(self._cfg_ref, qp, st, kp, byref(st, 16), vp, byref(st, 32), cu,
                                       cu_seqlens.numel() - 1, T, op, byref(st, 48), lp, dop, byref(st, 64),
                                       dqp, byref(st, 80), dkp, byref(st, 96), dvp, byref(st, 112), self._ws,
-                                      self._ws_bytes, _stream(stream)))
+                                      self._ws_bytes, _stream(stream, self.device)))
         return dq, dk, dv
