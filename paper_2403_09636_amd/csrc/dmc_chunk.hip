@@ -1362,6 +1362,16 @@ __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams 
   }
 }
 
+// Tile `idx` where every row has row_tiles places.
+__device__ __forceinline__ PackedTile row_tile(const ChunkParams &p, int idx) {
+  PackedTile t;
+  t.seq = idx / p.row_tiles;
+  t.tile = idx - t.seq * p.row_tiles;
+  t.start = clamp_token(p.cu[t.seq], p.total);
+  t.n = max(clamp_token(p.cu[t.seq + 1], p.total) - t.start, 0);
+  return t;
+}
+
 // The pieces of a tile put together: o = sum_i 2^(m_i - M) acc_i / sum_i
 // 2^(m_i - M) l_i.  One wave per column, lanes own D / 64 elements; bound by latency:
 // records are read sixteen at a time, or four where there are no more (256 wide tiles
@@ -1372,7 +1382,8 @@ __global__ __launch_bounds__(kThreads) void chunk_combine_kernel(ChunkParams p) 
   constexpr int E = D / 64, REC = D + 4;
   const int g = blockIdx.y, lane = threadIdx.x & 63;
   const int c = blockIdx.z * kWaves + (threadIdx.x >> 6);
-  const PackedTile pt = packed_tile(p.cu, p.rows, p.total, blockIdx.x, p.tile_shift);
+  const PackedTile pt = p.row_tiles > 0 ? row_tile(p, blockIdx.x)
+                                        : packed_tile(p.cu, p.rows, p.total, blockIdx.x, p.tile_shift);
   const int n = min(pt.n, p.max_chunk);
   const int t = (pt.tile << p.tile_shift) + c / G;
   if (pt.tile < 0 || t >= n) return;
@@ -1459,10 +1470,17 @@ void attend_bf16(const ChunkParams &p, bool wide, unsigned pieces, hipStream_t s
 }
 
 template <int ES, int D, int G>
-hipError_t chunk_attend(const ChunkParams &p, bool vt, bool wide, hipStream_t s) {
+hipError_t chunk_attend(ChunkParams p, bool vt, bool wide, hipStream_t s) {
   hipError_t e = vt ? chunk_states<ES, D, (ES == 2 && G >= 4)>(p, s) : chunk_states<ES, D, false>(p, s);
   if (e != hipSuccess) return e;
-  const unsigned tiles = (p.total >> p.tile_shift) + p.rows;
+  // Tiles by the tensors' length, or by the longest rows where that makes less than half of them: a buffer may be
+  // far longer than the rows' tokens.  us by length -> by rows: 1 row of 4 tokens, 16/4 heads, 900 slots, in 1M rows
+  // 944 -> 56; 16 rows of 4, 64/8 heads, 8000 slots, in 64K rows 457 -> 68; but 4 rows of 512 in 2048, where the
+  // packed count leaves an XCD more spare places, 476 -> 481.
+  const int64_t row_tiles = (int64_t(std::min(p.max_chunk, p.total)) + (1 << p.tile_shift) - 1) >> p.tile_shift;
+  const int64_t packed = int64_t(p.total >> p.tile_shift) + p.rows;
+  p.row_tiles = 2 * row_tiles * p.rows <= packed ? static_cast<int32_t>(row_tiles) : 0;
+  const unsigned tiles = static_cast<unsigned>(p.row_tiles > 0 ? row_tiles * p.rows : packed);
   const unsigned pieces = p.fixed_parts > 0 ? unsigned(p.units) * p.fixed_parts
                                             : (tiles * p.hkv + p.piece_budget + 7) / 8 * 8;
   if constexpr (ES == 2) {

@@ -332,6 +332,7 @@ struct ChunkParams {
   float c, scale_log2;
   int32_t rows, total, max_chunk, units, hq, hkv, maxpages, max_slots, log2p, omega_src, decision_src;
   int32_t blocks64, blocks32, tile_shift, piece_budget, piece_min;
+  int32_t row_tiles;             // > 0: tiles are counted as so many to a row; 0: in the tensors' order (attend)
   int32_t fixed_parts;           // > 0: places for pieces of every unit, which has one narrow tile; no plan (attend)
 };
 // Tokens of a column tile of the attention (log2), and whether its workgroups take 128 columns or 32.
