@@ -7,10 +7,15 @@
 //   dQ = dS K / sqrt(d),  dK = dS^T Q / sqrt(d)
 // with dK and dV summed over the query heads of a kv head's group.
 //
-// Bound by the matrix cores: 2 products forward, 7 of the backward's (dq and
-// the two halves of dk, dv each form S again; one kernel for all of them would
-// need the scores once, but either atomics, whose order changes results, or
-// more accumulators than the register file holds).
+// Bound by the matrix cores and the vector work of the softmax beside them: 2
+// products forward, 8 backward for the 5 of the formulas (dq: S, dP, dQ; the dV
+// launch: S, dV; the dK launch: S, dP, dK).  One kernel for all of them would form
+// S and dP once, but needs either atomics, whose order changes results, or the
+// accumulators of all three; dV and dK in one launch, a product less, need 128
+// accumulator and 64 operand registers, which leaves one wave per SIMD (not tried).
+// Of the SIMD cycles of the large cases the matrix pipes are busy for 36 - 52 %
+// (a large matrix product here reaches 47 % of its peak), vector instructions issue
+// in 26 - 43 %; LDS moves data in 22 - 28 %, without bank conflicts.
 //
 // A workgroup owns a tile of one head (128 columns in bf16, 32 in fp32) of one
 // sequence, whose other side streams past it in blocks of 32 rows.  Blocks and
@@ -142,9 +147,10 @@ __device__ __forceinline__ const char *row_at(const void *base, const int64_t (&
 //   S^T[key][col] = K . Q^T;   O^T[dim][col] += V^T P^T;   dQ^T[dim][col] += K^T dS^T
 // Score row m is key pi(m) (bits 2 and 3 of m swapped), which makes a lane's
 // score registers the operand of the second product.  Forward: block kb's
-// exponentials run between the score products of block kb + 1.  Bound by the matrix
-// cores and the softmax beside them: 5 sequences up to 8192, 32 heads, d 128, forward
-// 1080 us (920 TFLOP/s); 6 up to 4096, 32/8 heads, forward 500 us, dq 660 us.
+// exponentials run between the score products of block kb + 1.  5 sequences up to
+// 8192, 32 heads, d 128: a forward pass 1045 us (952 TFLOP/s); 6 up to 4096, 32/8
+// heads: forward 512 us, dq 657 us (medians of a trace).  dq at d = 128 holds queries,
+// output gradients and accumulators in 192 registers and spills 10 of the rest.
 // ---------------------------------------------------------------------------
 template <int D, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams p, int ntiles) {
@@ -501,7 +507,9 @@ __global__ __launch_bounds__(kThreads, 2) void causal_query_kernel(CausalParams 
 // each holds half the accumulators and runs two waves per SIMD.
 //   S[row][key] = Q . K^T,  dP[row][key] = dO . V^T   (rows pi-permuted)
 //   dV^T[dim][key] += dO^T P,  dK^T[dim][key] += Q^T dS
-// 6 sequences up to 4096, 32/8 heads, d 128: dV 556-586 us, dK 748-777 us.
+// 6 sequences up to 4096, 32/8 heads, d 128: dV 580 us, dK 757 us (medians of a trace).
+// P and dS enter the products rounded to bf16, the operands' type: off by at most
+// 2^-8 of each, at random, where the gradients are rounded by as much in the end.
 template <int D, int PART>
 __global__ __launch_bounds__(kThreads, 2) void causal_key_kernel(CausalParams p) {
   static_assert(PART == 1 || PART == 2, "dV part or dK part");

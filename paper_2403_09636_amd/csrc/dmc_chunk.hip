@@ -109,9 +109,11 @@ __device__ __forceinline__ char *page_of(const ChunkParams &p, int u, int s) {
 //   ATTEND  every state, closed states, counts; and the plan of the attention (one more workgroup)
 //   APPEND  closed states and the last one into the pages (pages allocated before)
 //   ONE     the same for rows of one block: allocates the pages itself
-// Bound by reading k, v and writing the states: 6 prompts up to 4096 tokens, 32
-// heads, d 128:, SUMS 70-100 us, ATTEND 138, APPEND 122; by the
-// round trips of one workgroup on a few tokens (24 rows of 6: 10 us, 1 row of 4: 6).
+// Bound by reading k, v and writing the states (6 prompts up to 4096 tokens, 32
+// heads, d 128: SUMS 68-100 us, ATTEND 136, APPEND 120), or by the round trips of one
+// workgroup on a few tokens (24 rows of 6: 10 us, 1 row of 4: 6).  Sums and z are
+// fp32; a state is rounded to the cache's type as a slot of that cache is, which is
+// what the token attends to.
 enum { SUMS, ATTEND, APPEND, ONE };
 
 __device__ void plan_pieces(const ChunkParams &p);
@@ -320,7 +322,8 @@ __global__ __launch_bounds__(kStateThreads) void chunk_states_kernel(ChunkParams
       return;
     }
     // records of the blocks before, back to one with a start (its record holds
-    // what is open at its end; the first block's includes the cached open slot)
+    // what is open at its end; the first block's includes the cached open slot);
+    // one after another, so a row that never opens a slot walks back over all of it
     const int32_t *st = p.starts + int64_t(g) * p.blocks64 + c.index;
     for (int j = 1; j <= pt.tile; ++j) {
       const float *cr = p.carry + (int64_t(g) * p.blocks64 + c.index - j) * carry_stride(D);
@@ -684,12 +687,13 @@ __device__ __forceinline__ int page_entry(const int32_t *ptab, int64_t i) {
 //
 // WIDE (many query rows): four waves of 32 columns share the blocks, which come
 // into LDS by direct transfers (a ring of four, three ahead); bound by the
-// matrix cores and the softmax (512 tokens of 4 rows, 64/8 heads, on 6000 slots: 481-507
-// us).  Narrow (few rows): one tile of 32 columns whose
+// matrix cores and the softmax (512 tokens of 4 rows, 64/8 heads, on 6000 slots: 502
+// us, matrix pipes busy for 40 % of the SIMD cycles, vector issue 31 %, LDS 20 %).  Narrow (few rows): one tile of 32 columns whose
 // waves take every fourth block, the keys straight into registers and the values
 // into a ring of two blocks of the wave's own, one block ahead; bound by memory
 // (two workgroups and 128 KB of requests per compute unit; 24 rows of 6 tokens, 32 heads,
-// up to 4096 slots: 87-89 us, 5.2 TB/s).
+// up to 4096 slots: 90 us, 5.2 TB/s).  (Medians of a trace.)  The kernels for pages
+// smaller than a block spill 3 to 7 registers at d = 128.
 //
 // BIG: pages of >= 32 slots (a block lies in one page); VT: value pages, and
 // the blocks of closed values, stored transposed.
@@ -825,7 +829,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
       for (int i = 0; i < NTL; ++i) acc[i] *= f;
     }
   };
-  // P rounded to bf16 for the value product; its sum is over the rounded values.
+  // P rounded to bf16, the type of the value product's operands (off by at most 2^-8 of
+  // each, at random; the output is rounded by as much); its sum is over the rounded
+  // values, so that the weights add up to 1.
   auto operands = [&](const float (&ev)[16], uint4 (&pb)[2]) {
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
@@ -1195,7 +1201,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attend_kernel(ChunkParams p
 // whose four waves take every fourth block of its piece straight from the pages
 // and the closed states; their online-softmax states meet in LDS.  Bound by the
 // fp32 matrix rate, and by the chain of blocks of a wave (5 rows of 77 tokens, 12/6
-// heads, d 64, on up to 1500 tokens' slots: 21 us).
+// heads, d 64, on up to 1500 tokens' slots: 22 us).
 // ---------------------------------------------------------------------------
 template <int D, int G>
 __global__ __launch_bounds__(kThreads) void chunk_attend_f32_kernel(ChunkParams p) {
