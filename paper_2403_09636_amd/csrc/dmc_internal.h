@@ -326,7 +326,7 @@ struct ChunkParams {
   int32_t *piece_base;           // [8][ceil(U / 8) + 1]: pieces before them on their XCD (attend)
   int32_t *pieces;               // [U]: pieces per tile of the unit's columns (attend)
   int32_t *record_base;          // [U]: partial records before the unit's (attend)
-  float *partials;               // [piece_budget][columns][d + 4] (attend)
+  float *partials;               // [records][columns][d + 4], one record to a piece of a tile of several (attend)
   int32_t *old_len;              // [U]: length before the append, -1: the unit's chunk is dropped (append)
   float *old_z;                  // [U] (append)
   float c, scale_log2;
