@@ -688,12 +688,13 @@ __device__ __forceinline__ int page_entry(const int32_t *ptab, int64_t i) {
 // WIDE (many query rows): four waves of 32 columns share the blocks, which come
 // into LDS by direct transfers (a ring of four, three ahead); bound by the
 // matrix cores and the softmax (512 tokens of 4 rows, 64/8 heads, on 6000 slots: 502
-// us, matrix pipes busy for 40 % of the SIMD cycles, vector issue 31 %, LDS 20 %).  Narrow (few rows): one tile of 32 columns whose
-// waves take every fourth block, the keys straight into registers and the values
-// into a ring of two blocks of the wave's own, one block ahead; bound by memory
-// (two workgroups and 128 KB of requests per compute unit; 24 rows of 6 tokens, 32 heads,
-// up to 4096 slots: 90 us, 5.2 TB/s).  (Medians of a trace.)  The kernels for pages
-// smaller than a block spill 3 to 7 registers at d = 128.
+// us, matrix pipes busy for 40 % of the SIMD cycles, vector issue 31 %, LDS 20 %).
+// Narrow (few rows): one tile of 32 columns whose waves take every fourth block, the
+// keys straight into registers and the values into a ring of two blocks of the wave's
+// own, one block ahead; bound by memory (two workgroups and 128 KB of requests per
+// compute unit; 24 rows of 6 tokens, 32 heads, up to 4096 slots: 90 us, 5.2 TB/s).
+// (Medians of a trace.)  The kernels for pages smaller than a block spill 3 to 7
+// registers at d = 128.
 //
 // BIG: pages of >= 32 slots (a block lies in one page); VT: value pages, and
 // the blocks of closed values, stored transposed.

@@ -77,7 +77,7 @@ def test_many_rows(torch_cuda, dtype, tail):
     lens[0], lens[41], lens[99] = 5, 90, 66
     c = Case(8, hkv, 64, dtype, slots, max_tokens=sum(lens) + tail, max_chunk=90, extra=100)
     q, k, v = c.tokens(lens, 2.0, tail=tail)
-    out = f64(c.chunk.attend(0, q, k, v, cu_of(lens).cuda()))
+    out = f64(c.chunk.attend(0, q, k, v, cu_of(lens).cuda(), out=torch_cuda.zeros_like(q)))
     c.chunk.append(0, k, v, q, cu_of(lens).cuda())
     L = c.cache.lengths(0).cpu().numpy()
     sample = (0, 41, 63, 64, 65, 99)
