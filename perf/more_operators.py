@@ -187,25 +187,31 @@ def prepare(case, seed):
     held, page = _contexts(case), case["page"]
     need = [-(-(max(n, 0) + m) // page) for n, m in zip(held, lens)]
     width, pages = max(need), sum(need) + 3
-    # the pages of a cache that has been in use for a while lie in no order
-    order = torch.randperm(pages, generator=gen, device=DEVICE, dtype=torch.int32)
-    table = torch.full((case["rows"], width), -1, device=DEVICE, dtype=torch.int32)
-    for b, (at, n) in enumerate(zip(_cu(need), need)):
-        table[b, :n] = order[at:at + n]
-    st.update(held=held, table=table, lengths=_int32(held))
-    st["kp"], st["vp"] = (torch.randn((pages, hkv, page, d), generator=gen, device=DEVICE, dtype=dt) for _ in range(2))
-    st["q"], k, v = _heads(case, gen, T, hq, hkv, hkv)
-    st["cu"] = None if case["chunk"] == 1 else _int32(_cu(lens))
-    if case["kind"] == "append":
-        st.update(k=k, v=v, freqs=_freqs(case), q_out=torch.empty((T, hq, d), device=DEVICE, dtype=dt))
-    else:
-        st["q"] *= 2   # scores that tell tokens apart
-        st.update(out=torch.empty((T, hq, d), device=DEVICE, dtype=dt), lse=torch.empty((T, hq), device=DEVICE))
+    st.update(held=held, freqs=_freqs(case) if case["kind"] == "append" else None)
     if own:
         cfg = dmc.make_full_config(case["rows"], hq, hkv, d, case["dtype"], page_size=page, max_pages=width,
                                    num_pages=pages, rotary_dim=case.get("rotary", 0),
                                    pairs=case.get("pairs", "halves"))
-        st["full"] = dmc.DMCFull(cfg, T, case["chunk"], inv_freq=st.get("freqs"), device=DEVICE)
+        full = dmc.DMCFull(cfg, max_tokens=T, max_chunk=case["chunk"], inv_freq=st["freqs"], device=DEVICE)
+        st.update(full=full, kp=full.k_pages[0], vp=full.v_pages[0], table=full.page_table, lengths=full.lengths)
+    else:
+        st["kp"], st["vp"] = (torch.empty((pages, hkv, page, d), device=DEVICE, dtype=dt) for _ in range(2))
+        st["table"], st["lengths"] = _int32([[0] * width] * case["rows"]), _int32([0] * case["rows"])
+    st["lengths"].copy_(_int32(held))
+    # the pages of a cache that has been in use for a while lie in no order
+    order = torch.randperm(pages, generator=gen, device=DEVICE, dtype=torch.int32)
+    st["table"].fill_(-1)
+    for b, (at, n) in enumerate(zip(_cu(need), need)):
+        st["table"][b, :n] = order[at:at + n]
+    st["kp"].normal_(generator=gen)
+    st["vp"].normal_(generator=gen)
+    st["q"], k, v = _heads(case, gen, T, hq, hkv, hkv)
+    st["cu"] = None if case["chunk"] == 1 else _int32(_cu(lens))
+    if case["kind"] == "append":
+        st.update(k=k, v=v, q_out=torch.empty((T, hq, d), device=DEVICE, dtype=dt))
+    else:
+        st["q"] *= 2   # scores that tell tokens apart
+        st.update(out=torch.empty((T, hq, d), device=DEVICE, dtype=dt), lse=torch.empty((T, hq), device=DEVICE))
     return st
 
 
@@ -225,13 +231,11 @@ def _run_own(st):
     full = st["full"]
     if case["kind"] == "append":
         if not case["queries"]:
-            full.append(st["kp"], st["vp"], st["table"], st["lengths"], st["k"], st["v"], cu_seqlens=st["cu"])
+            full.append(0, st["k"], st["v"], cu_seqlens=st["cu"])
             return dict(kp=st["kp"], vp=st["vp"])
-        full.append(st["kp"], st["vp"], st["table"], st["lengths"], st["k"], st["v"], q=st["q"],
-                    q_out=st["q_out"], cu_seqlens=st["cu"])
+        full.append(0, st["k"], st["v"], q=st["q"], q_out=st["q_out"], cu_seqlens=st["cu"])
         return dict(kp=st["kp"], vp=st["vp"], q_out=st["q_out"])
-    full.attend(st["kp"], st["vp"], st["table"], st["lengths"], st["q"], cu_seqlens=st["cu"], out=st["out"],
-                lse=st["lse"])
+    full.attend(0, st["q"], cu_seqlens=st["cu"], max_chunk=case["chunk"], out=st["out"], lse=st["lse"])
     return dict(out=st["out"], lse=st["lse"])
 
 
