@@ -403,7 +403,7 @@ def _exact_append(st):
     where = torch.tensor([x * page + pos[t] % page for x, t in zip(pages, live)], device=DEVICE, dtype=torch.long)
     live = torch.tensor(live, device=DEVICE, dtype=torch.long)
     for pool, new in ((kp, k), (vp, st["v"].double())):
-        flat = pool.transpose(1, 2).reshape(-1, case["hkv"], case["d"])
+        flat = pool.transpose(1, 2).reshape(-1, case["hkv"], case["d"]).clone()
         flat[where] = new[live]
         pool.copy_(flat.view(len(pool), page, case["hkv"], case["d"]).transpose(1, 2))
     res = dict(kp=kp, vp=vp)
