@@ -463,6 +463,132 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q_dev,
                                const int64_t dv_strides[2], void *workspace_dev,
                                size_t workspace_bytes, dmc_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Position rotation of packed queries and keys, for the layers' inputs in
+ * training (before dmc_causal_forward) and its gradients.  Pair j of a head is
+ * (x[j], x[j + r/2]) (HALVES) or (x[2j], x[2j + 1]) (ADJACENT) of its first
+ * r = rotary_dim elements; at position p it turns by a = p * inv_freq[j]:
+ *   (x, y) -> (x cos a - y sin a, x sin a + y cos a).
+ * The other elements are copied.  Angles are formed in 64 bits, so that far
+ * positions keep their fraction of a turn; products and sums are fp32, rounded
+ * once.  The rotation is linear and orthogonal: its gradient with respect to x is
+ * the rotation by -a of the result's gradient (inverse = 1).
+ *   q_dev, q_out_dev: [total_tokens, Hq, d], k_dev, k_out_dev: [total_tokens, Hkv,
+ *     d], config dtype, element strides of the token and head axes (d
+ *     contiguous), 16-byte aligned, strides non-negative multiples of 8.  Inputs
+ *     may be broadcast (strides of 0); the rows of an output may not overlap each
+ *     other, nor an output another tensor, but q_out may be q itself and k_out k
+ *     itself (same pointer and strides).
+ *   positions_dev: int32 [total_tokens], any value.
+ *   inv_freq_dev: fp32 [rotary_dim / 2]; not read (may be NULL) if rotary_dim is 0.
+ * The call only enqueues a kernel, so it can be captured in a HIP graph.
+ * ------------------------------------------------------------------------- */
+typedef enum { DMC_PAIRS_HALVES = 0, DMC_PAIRS_ADJACENT = 1 } dmc_rotary_pairs;
+
+typedef struct dmc_rotary_config {
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t dtype;             /* dmc_dtype */
+  int32_t rotary_dim;        /* r: a multiple of 16 in [0, head_dim] */
+  int32_t rotary_pairs;      /* dmc_rotary_pairs */
+} dmc_rotary_config;
+
+dmc_status dmc_rotate(const dmc_rotary_config *cfg, const void *q_dev, const int64_t q_strides[2],
+                      const void *k_dev, const int64_t k_strides[2], const int32_t *positions_dev,
+                      const float *inv_freq_dev, int32_t total_tokens, int32_t inverse,
+                      void *q_out_dev, const int64_t q_out_strides[2], void *k_out_dev,
+                      const int64_t k_out_strides[2], dmc_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A paged cache that keeps every token (Sec. 2.1: no compression; all key
+ * elements count), for layers that keep their full cache and for the
+ * uncompressed model that a DMC model is trained from and measured against.  The
+ * storage is the caller's:
+ *   k_pages_dev, v_pages_dev: [num_pages, Hkv, page_size, d] of one layer,
+ *     contiguous, 16-byte aligned, config dtype.
+ *   page_table_dev: int32 [batch, max_pages]: token p of row b lies in slot
+ *     p % page_size of page page_table[b, p / page_size].  Rows may share pages
+ *     that no call writes (a common prefix); entries past a row's tokens are not
+ *     read.
+ *   lengths_dev: int32 [batch]: the tokens that row b holds before the call.  The
+ *     call's new tokens of the row follow at the positions lengths[b], lengths[b]
+ *     + 1, ...; the caller adds their number once every layer has appended and
+ *     attended.  A negative length marks a row that is not in use (a batch that is
+ *     not full): its tokens are not stored, and their rows of q_out and out are
+ *     zeros, of lse -infinity.
+ * New tokens are one per batch row (cu_seqlens_dev NULL, total_tokens = batch: a
+ * decode step), or packed: row b's are the tokens cu[b] .. cu[b+1]-1, with
+ * cu_seqlens_dev int32 [batch + 1], not decreasing; rows may have none, and tokens
+ * outside every row are neither read nor written, their rows in the outputs
+ * staying as they were.
+ *   Tensors are [total_tokens, heads, d] in the config dtype with element strides
+ *   of the token and head axes (d contiguous), 16-byte aligned, strides
+ *   non-negative multiples of 8.  Inputs may be broadcast (strides of 0); the rows
+ *   of an output may not overlap each other, nor an output another tensor.
+ *   flags_dev: optional int32 word in device memory, into which the kernels OR
+ *     what they find (dmc_full_flag); the caller clears and reads it.
+ *     ROW_FULL: a token's position is past max_pages * page_size - 1: it is
+ *     dropped as in a row that is not in use.  BAD_ROWS: boundaries outside [0,
+ *     total_tokens] or decreasing, a length past the capacity, or more than
+ *     max_chunk tokens in a row; they are clamped (of such a row the tokens past
+ *     max_chunk are not processed).  BAD_PAGE: a page id outside [0, num_pages):
+ *     tokens are not stored there; attention reads page 0 in its place.  There is
+ *     no access outside the tensors, pools and tables; results of a row with
+ *     BAD_ROWS or BAD_PAGE are undefined.
+ * Calls only enqueue kernels (no allocation, no memset, no synchronisation);
+ * lengths, boundaries and page table are read on the device, so that a captured
+ * call serves later steps too.
+ * ------------------------------------------------------------------------- */
+typedef enum { DMC_FLAG_ROW_FULL = 2, DMC_FLAG_BAD_ROWS = 4, DMC_FLAG_BAD_PAGE = 8 } dmc_full_flag;
+
+typedef struct dmc_full_config {
+  int32_t batch;             /* rows of the page table, up to 4096 */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;      /* num_q_heads a multiple of it, any G */
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t dtype;             /* dmc_dtype of the pages, inputs and outputs */
+  int32_t page_size;         /* tokens per page, power of two in [8, 65536] */
+  int32_t max_pages;         /* page-table width; max_pages * page_size up to 2^30 */
+  int32_t num_pages;         /* pages of a pool */
+  int32_t rotary_dim;        /* elements of a head that append rotates: a multiple of 16 in [0, head_dim] */
+  int32_t rotary_pairs;      /* dmc_rotary_pairs */
+} dmc_full_config;
+
+/* Append: the new tokens' keys, rotated by their positions (as dmc_rotate does,
+ * inv_freq_dev as there), and values enter their rows' pages; with queries
+ * (q_dev not NULL), q_out_dev receives these rotated.  q_out may be q itself. */
+dmc_status dmc_full_append(const dmc_full_config *cfg, const void *k_dev, const int64_t k_strides[2],
+                           const void *v_dev, const int64_t v_strides[2], const void *q_dev,
+                           const int64_t q_strides[2], const float *inv_freq_dev,
+                           const int32_t *cu_seqlens_dev, int32_t total_tokens,
+                           const int32_t *lengths_dev, const int32_t *page_table_dev,
+                           void *k_pages_dev, void *v_pages_dev, void *q_out_dev,
+                           const int64_t q_out_strides[2], int32_t *flags_dev,
+                           dmc_stream_t stream);
+
+/* Workspace bytes of dmc_full_attend for up to total_tokens new tokens, at most
+ * max_chunk in a row (0 if invalid, see dmc_last_error). */
+size_t dmc_full_workspace_bytes(const dmc_full_config *cfg, int32_t total_tokens, int32_t max_chunk);
+
+/* Attention of the new tokens, already appended, over their rows' caches: the
+ * token at position p attends to the row's tokens 0 .. p, with scale 1/sqrt(d).
+ *   q_dev, out_dev: [total_tokens, Hq, d].
+ *   max_chunk >= 1: the most new tokens of any row (1 if cu_seqlens_dev is NULL).
+ *   lse_dev: optional fp32 [total_tokens, Hq] contiguous: log sum exp of every
+ *     query's scores (natural logarithm), with which parts can be joined.
+ *   workspace_dev: caller-owned device memory, 256-byte aligned; it carries
+ *     nothing between calls, and calls that may overlap need one each.
+ * A token that a query does not see never reaches it, whatever its key and value
+ * hold.  Nothing is accumulated with atomics: results are the same from run to
+ * run. */
+dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q_dev, const int64_t q_strides[2],
+                           const int32_t *cu_seqlens_dev, int32_t total_tokens, int32_t max_chunk,
+                           const int32_t *lengths_dev, const int32_t *page_table_dev,
+                           const void *k_pages_dev, const void *v_pages_dev, void *out_dev,
+                           const int64_t out_strides[2], float *lse_dev, int32_t *flags_dev,
+                           void *workspace_dev, size_t workspace_bytes, dmc_stream_t stream);
+
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *dmc_last_error(void);
 

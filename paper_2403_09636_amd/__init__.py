@@ -6,4 +6,5 @@ include/dmc.h); ``binding`` marshals torch tensors into it.
 from .binding import (DMCCache, DMCError, CacheConfig, make_config,  # noqa: F401
                       workspace_bytes, LIB_PATH, EXPORTS, DMCTrainer, TrainConfig,
                       make_train_config, DMCCausal, CausalConfig, make_causal_config,
-                      DMCChunk)
+                      DMCChunk, DMCRotation, RotaryConfig, make_rotary_config, DMCFull,
+                      FullConfig, make_full_config)

@@ -21,6 +21,9 @@ DMC_DECISION_PER_HEAD, DMC_DECISION_SHARED_LAYER = 0, 1
 OMEGA_SRC = {"lead": DMC_OMEGA_LEAD_QHEAD, "group_mean": DMC_OMEGA_GROUP_MEAN,
              "uniform": DMC_OMEGA_UNIFORM}
 DECISION_SRC = {"per_head": DMC_DECISION_PER_HEAD, "shared_layer": DMC_DECISION_SHARED_LAYER}
+DMC_PAIRS_HALVES, DMC_PAIRS_ADJACENT = 0, 1
+PAIRS = {"halves": DMC_PAIRS_HALVES, "adjacent": DMC_PAIRS_ADJACENT}
+DMC_FLAG_ROW_FULL, DMC_FLAG_BAD_ROWS, DMC_FLAG_BAD_PAGE = 2, 4, 8
 STATUS_NAMES = {0: "DMC_OK", 1: "DMC_ERR_INVALID_ARG", 2: "DMC_ERR_UNSUPPORTED",
                 3: "DMC_ERR_CAPACITY", 4: "DMC_ERR_HIP"}
 
@@ -31,7 +34,8 @@ EXPORTS = ("dmc_cache_workspace_bytes", "dmc_cache_alloc", "dmc_cache_free", "dm
            "dmc_cache_import", "dmc_cache_check", "dmc_cache_pages_used", "dmc_last_error",
            "dmc_train_workspace_bytes", "dmc_train_forward", "dmc_train_backward",
            "dmc_chunk_workspace_bytes", "dmc_chunk_attend", "dmc_chunk_append",
-           "dmc_causal_workspace_bytes", "dmc_causal_forward", "dmc_causal_backward")
+           "dmc_causal_workspace_bytes", "dmc_causal_forward", "dmc_causal_backward",
+           "dmc_rotate", "dmc_full_append", "dmc_full_workspace_bytes", "dmc_full_attend")
 
 
 class CacheConfig(ctypes.Structure):
@@ -55,6 +59,19 @@ class CausalConfig(ctypes.Structure):
     """Mirror of dmc_causal_config."""
     _fields_ = [("num_q_heads", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32),
                 ("dtype", c_int32)]
+
+
+class RotaryConfig(ctypes.Structure):
+    """Mirror of dmc_rotary_config."""
+    _fields_ = [("num_q_heads", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32),
+                ("dtype", c_int32), ("rotary_dim", c_int32), ("rotary_pairs", c_int32)]
+
+
+class FullConfig(ctypes.Structure):
+    """Mirror of dmc_full_config."""
+    _fields_ = [("batch", c_int32), ("num_q_heads", c_int32), ("num_kv_heads", c_int32),
+                ("head_dim", c_int32), ("dtype", c_int32), ("page_size", c_int32), ("max_pages", c_int32),
+                ("num_pages", c_int32), ("rotary_dim", c_int32), ("rotary_pairs", c_int32)]
 
 
 class DMCError(RuntimeError):
@@ -116,6 +133,14 @@ def _load():
                                        *packed, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.dmc_causal_backward.argtypes = [POINTER(CausalConfig), *packed * 3, c_void_p, c_int32, c_int32,
                                         *packed, c_void_p, *packed * 4, c_void_p, c_size_t, c_void_p]
+    lib.dmc_rotate.argtypes = [POINTER(RotaryConfig), *packed * 2, c_void_p, c_void_p, c_int32, c_int32, *packed * 2,
+                               c_void_p]
+    lib.dmc_full_append.argtypes = [POINTER(FullConfig), *packed * 3, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                    c_void_p, c_void_p, *packed, c_void_p, c_void_p]
+    lib.dmc_full_workspace_bytes.argtypes = [POINTER(FullConfig), c_int32, c_int32]
+    lib.dmc_full_workspace_bytes.restype = c_size_t
+    lib.dmc_full_attend.argtypes = [POINTER(FullConfig), *packed, c_void_p, c_int32, c_int32, c_void_p, c_void_p,
+                                    c_void_p, c_void_p, *packed, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
         if not name.endswith("workspace_bytes") and name != "dmc_last_error":
             getattr(lib, name).restype = c_int32
@@ -534,6 +559,84 @@ def check_causal_args(cfg, device, q, k, v, cu_seqlens, out, lse, dout=None, dq=
                **{name: t for name, t, _, _ in (*inputs, *outputs)})
 
 
+def _check_in_place(pairs, read, arrays):
+    """Outputs share no memory with another tensor, but with the input of their own if both are the same
+    rows: pairs of (name, input, output name, output), other tensors read, contiguous arrays."""
+    for i, (name, x, out_name, out) in enumerate(pairs):
+        same = out.data_ptr() == x.data_ptr() and out.stride() == x.stride()
+        others = [(n, t) for j, (n, t, _, _) in enumerate(pairs) if j != i]
+        others += [(n, t) for _, _, n, t in pairs[:i]]
+        _check_apart([(out_name, out)], [*([] if same else [(name, x)]), *others, *read, *arrays])
+
+
+def check_rotary_args(cfg, device, q, k, positions, inv_freq, q_out, k_out):
+    """dmc_rotate: packed q, q_out [T, Hq, d] and k, k_out [T, Hkv, d], positions int32 [T], inv_freq
+    float32 [rotary_dim / 2] (None if that is 0); an output may be its own input."""
+    import torch
+    dt = torch.float32 if cfg.dtype == DMC_FP32 else torch.bfloat16
+    Hq, Hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    _check_rows("q", q, dt, None, Hq, d)
+    T = q.shape[0]
+    _check_rows("k", k, dt, T, Hkv, d)
+    _check_rows("q_out", q_out, dt, T, Hq, d)
+    _check_rows("k_out", k_out, dt, T, Hkv, d)
+    _check("positions", positions, torch.int32, (T,), align16=False)
+    arrays = [("positions", positions)]
+    if cfg.rotary_dim:
+        _check("inv_freq", inv_freq, torch.float32, (cfg.rotary_dim // 2,), align16=False)
+        arrays.append(("inv_freq", inv_freq))
+    _check_in_place([("q", q, "q_out", q_out), ("k", k, "k_out", k_out)], [], arrays)
+    _on_device(device, q=q, k=k, q_out=q_out, k_out=k_out, **dict(arrays))
+
+
+def _check_full_tokens(cfg, T, cu_seqlens):
+    if cu_seqlens is not None:
+        _check_cu(cu_seqlens, cfg.batch)
+    elif T != cfg.batch:
+        _fail(f"{T} tokens without cu_seqlens, one for each of {cfg.batch} rows expected")
+
+
+def check_full_append_args(cfg, device, storage, k, v, q=None, q_out=None, cu_seqlens=None):
+    """dmc_full_append: packed k, v [T, Hkv, d], q, q_out [T, Hq, d] (both or none; q_out may be q),
+    cu_seqlens int32 [batch + 1] or None (T = batch); storage: the cache's own tensors, by name."""
+    import torch
+    dt = cache_dtype(cfg)
+    Hq, Hkv, d = cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    _check_rows("k", k, dt, None, Hkv, d)
+    T = k.shape[0]
+    _check_rows("v", v, dt, T, Hkv, d)
+    if (q is None) != (q_out is None):
+        _fail("q and q_out go together")
+    read = [("k", k), ("v", v)]
+    if q is not None:
+        _check_rows("q", q, dt, T, Hq, d)
+        _check_rows("q_out", q_out, dt, T, Hq, d)
+    _check_full_tokens(cfg, T, cu_seqlens)
+    own = list(storage.items())
+    if q is not None:
+        _check_in_place([("q", q, "q_out", q_out)], read, [*own, ("cu_seqlens", cu_seqlens)])
+        read.append(("q", q))
+    _check_apart([x for x in own if x[0] in ("k_pages", "v_pages")], [*read, ("cu_seqlens", cu_seqlens)])
+    _on_device(device, k=k, v=v, q=q, q_out=q_out, cu_seqlens=cu_seqlens)
+
+
+def check_full_attend_args(cfg, device, storage, q, out, lse=None, cu_seqlens=None):
+    """dmc_full_attend: packed q, out [T, Hq, d], lse float32 [T, Hq] or None, cu_seqlens int32 [batch + 1]
+    or None (T = batch); storage: the cache's own tensors, by name."""
+    import torch
+    dt = cache_dtype(cfg)
+    Hq, d = cfg.num_q_heads, cfg.head_dim
+    _check_rows("q", q, dt, None, Hq, d)
+    T = q.shape[0]
+    _check_rows("out", out, dt, T, Hq, d)
+    if lse is not None:
+        _check("lse", lse, torch.float32, (T, Hq), align16=False)
+    _check_full_tokens(cfg, T, cu_seqlens)
+    read = [("q", q), *storage.items(), ("cu_seqlens", cu_seqlens)]
+    _check_apart([("out", out), ("lse", lse)], read)
+    _on_device(device, q=q, out=out, lse=lse, cu_seqlens=cu_seqlens)
+
+
 def _stream(stream, device):
     """The handle of a stream, or of the current one of the device that the call's tensors are on
     (which need not be the current device)."""
@@ -889,3 +992,196 @@ class DMCCausal:
                                       dqp, byref(st, 80), dkp, byref(st, 96), dvp, byref(st, 112), self._ws,
                                       self._ws_bytes, _stream(stream, self.device)))
         return dq, dk, dv
+
+
+def make_rotary_config(num_q_heads, num_kv_heads, head_dim, dtype="bf16", rotary_dim=None, pairs="halves") -> RotaryConfig:
+    """A dmc_rotary_config: rotary_dim elements of every head turn (default: all of them), in pairs
+    (i, i + rotary_dim / 2) ('halves') or (2 i, 2 i + 1) ('adjacent')."""
+    return RotaryConfig(num_q_heads, num_kv_heads, head_dim, DMC_FP32 if dtype in ("fp32", "float32") else DMC_BF16,
+                        head_dim if rotary_dim is None else rotary_dim, PAIRS[pairs])
+
+
+class DMCRotation:
+    """The position rotation of packed queries and keys (forward + backward), for the inputs of DMCCausal.
+    inv_freq float32 [rotary_dim / 2]: radians per position of every pair."""
+
+    def __init__(self, cfg: RotaryConfig, inv_freq=None, device="cuda"):
+        import torch
+        self.cfg = cfg
+        self._cfg_ref = byref(cfg)
+        self.device = _cuda_device(device)
+        fp32 = cfg.dtype == DMC_FP32
+        self._call = _PackedCall(torch.float32 if fp32 else torch.bfloat16, self.device, cfg.head_dim, 4 if fp32 else 2)
+        self.inv_freq = inv_freq
+        if cfg.rotary_dim:
+            _check("inv_freq", inv_freq, torch.float32, (cfg.rotary_dim // 2,), align16=False)
+            _on_device(self.device, inv_freq=inv_freq)
+
+    def _rotate(self, q, k, positions, q_out, k_out, inverse, stream):
+        q_out = torch_empty_like(q) if q_out is None else q_out
+        k_out = torch_empty_like(k) if k_out is None else k_out
+        call, cfg = self._call, self.cfg
+        T = call.rows(q)
+        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
+        pos, args = call.array(positions, call.i32, (T,)), None
+        freq = self.inv_freq.data_ptr() if cfg.rotary_dim else None
+        if pos is not None and T > 0:
+            read = [(pos, pos + 4 * T)]
+            if freq is not None:
+                read.append((freq, freq + 2 * cfg.rotary_dim))
+            args = call.tensors(T, ((q, Hq), (k, Hkv)), ((q_out, Hq), (k_out, Hkv)), read)
+        if args is None:
+            check_rotary_args(cfg, self.device, q, k, positions, self.inv_freq, q_out, k_out)
+            args, pos = _packed_args(q, k, q_out, k_out), positions.data_ptr()
+        (qp, kp, qop, kop), st = args
+        check(lib.dmc_rotate(self._cfg_ref, qp, st, kp, byref(st, 16), pos, freq, T, inverse, qop, byref(st, 32), kop,
+                             byref(st, 48), _stream(stream, self.device)))
+        return q_out, k_out
+
+    def forward(self, q, k, positions, q_out=None, k_out=None, stream=None):
+        """(q_out [T, Hq, d], k_out [T, Hkv, d]): q and k turned by positions int32 [T]; q_out may be q
+        itself, k_out k."""
+        return self._rotate(q, k, positions, q_out, k_out, 0, stream)
+
+    def backward(self, dq_out, dk_out, positions, dq=None, dk=None, stream=None):
+        """(dq, dk): gradients with respect to q and k, given those with respect to q_out and k_out."""
+        return self._rotate(dq_out, dk_out, positions, dq, dk, 1, stream)
+
+
+def make_full_config(batch, num_q_heads, num_kv_heads, head_dim, dtype="bf16", page_size=32, max_pages=128, num_pages=None,
+                     rotary_dim=0, pairs="halves") -> FullConfig:
+    """A dmc_full_config: rows of up to max_pages * page_size tokens; num_pages defaults to room for every row at
+    capacity.  rotary_dim elements of every head are turned by append (0: keys and queries are stored as they are)."""
+    return FullConfig(batch, num_q_heads, num_kv_heads, head_dim, DMC_FP32 if dtype in ("fp32", "float32") else DMC_BF16,
+                      page_size, max_pages, batch * max_pages if num_pages is None else num_pages, rotary_dim, PAIRS[pairs])
+
+
+class DMCFull:
+    """Paged caches of layers that keep every token, with the workspace for calls of up to max_tokens new tokens
+    (default: one per row), at most max_chunk in a row.  The program owns what a scheduler decides and writes it in
+    place:
+
+    - page_table, int32 [batch, max_pages]: the pages of every row, shared by the layers;
+    - lengths, int32 [batch]: the tokens that every row holds before a call (negative: row not in use); the
+      program adds the new ones once all layers have appended and attended;
+    - k_pages, v_pages [num_layers, num_pages, Hkv, page_size, d], to copy whole pages in or out."""
+
+    def __init__(self, cfg: FullConfig, max_tokens=None, max_chunk=1, inv_freq=None, num_layers=1, device="cuda"):
+        import torch
+        self.cfg, self.num_layers = cfg, num_layers
+        self._cfg_ref = byref(cfg)
+        self.device = _cuda_device(device)
+        self.dtype = cache_dtype(cfg)
+        self.max_tokens = cfg.batch if max_tokens is None else max_tokens
+        self.max_chunk = max_chunk
+        n = lib.dmc_full_workspace_bytes(self._cfg_ref, self.max_tokens, max_chunk)
+        if n == 0:
+            raise DMCError(DMC_ERR_INVALID_ARG, last_error())
+        if num_layers < 1:
+            _fail("num_layers must be >= 1")
+        if cfg.rotary_dim:
+            _check("inv_freq", inv_freq, torch.float32, (cfg.rotary_dim // 2,), align16=False)
+            _on_device(self.device, inv_freq=inv_freq)
+        shape = (num_layers, cfg.num_pages, cfg.num_kv_heads, cfg.page_size, cfg.head_dim)
+        dev, i32 = self.device, torch.int32
+        self._storage = dict(k_pages=torch.empty(shape, dtype=self.dtype, device=dev),
+                             v_pages=torch.empty(shape, dtype=self.dtype, device=dev),
+                             page_table=torch.zeros((cfg.batch, cfg.max_pages), dtype=i32, device=dev),
+                             lengths=torch.zeros(cfg.batch, dtype=i32, device=dev),
+                             flags=torch.zeros(1, dtype=i32, device=dev))
+        if cfg.rotary_dim:
+            self._storage["inv_freq"] = inv_freq
+        self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
+        self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
+        self._ws_bytes = n
+        es = 4 if cfg.dtype == DMC_FP32 else 2
+        self._call = _PackedCall(self.dtype, dev, cfg.head_dim, es)
+        self._cu_shape = (cfg.batch + 1,)
+        self._layer_bytes = self.k_pages[0].numel() * es
+        # where the object's own tensors lie, for the calls (the attributes cannot be rebound)
+        self._spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._storage.values()]
+        self._kp, self._vp, self._table, self._lens, self._flags = (lo for lo, _ in self._spans[:5])
+        self._freq = inv_freq.data_ptr() if cfg.rotary_dim else None
+
+    k_pages = property(lambda self: self._storage["k_pages"])
+    v_pages = property(lambda self: self._storage["v_pages"])
+    page_table = property(lambda self: self._storage["page_table"])
+    lengths = property(lambda self: self._storage["lengths"])
+    flags = property(lambda self: self._storage["flags"])
+
+    def _pages(self, layer):
+        if not 0 <= layer < self.num_layers:
+            _fail(f"layer {layer} outside [0, {self.num_layers})")
+        return self._kp + layer * self._layer_bytes, self._vp + layer * self._layer_bytes
+
+    def _rows(self, T, cu_seqlens):
+        """Address and byte ranges of the boundaries; False if the full check has to look at them."""
+        if T > self.max_tokens:
+            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
+        if cu_seqlens is None:
+            return (None, ()) if T == self.cfg.batch else False
+        cu = self._call.array(cu_seqlens, self._call.i32, self._cu_shape)
+        return False if cu is None else (cu, ((cu, cu + 4 * self.cfg.batch + 4),))
+
+    def append(self, layer, k, v, q=None, q_out=None, cu_seqlens=None, stream=None):
+        """Append new tokens' keys, turned by their positions, and values [T, Hkv, d] to the layer's pages: one per
+        row, or with cu_seqlens int32 [batch + 1] row b's being the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1.
+        With q [T, Hq, d], returns q_out, the queries turned likewise (q_out may be q itself)."""
+        if q is not None and q_out is None:
+            q_out = torch_empty_like(q)
+        call, cfg = self._call, self.cfg
+        kp, vp = self._pages(layer)
+        T = call.rows(k)
+        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
+        rows, args = self._rows(T, cu_seqlens), None
+        if rows and T > 0:
+            if q is None:
+                args = call.tensors(T, ((k, Hkv), (v, Hkv)), (), rows[1], self._spans[:2])
+            else:
+                args = call.tensors(T, ((k, Hkv), (v, Hkv), (q, Hq)), ((q_out, Hq),), (*rows[1], *self._spans[2:]),
+                                    self._spans[:2])
+        if args is None:
+            check_full_append_args(cfg, self.device, self._storage, k, v, q, q_out, cu_seqlens)
+            args = _packed_args(k, v) if q is None else _packed_args(k, v, q, q_out)
+            rows = (None if cu_seqlens is None else cu_seqlens.data_ptr(),)
+        ptrs, st = args
+        qp, qop = ptrs[2:] if q is not None else (None, None)
+        check(lib.dmc_full_append(self._cfg_ref, ptrs[0], st, ptrs[1], byref(st, 16), qp, byref(st, 32) if qp else None,
+                                  self._freq, rows[0], T, self._lens, self._table, kp, vp, qop,
+                                  byref(st, 48) if qp else None, self._flags, _stream(stream, self.device)))
+        return q_out
+
+    def attend(self, layer, q, cu_seqlens=None, max_chunk=None, out=None, lse=None, stream=None):
+        """Attention of new tokens' queries [T, Hq, d], whose keys and values are in the pages already, over their
+        rows' caches up to themselves; at most max_chunk (default: the object's) of them in a row.  Returns (out
+        [T, Hq, d], lse [T, Hq] fp32); rows of tokens outside every chunk stay as they are."""
+        import torch
+        if out is None:
+            out = torch_empty_like(q)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        call, cfg = self._call, self.cfg
+        kp, vp = self._pages(layer)
+        T, Hq = call.rows(q), cfg.num_q_heads
+        max_chunk = 1 if cu_seqlens is None else self.max_chunk if max_chunk is None else max_chunk
+        if max_chunk > self.max_chunk:
+            _fail(f"chunks of {max_chunk} tokens, the workspace holds {self.max_chunk}")
+        rows, args, lp = self._rows(T, cu_seqlens), None, call.array(lse, call.f32, (T, Hq))
+        if rows and lp is not None and T > 0:
+            args = call.tensors(T, ((q, Hq),), ((out, Hq),), (*rows[1], *self._spans), ((lp, lp + 4 * T * Hq),))
+        if args is None:
+            check_full_attend_args(cfg, self.device, self._storage, q, out, lse, cu_seqlens)
+            args, lp = _packed_args(q, out), lse.data_ptr()
+            rows = (None if cu_seqlens is None else cu_seqlens.data_ptr(),)
+        (qp, op), st = args
+        check(lib.dmc_full_attend(self._cfg_ref, qp, st, rows[0], T, max_chunk, self._lens, self._table, kp, vp, op,
+                                  byref(st, 16), lp, self._flags, self._ws, self._ws_bytes, _stream(stream, self.device)))
+        return out, lse
+
+    def check(self):
+        """Raise what the calls so far have found on the device (waits for them)."""
+        found = int(self.flags.item())
+        if found & DMC_FLAG_ROW_FULL:
+            raise DMCError(DMC_ERR_CAPACITY, f"a row is full (flags 0x{found:x})")
+        if found:
+            _fail(f"boundaries or lengths out of range, or page ids outside the pool (flags 0x{found:x})")

@@ -16,7 +16,8 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libdmc.so")
 SOURCES = [os.path.join(HERE, "dmc_api.cpp"), os.path.join(HERE, "dmc_kernels.hip"),
            os.path.join(HERE, "dmc_prompt.hip"), os.path.join(HERE, "dmc_train.hip"),
-           os.path.join(HERE, "dmc_causal.hip"), os.path.join(HERE, "dmc_chunk.hip")]
+           os.path.join(HERE, "dmc_causal.hip"), os.path.join(HERE, "dmc_chunk.hip"),
+           os.path.join(HERE, "dmc_full.hip")]
 ARCH = "gfx950"
 
 # Packed-fp32 VALU forms are disabled for every HIP translation unit.

@@ -1238,6 +1238,239 @@ dmc_status dmc_chunk_append(dmc_cache *cache, int32_t layer, const void *k, cons
   return DMC_OK;
 }
 
+// Full caches and the position rotation.
+static dmc_status validate_heads(int32_t hq, int32_t hkv, int32_t head_dim, int32_t dtype, int32_t rotary_dim,
+                                 int32_t rotary_pairs) {
+  if (hq < 1 || hkv < 1) return fail(DMC_ERR_INVALID_ARG, "head counts must be >= 1");
+  if (hq > 4096 || hkv > 4096) return fail(DMC_ERR_UNSUPPORTED, "more than 4096 heads");
+  if (head_dim != 64 && head_dim != 128) return fail(DMC_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", head_dim);
+  if (dtype != DMC_BF16 && dtype != DMC_FP32) return fail(DMC_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16 != 0)
+    return fail(DMC_ERR_INVALID_ARG, "rotary_dim %d is not a multiple of 16 in [0, %d]", rotary_dim, head_dim);
+  if (rotary_pairs != DMC_PAIRS_HALVES && rotary_pairs != DMC_PAIRS_ADJACENT)
+    return fail(DMC_ERR_INVALID_ARG, "unknown rotary_pairs %d", rotary_pairs);
+  return DMC_OK;
+}
+
+static dmc_status validate_full(const dmc_full_config *c) {
+  if (!c) return fail(DMC_ERR_INVALID_ARG, "config is NULL");
+  dmc_status st = validate_heads(c->num_q_heads, c->num_kv_heads, c->head_dim, c->dtype, c->rotary_dim, c->rotary_pairs);
+  if (st != DMC_OK) return st;
+  if (c->num_q_heads % c->num_kv_heads != 0)
+    return fail(DMC_ERR_INVALID_ARG, "num_q_heads (%d) must be a multiple of num_kv_heads (%d)",
+                c->num_q_heads, c->num_kv_heads);
+  if (c->batch < 1 || c->max_pages < 1 || c->num_pages < 1)
+    return fail(DMC_ERR_INVALID_ARG, "batch, max_pages and num_pages must be >= 1");
+  if (c->batch > 4096) return fail(DMC_ERR_UNSUPPORTED, "more than 4096 rows");
+  if (!pow2(c->page_size) || c->page_size < 8 || c->page_size > 65536)
+    return fail(DMC_ERR_INVALID_ARG, "page_size %d is not a power of two in [8, 65536]", c->page_size);
+  if (int64_t(c->max_pages) * c->page_size > (int64_t(1) << 30))
+    return fail(DMC_ERR_UNSUPPORTED, "rows of more than 2^30 tokens");
+  return DMC_OK;
+}
+
+// The rows and tokens of a call on a full cache.
+static dmc_status check_full_rows(const dmc_full_config &c, const int32_t *cu, int32_t total, const int32_t *lengths,
+                                  const int32_t *table, const void *k_pages, const void *v_pages) {
+  if (total < 0) return fail(DMC_ERR_INVALID_ARG, "total_tokens must be >= 0");
+  if (int64_t(total) * (c.num_q_heads + 2 * c.num_kv_heads) * c.head_dim > (int64_t(1) << 36) || total > (1 << 24))
+    return fail(DMC_ERR_UNSUPPORTED, "too many tokens for one call");
+  if (!cu && total != 0 && total != c.batch)
+    return fail(DMC_ERR_INVALID_ARG, "%d tokens without cu_seqlens, one for each of %d rows expected", total, c.batch);
+  if (total == 0) return DMC_OK;
+  if (!lengths || !table || !k_pages || !v_pages)
+    return fail(DMC_ERR_INVALID_ARG, "lengths, page_table, k_pages and v_pages must be non-NULL");
+  if (!aligned16(k_pages) || !aligned16(v_pages))
+    return fail(DMC_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+  return DMC_OK;
+}
+
+static dmc_status run_rotation(int es, int head_dim, bool paged, const dmc::RotateParams &p, dmc_stream_t stream) {
+  int dev = 0;
+  dmc_status st = memory_device(p.k, "k", &dev);
+  if (st != DMC_OK) return st;
+  DeviceGuard g(dev);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the tensors' device");
+  hipError_t e = dmc::launch_rotate(es, head_dim, paged, p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, paged ? "append launch" : "rotation launch");
+  return DMC_OK;
+}
+
+dmc_status dmc_rotate(const dmc_rotary_config *cfg, const void *q, const int64_t q_strides[2], const void *k,
+                      const int64_t k_strides[2], const int32_t *positions, const float *inv_freq, int32_t total,
+                      int32_t inverse, void *q_out, const int64_t q_out_strides[2], void *k_out,
+                      const int64_t k_out_strides[2], dmc_stream_t stream) {
+  if (!cfg) return fail(DMC_ERR_INVALID_ARG, "config is NULL");
+  dmc_status st = validate_heads(cfg->num_q_heads, cfg->num_kv_heads, cfg->head_dim, cfg->dtype, cfg->rotary_dim,
+                                 cfg->rotary_pairs);
+  if (st == DMC_OK) st = check_packed_counts(0, total);
+  if (st != DMC_OK) return st;
+  if (total == 0) return DMC_OK;
+  const int es = cfg->dtype == DMC_FP32 ? 4 : 2;
+  for (const Packed &t : {Packed{"q", q, q_strides, cfg->num_q_heads, false, false},
+                          Packed{"k", k, k_strides, cfg->num_kv_heads, false, false},
+                          Packed{"q_out", q_out, q_out_strides, cfg->num_q_heads, false, true},
+                          Packed{"k_out", k_out, k_out_strides, cfg->num_kv_heads, false, true}}) {
+    st = check_packed(t, total, cfg->head_dim, es);
+    if (st != DMC_OK) return st;
+  }
+  if (!positions || (cfg->rotary_dim > 0 && !inv_freq))
+    return fail(DMC_ERR_INVALID_ARG, "positions and inv_freq must be non-NULL");
+  dmc::RotateParams p{};
+  p.q = q;
+  p.k = k;
+  p.qo = q_out;
+  p.ko = k_out;
+  copy_strides(p.qs, q_strides);
+  copy_strides(p.ks, k_strides);
+  copy_strides(p.qos, q_out_strides);
+  copy_strides(p.kos, k_out_strides);
+  p.inv_freq = inv_freq;
+  p.positions = positions;
+  p.total = total;
+  p.hq = cfg->num_q_heads;
+  p.hkv = cfg->num_kv_heads;
+  p.r = cfg->rotary_dim;
+  p.halves = cfg->rotary_pairs == DMC_PAIRS_HALVES;
+  p.inverse = inverse != 0;
+  return run_rotation(es, cfg->head_dim, false, p, stream);
+}
+
+dmc_status dmc_full_append(const dmc_full_config *cfg, const void *k, const int64_t k_strides[2], const void *v,
+                           const int64_t v_strides[2], const void *q, const int64_t q_strides[2],
+                           const float *inv_freq, const int32_t *cu, int32_t total, const int32_t *lengths,
+                           const int32_t *table, void *k_pages, void *v_pages, void *q_out,
+                           const int64_t q_out_strides[2], int32_t *flags, dmc_stream_t stream) {
+  dmc_status st = validate_full(cfg);
+  if (st == DMC_OK) st = check_full_rows(*cfg, cu, total, lengths, table, k_pages, v_pages);
+  if (st != DMC_OK || total == 0) return st;
+  const int es = cfg->dtype == DMC_FP32 ? 4 : 2;
+  for (const Packed &t : {Packed{"k", k, k_strides, cfg->num_kv_heads, false, false},
+                          Packed{"v", v, v_strides, cfg->num_kv_heads, false, false},
+                          Packed{"q", q, q_strides, cfg->num_q_heads, false, false},
+                          Packed{"q_out", q_out, q_out_strides, cfg->num_q_heads, false, true}}) {
+    if (!q && t.name[0] == 'q') continue;
+    st = check_packed(t, total, cfg->head_dim, es);
+    if (st != DMC_OK) return st;
+  }
+  if (cfg->rotary_dim > 0 && !inv_freq) return fail(DMC_ERR_INVALID_ARG, "inv_freq must be non-NULL");
+  dmc::RotateParams p{};
+  p.k = k;
+  p.v = v;
+  copy_strides(p.ks, k_strides);
+  copy_strides(p.vs, v_strides);
+  if (q) {
+    p.q = q;
+    p.qo = q_out;
+    copy_strides(p.qs, q_strides);
+    copy_strides(p.qos, q_out_strides);
+    p.hq = cfg->num_q_heads;
+  }
+  p.inv_freq = inv_freq;
+  p.cu = cu;
+  p.len = lengths;
+  p.table = table;
+  p.kp = static_cast<char *>(k_pages);
+  p.vp = static_cast<char *>(v_pages);
+  p.flags = flags;
+  p.total = total;
+  p.rows = cfg->batch;
+  p.hkv = cfg->num_kv_heads;
+  p.r = cfg->rotary_dim;
+  p.halves = cfg->rotary_pairs == DMC_PAIRS_HALVES;
+  p.log2p = ilog2(cfg->page_size);
+  p.max_pages = cfg->max_pages;
+  p.num_pages = cfg->num_pages;
+  p.capacity = cfg->max_pages * cfg->page_size;
+  return run_rotation(es, cfg->head_dim, true, p, stream);
+}
+
+static dmc_status check_full_sizes(const dmc_full_config *c, int32_t total, int32_t max_chunk) {
+  dmc_status st = validate_full(c);
+  if (st != DMC_OK) return st;
+  if (total < 0) return fail(DMC_ERR_INVALID_ARG, "total_tokens must be >= 0");
+  if (max_chunk < 1) return fail(DMC_ERR_INVALID_ARG, "max_chunk must be >= 1");
+  if (int64_t(std::max(total, max_chunk)) * c->num_q_heads > (int64_t(1) << 30) || max_chunk > (1 << 24))
+    return fail(DMC_ERR_UNSUPPORTED, "too many tokens and heads for one call");
+  return DMC_OK;
+}
+
+struct FullLayout {
+  int tile_cols;
+  int64_t record_floats;
+  size_t units, partials, total;
+};
+
+static FullLayout full_layout(const dmc_full_config &c, int32_t max_chunk) {
+  FullLayout L{};
+  L.tile_cols = dmc::full_tile_cols(c.dtype == DMC_FP32 ? 4 : 2, max_chunk, c.num_q_heads / c.num_kv_heads);
+  L.record_floats = int64_t(L.tile_cols) * (c.head_dim + 2);
+  L.units = 0;
+  L.partials = align_up(size_t(dmc::kFullPlaces) * sizeof(dmc::FullUnit), 256);
+  L.total = L.partials + align_up(size_t(dmc::kFullPlaces) * 2 * L.record_floats * 4, 256);
+  return L;
+}
+
+size_t dmc_full_workspace_bytes(const dmc_full_config *cfg, int32_t total, int32_t max_chunk) {
+  if (check_full_sizes(cfg, total, max_chunk) != DMC_OK) return 0;
+  return full_layout(*cfg, max_chunk).total;
+}
+
+dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int64_t q_strides[2], const int32_t *cu,
+                           int32_t total, int32_t max_chunk, const int32_t *lengths, const int32_t *table,
+                           const void *k_pages, const void *v_pages, void *out, const int64_t out_strides[2],
+                           float *lse, int32_t *flags, void *ws, size_t bytes, dmc_stream_t stream) {
+  dmc_status st = check_full_sizes(cfg, total, max_chunk);
+  if (st == DMC_OK) st = check_full_rows(*cfg, cu, total, lengths, table, k_pages, v_pages);
+  if (st != DMC_OK || total == 0) return st;
+  const int es = cfg->dtype == DMC_FP32 ? 4 : 2;
+  for (const Packed &t : {Packed{"q", q, q_strides, cfg->num_q_heads, false, false},
+                          Packed{"out", out, out_strides, cfg->num_q_heads, false, true}}) {
+    st = check_packed(t, total, cfg->head_dim, es);
+    if (st != DMC_OK) return st;
+  }
+  if (!cu) max_chunk = 1;
+  const FullLayout L = full_layout(*cfg, max_chunk);
+  if (!ws) return fail(DMC_ERR_INVALID_ARG, "workspace must be non-NULL");
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(DMC_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (bytes < L.total) return fail(DMC_ERR_INVALID_ARG, "workspace has %zu bytes, needs %zu", bytes, L.total);
+  dmc::FullParams p{};
+  p.q = q;
+  p.out = out;
+  copy_strides(p.qs, q_strides);
+  copy_strides(p.os, out_strides);
+  p.lse = lse;
+  p.cu = cu;
+  p.len = lengths;
+  p.table = table;
+  p.kp = static_cast<const char *>(k_pages);
+  p.vp = static_cast<const char *>(v_pages);
+  p.flags = flags;
+  p.units = reinterpret_cast<dmc::FullUnit *>(static_cast<char *>(ws) + L.units);
+  p.partials = reinterpret_cast<float *>(static_cast<char *>(ws) + L.partials);
+  p.record_floats = L.record_floats;
+  p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
+  p.total = total;
+  p.rows = cfg->batch;
+  p.hq = cfg->num_q_heads;
+  p.hkv = cfg->num_kv_heads;
+  p.log2p = ilog2(cfg->page_size);
+  p.max_pages = cfg->max_pages;
+  p.num_pages = cfg->num_pages;
+  p.capacity = cfg->max_pages * cfg->page_size;
+  p.max_chunk = max_chunk;
+  p.places = dmc::kFullPlaces;
+  p.tile_cols = L.tile_cols;
+  int dev = 0;
+  st = memory_device(ws, "the workspace", &dev);
+  if (st != DMC_OK) return st;
+  DeviceGuard g(dev);
+  if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the workspace's device");
+  hipError_t e = dmc::launch_full_attend(es, cfg->head_dim, p, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "full attention launch");
+  return DMC_OK;
+}
+
 static dmc_status read_control(dmc_cache *cache, dmc_stream_t stream, dmc::Control *out) {
   DeviceGuard g(cache->device);
   if (!g.ok) return fail(DMC_ERR_HIP, "cannot select the cache's device");

@@ -18,6 +18,7 @@ enum : int32_t {
   FLAG_POOL_EXHAUSTED = 1,   // no free page for an append
   FLAG_SLOTS_EXHAUSTED = 2,  // unit already holds max_slots_per_seq slots
   FLAG_BAD_LENGTH = 4,       // imported length or prompt length out of range
+  FLAG_BAD_PAGE = 8,         // full caches: page id outside the pool
 };
 
 // Control block at the start of the control section.
@@ -380,6 +381,54 @@ inline ChunkSplit chunk_split(int cu_count, int rows, int hkv, int group, int ma
 hipError_t launch_chunk_attend(int elem_bytes, int head_dim, int group, bool vt, bool wide, const ChunkParams &p,
                                hipStream_t s);
 hipError_t launch_chunk_append(int elem_bytes, int head_dim, bool vt, const ChunkParams &p, hipStream_t s);
+
+// Position rotation of packed tensors, and the append to a full cache (dmc_full.hip).
+// Tensors are [total, heads, d] with element strides of the token and head axes.
+struct RotateParams {
+  const void *q, *k, *v;         // v: append only
+  void *qo, *ko;                 // ko: rotation only
+  int64_t qs[2], ks[2], vs[2], qos[2], kos[2];
+  const float *inv_freq;         // [r / 2]
+  const int32_t *positions;      // [total] (rotation)
+  // append
+  const int32_t *cu;             // [rows + 1], nullptr: one token per row
+  const int32_t *len;            // [rows], < 0: not in use
+  const int32_t *table;          // [rows, max_pages]
+  char *kp, *vp;                 // [num_pages][hkv][P][d]
+  int32_t *flags;                // optional
+  int32_t total, rows, hq, hkv, r, halves, inverse, log2p, max_pages, num_pages, capacity;   // hq 0: no queries
+};
+// (elem_bytes, head_dim); paged: append, else rotation.
+hipError_t launch_rotate(int elem_bytes, int head_dim, bool paged, const RotateParams &p, hipStream_t s);
+
+// Attention of new tokens over a full cache.
+struct FullUnit {                // a unit that starts in a range of the work and goes on in the next one
+  int32_t pieces, row_start, head, first_col, cols;   // pieces 0: none (the others are not set then)
+};
+struct FullParams {
+  const void *q;
+  void *out;
+  int64_t qs[2], os[2];
+  float *lse;                    // optional [total, hq]
+  const int32_t *cu, *len, *table;
+  const char *kp, *vp;
+  int32_t *flags;                // optional
+  FullUnit *units;               // workspace: [places]
+  float *partials;               // workspace: [places][2][record_floats]
+  int64_t record_floats;
+  float scale_log2;
+  int32_t total, rows, hq, hkv, log2p, max_pages, num_pages, capacity, max_chunk, places, tile_cols;
+};
+// Workgroups of the attention: two to each of 256 compute units.
+constexpr int kFullPlaces = 512;
+// Query columns of a tile: 16 or 32 (bf16) that all waves of a workgroup share; wider
+// ones, of whole tokens, once a row has more: 128 (bf16) or 64 (fp32).
+constexpr inline int full_tile_cols(int elem_bytes, int64_t max_chunk, int group) {
+  const int64_t cols = max_chunk * group;
+  if (elem_bytes == 4) return cols <= 16 || group > 64 ? 16 : 64;
+  return cols <= 16 ? 16 : cols <= 32 || group > 128 ? 32 : 128;
+}
+hipError_t launch_full_attend(int elem_bytes, int head_dim, const FullParams &p, hipStream_t s);
 
 // Launchers (return hipGetLastError() after enqueueing).
 hipError_t launch_reset(const ResetParams &p, hipStream_t s);
