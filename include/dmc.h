@@ -568,7 +568,11 @@ dmc_status dmc_full_append(const dmc_full_config *cfg, const void *k_dev, const 
                            dmc_stream_t stream);
 
 /* Workspace bytes of dmc_full_attend for up to total_tokens new tokens, at most
- * max_chunk in a row (0 if invalid, see dmc_last_error). */
+ * max_chunk in a row (0 if invalid, see dmc_last_error).  Its first
+ * DMC_FULL_COUNTER_BYTES count finished parts: the caller fills them with zeros
+ * before the first call, and every call leaves them zero; beyond them the workspace
+ * carries nothing between calls. */
+#define DMC_FULL_COUNTER_BYTES 8192
 size_t dmc_full_workspace_bytes(const dmc_full_config *cfg, int32_t total_tokens, int32_t max_chunk);
 
 /* Attention of the new tokens, already appended, over their rows' caches: the
@@ -577,11 +581,10 @@ size_t dmc_full_workspace_bytes(const dmc_full_config *cfg, int32_t total_tokens
  *   max_chunk >= 1: the most new tokens of any row (1 if cu_seqlens_dev is NULL).
  *   lse_dev: optional fp32 [total_tokens, Hq] contiguous: log sum exp of every
  *     query's scores (natural logarithm), with which parts can be joined.
- *   workspace_dev: caller-owned device memory, 256-byte aligned; it carries
- *     nothing between calls, and calls that may overlap need one each.
+ *   workspace_dev: caller-owned device memory, 256-byte aligned, its counters zero
+ *     (dmc_full_workspace_bytes); calls that may overlap need one each.
  * A token that a query does not see never reaches it, whatever its key and value
- * hold.  Nothing is accumulated with atomics: results are the same from run to
- * run. */
+ * hold.  Parts are joined in a fixed order: results are the same from run to run. */
 dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q_dev, const int64_t q_strides[2],
                            const int32_t *cu_seqlens_dev, int32_t total_tokens, int32_t max_chunk,
                            const int32_t *lengths_dev, const int32_t *page_table_dev,

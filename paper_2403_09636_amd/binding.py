@@ -23,6 +23,7 @@ OMEGA_SRC = {"lead": DMC_OMEGA_LEAD_QHEAD, "group_mean": DMC_OMEGA_GROUP_MEAN,
 DECISION_SRC = {"per_head": DMC_DECISION_PER_HEAD, "shared_layer": DMC_DECISION_SHARED_LAYER}
 DMC_PAIRS_HALVES, DMC_PAIRS_ADJACENT = 0, 1
 PAIRS = {"halves": DMC_PAIRS_HALVES, "adjacent": DMC_PAIRS_ADJACENT}
+DMC_FULL_COUNTER_BYTES = 8192
 DMC_FLAG_ROW_FULL, DMC_FLAG_BAD_ROWS, DMC_FLAG_BAD_PAGE = 2, 4, 8
 STATUS_NAMES = {0: "DMC_OK", 1: "DMC_ERR_INVALID_ARG", 2: "DMC_ERR_UNSUPPORTED",
                 3: "DMC_ERR_CAPACITY", 4: "DMC_ERR_HIP"}
@@ -1092,7 +1093,9 @@ class DMCFull:
         if cfg.rotary_dim:
             self._storage["inv_freq"] = inv_freq
         self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
-        self._ws = c_void_p((self.workspace.data_ptr() + 255) // 256 * 256)
+        at = -self.workspace.data_ptr() % 256
+        self.workspace[at:at + DMC_FULL_COUNTER_BYTES].zero_()
+        self._ws = c_void_p(self.workspace.data_ptr() + at)
         self._ws_bytes = n
         es = 4 if cfg.dtype == DMC_FP32 else 2
         self._call = _PackedCall(self.dtype, dev, cfg.head_dim, es)

@@ -1395,18 +1395,21 @@ static dmc_status check_full_sizes(const dmc_full_config *c, int32_t total, int3
   return DMC_OK;
 }
 
+static_assert(DMC_FULL_COUNTER_BYTES >= dmc::kFullPlaces * 3 * sizeof(int32_t), "counters");
+
 struct FullLayout {
   int tile_cols;
   int64_t record_floats;
-  size_t units, partials, total;
+  size_t counters, cut_units, partials, total;
 };
 
 static FullLayout full_layout(const dmc_full_config &c, int32_t max_chunk) {
   FullLayout L{};
   L.tile_cols = dmc::full_tile_cols(c.dtype == DMC_FP32 ? 4 : 2, max_chunk, c.num_q_heads / c.num_kv_heads);
   L.record_floats = int64_t(L.tile_cols) * (c.head_dim + 2);
-  L.units = 0;
-  L.partials = align_up(size_t(dmc::kFullPlaces) * sizeof(dmc::FullUnit), 256);
+  L.counters = 0;
+  L.cut_units = DMC_FULL_COUNTER_BYTES;
+  L.partials = L.cut_units + align_up(size_t(dmc::kFullPlaces) * sizeof(dmc::FullPiece), 256);
   L.total = L.partials + align_up(size_t(dmc::kFullPlaces) * 2 * L.record_floats * 4, 256);
   return L;
 }
@@ -1446,7 +1449,8 @@ dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int6
   p.kp = static_cast<const char *>(k_pages);
   p.vp = static_cast<const char *>(v_pages);
   p.flags = flags;
-  p.units = reinterpret_cast<dmc::FullUnit *>(static_cast<char *>(ws) + L.units);
+  p.counters = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + L.counters);
+  p.cut_units = reinterpret_cast<dmc::FullPiece *>(static_cast<char *>(ws) + L.cut_units);
   p.partials = reinterpret_cast<float *>(static_cast<char *>(ws) + L.partials);
   p.record_floats = L.record_floats;
   p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
@@ -1461,6 +1465,12 @@ dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int6
   p.max_chunk = max_chunk;
   p.places = dmc::kFullPlaces;
   p.tile_cols = L.tile_cols;
+  const int G = cfg->num_q_heads / cfg->num_kv_heads;
+  p.tile_tokens = std::max(1, L.tile_cols / G);
+  const int64_t tiles = int64_t(total) * G / L.tile_cols + cfg->batch;
+  p.one_launch = dmc::full_one_launch(tiles, cfg->num_kv_heads, p.capacity);
+  p.group_shift = ilog2(G) - 1;
+  p.group_magic = G > 1 ? static_cast<uint32_t>(((uint64_t(1) << (31 + ilog2(G))) + G - 1) / G) : 0;
   int dev = 0;
   st = memory_device(ws, "the workspace", &dev);
   if (st != DMC_OK) return st;

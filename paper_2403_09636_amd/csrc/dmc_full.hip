@@ -218,53 +218,36 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
 // ---------------------------------------------------------------------------
 // Attention: how the work is shared out.  A unit is one column tile (query
 // columns: the pairs of a new token and a head of one kv head's group) of one row
-// and kv head; it takes as many keys as its row holds.  The units of all rows lie
-// one after another in a space of keys, row by row, which is cut into equal
-// ranges, one to a workgroup; a block of 32 keys belongs to the range that its
-// first key lies in.  A workgroup whose range holds a unit whole writes its output,
-// else a partial record (running maximum, sum and accumulator): the record of a
-// unit that started in an earlier range in the workgroup's first place, that of
-// one that goes on in the next range in its second.  The workgroup where a unit
-// starts describes it for the combine pass.
+// and kv head; it takes as many keys as its row holds (or its last token sees).
+// Units are cut into pieces of keys, in ranges, one to a workgroup:
+//   - few units and keys (latency counts): every unit in equal pieces, one piece to
+//     a workgroup;
+//   - else the units of all rows lie one after another in a space of keys, row by
+//     row, which is cut into equal ranges; a block of keys belongs to the range that
+//     its first key lies in.  A range may hold several pieces.
+// A unit in one piece goes straight to the output.  Else every piece leaves a
+// record (running maximum, sum and accumulator), to be joined in the order of the
+// keys: o = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i.  That is done by the
+// workgroup that finishes a unit's last piece (a counter tells) where the caches'
+// capacity is small, else by a second launch (p.one_launch).
 // ---------------------------------------------------------------------------
-// Sums of the rows' keys before every row, in LDS (prefix[rows + 1]); the total.
-template <typename Weight>
-__device__ __forceinline__ int64_t scan_rows(int64_t *prefix, int64_t *sums, int rows, Weight &&weight) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (rows + kThreads - 1) / kThreads, b0 = min(tid * per, rows), b1 = min(b0 + per, rows);
-  int64_t own = 0;
-  for (int b = b0; b < b1; ++b) {
-    prefix[b] = own;
-    own += weight(b);
-  }
-  int64_t x = own;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) sums[wave] = x;
-  __syncthreads();
-  int64_t before = x - own, all = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < wave) before += sums[i];
-    all += sums[i];
-  }
-  for (int b = b0; b < b1; ++b) prefix[b] += before;
-  if (tid == 0) prefix[rows] = all;
-  __syncthreads();
-  return all;
+
+// A wave-uniform value, made visibly so (SGPRs).
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = uniform(static_cast<int>(x)), hi = uniform(static_cast<int>(x >> 32));
+  return static_cast<int64_t>((uint64_t(hi) << 32) | lo);
 }
-// The row whose keys hold position pos of the space (pos < prefix[rows]).
-__device__ __forceinline__ int row_at_key(const int64_t *prefix, int rows, int64_t pos) {
-  int lo = 0, hi = rows;   // prefix[lo] <= pos < prefix[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (prefix[mid] <= pos) lo = mid;
-    else hi = mid;
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
+
+// Sums over the wave's lanes up to each (row_shr 1, 2, 4, 8, row_bcast 15, 31: no LDS).
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
 }
 
 // Workgroup i runs on XCD i mod 8: each XCD takes one run of ranges, so that the
@@ -273,18 +256,15 @@ __device__ __forceinline__ int range_of_block(int blocks) {
   return (blocks & 7) ? static_cast<int>(blockIdx.x) : (blockIdx.x & 7) * (blocks >> 3) + (blockIdx.x >> 3);
 }
 
-// Rows of out and lse of tokens that are dropped (a row not in use, or full).
+// Rows of out and lse of row b's tokens that are dropped (not in use, or full).
 template <int ES, int D>
-__device__ __forceinline__ void clear_dropped(const FullParams &p) {
-  for (int b = blockIdx.x; b < p.rows; b += gridDim.x) {
-    const FullRow r = full_row(p.cu, p.len, p.total, p.capacity, b);
-    const int first = min(r.m, r.given), items = (r.given - first) * p.hq;
-    constexpr int VPR = D * ES / 16;
-    for (int64_t i = threadIdx.x; i < int64_t(items) * VPR; i += kThreads) {
-      const int64_t x = i / VPR, t = r.start + first + x / p.hq, h = x % p.hq;
-      st16(static_cast<char *>(p.out) + (t * p.os[0] + h * p.os[1]) * ES + (i % VPR) * 16, make_uint4(0, 0, 0, 0));
-      if (p.lse && i % VPR == 0) p.lse[t * p.hq + h] = neg_inf();
-    }
+__device__ __forceinline__ void clear_dropped(const FullParams &p, const FullRow &r) {
+  const int first = min(r.m, r.given), items = (r.given - first) * p.hq;
+  constexpr int VPR = D * ES / 16;
+  for (int64_t i = threadIdx.x; i < int64_t(items) * VPR; i += kThreads) {
+    const int64_t x = i / VPR, t = r.start + first + x / p.hq, h = x % p.hq;
+    st16(static_cast<char *>(p.out) + (t * p.os[0] + h * p.os[1]) * ES + (i % VPR) * 16, make_uint4(0, 0, 0, 0));
+    if (p.lse && i % VPR == 0) p.lse[t * p.hq + h] = neg_inf();
   }
 }
 
@@ -301,6 +281,21 @@ __device__ __forceinline__ int table_entry(const int32_t *table, int i) {
   return reinterpret_cast<const_i32_t *>(reinterpret_cast<uintptr_t>(table))[__builtin_amdgcn_readfirstlane(i)];
 }
 
+// Fewest keys of a piece, and the most per workgroup for which units are cut equally.
+constexpr int kNarrowRange = 256, kWideRange = 1024, kEqualKeys = 1024;
+
+// a / G for a < 2^31, by a multiplication (G = 1: group_shift < 0).
+__device__ __forceinline__ int div_group(const FullParams &p, int a) {
+  return p.group_shift < 0 ? a : static_cast<int>(__umulhi(static_cast<uint32_t>(a), p.group_magic) >> p.group_shift);
+}
+// a / b for a < 2^22, b > 0 (a tenth of a microsecond less than the general division).
+__device__ __forceinline__ int small_div(int a, int b) {
+  int q = static_cast<int>(static_cast<float>(a) * __builtin_amdgcn_rcpf(static_cast<float>(b)));
+  const int r = a - q * b;
+  q += r >= b ? 1 : r < 0 ? -1 : 0;
+  return uniform(q);
+}
+
 // How the columns of a row and kv head are cut into tiles.  A row of m new tokens
 // at n ..:
 //   whole rows (TRI false): tiles of `cols` columns, each over all n + m keys;
@@ -310,14 +305,10 @@ __device__ __forceinline__ int table_entry(const int32_t *table, int i) {
 template <bool TRI>
 struct Tiles {
   int n, m, count, step;   // step: tokens of a tile (TRI) or its columns
-  __device__ __forceinline__ Tiles(int n_, int m_, int G, int cols) : n(n_), m(m_) {
-    if constexpr (TRI) {
-      step = cols / G;
-      count = (m + step - 1) / step;
-    } else {
-      step = cols;
-      count = (m * G + cols - 1) / cols;
-    }
+  __device__ __forceinline__ Tiles(int n_, int m_, int G, int cols, int tokens) : n(n_), m(m_) {
+    step = TRI ? tokens : cols;
+    const int all = TRI ? m : m * G;
+    count = all <= step ? 1 : (all + step - 1) / step;
   }
   __device__ __forceinline__ int keys(int t) const { return TRI ? n + min(m, (t + 1) * step) : n + m; }
   __device__ __forceinline__ int64_t before(int t) const {
@@ -337,48 +328,193 @@ struct Tiles {
   __device__ __forceinline__ int first_col(int t, int G) const { return TRI ? t * step * G : t * step; }
 };
 
-// A piece of a unit: keys k0 .. k1 - 1 of the `keys` that tile columns col0 .. col0 +
-// cols - 1 of row b and kv head h take.
-struct Piece {
-  int b, n, start, h, col0, cols, keys, k0, k1;
+typedef FullPiece Piece;
+
+// The rows and their shares of the work.  Up to 64 rows: every wave loads them all,
+// one to a lane, and keeps its own copy in LDS (no barrier, and no second load of a
+// row when a piece of it is taken); else sums before every row in LDS
+// (prefix[rows + 1]).
+struct RowPlace {
+  int64_t before;   // keys (or ranges) of the rows before it
+  int32_t start, n, m, pieces;
 };
-// The next piece of a range of the space that starts at pos (in row b or later).
-template <bool TRI>
-__device__ __forceinline__ Piece next_piece(const FullParams &p, const int64_t *prefix, int b, int64_t pos, int64_t hi,
-                                            int G) {
-  while (prefix[b + 1] <= pos) ++b;
-  Piece x;
-  x.b = __builtin_amdgcn_readfirstlane(b);
-  const FullRow r = full_row(p.cu, p.len, p.total, p.capacity, x.b);
-  x.n = __builtin_amdgcn_readfirstlane(r.n);
-  x.start = __builtin_amdgcn_readfirstlane(r.start);
-  const int m = __builtin_amdgcn_readfirstlane(min(r.m, p.max_chunk));
-  const Tiles<TRI> tiles(x.n, m, G, p.tile_cols);
-  const int64_t per_head = tiles.all(), off = pos - prefix[x.b];
-  x.h = __builtin_amdgcn_readfirstlane(static_cast<int>(off / per_head));
-  const int64_t in_head = off - x.h * per_head;
-  const int t = __builtin_amdgcn_readfirstlane(tiles.at(in_head));
-  x.keys = tiles.keys(t);
-  x.k0 = __builtin_amdgcn_readfirstlane(static_cast<int>(in_head - tiles.before(t)));
-  x.k1 = __builtin_amdgcn_readfirstlane(static_cast<int>(min(int64_t(x.keys), x.k0 + (hi - pos))));
-  x.col0 = tiles.first_col(t, G);
-  x.cols = min(TRI ? tiles.step * G : tiles.step, m * G - x.col0);
-  return x;
-}
-// The keys of all units of row b.
-template <bool TRI>
-__device__ __forceinline__ int64_t row_keys(const FullParams &p, int b, int G) {
-  const FullRow r = full_row(p.cu, p.len, p.total, p.capacity, b);
-  const int m = min(r.m, p.max_chunk);
-  return m > 0 ? p.hkv * Tiles<TRI>(r.n, m, G, p.tile_cols).all() : int64_t(0);
-}
-// Describes the unit that starts in this range and goes on in the next one.
-__device__ __forceinline__ void describe_unit(FullUnit *u, const Piece &x, int64_t pos, int64_t per, int range, int G) {
-  u->pieces = static_cast<int>((pos + x.keys - 1) / per) - range + 1;
-  u->row_start = x.start;
-  u->head = x.h * G;
-  u->first_col = x.col0;
-  u->cols = x.cols;
+struct SpaceLds {
+  RowPlace rows[kWaves][64];
+  int64_t sums[kWaves];
+};
+template <int ES, int D, bool TRI, int LEAST>   // LEAST: fewest keys of a piece
+struct Space {
+  const FullParams &p;
+  int64_t *prefix;
+  RowPlace *places;
+  int64_t all, per, pos, hi;   // pos, hi: what is left of this workgroup's range
+  int G, range, b;             // b: where the last piece was found
+  bool few, equal;             // equal: equal pieces of every unit
+
+  __device__ __forceinline__ Tiles<TRI> tiles(int n, int m) const { return Tiles<TRI>(n, m, G, p.tile_cols, p.tile_tokens); }
+  __device__ __forceinline__ FullRow load(int i) const { return full_row(p.cu, p.len, p.total, p.capacity, i); }
+
+  // Sums up the rows; writes the rows of dropped tokens, and in the first workgroup
+  // the flags of what it finds wrong.
+  __device__ __forceinline__ Space(const FullParams &p_, int64_t *prefix_, SpaceLds &lds)
+      : p(p_), prefix(prefix_), G(p_.hq / p_.hkv), range(range_of_block(gridDim.x)), b(0), few(p_.rows <= 64), equal(false) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int grid = gridDim.x;
+    places = lds.rows[wave];
+    if (few) {
+      FullRow row{0, 0, 0, 0};
+      if (lane < p.rows) row = load(lane);
+      const int m = min(row.m, p.max_chunk), keys = row.n + m;
+      const Tiles<TRI> t = tiles(row.n, m);
+      // (capped, so that 64 of them stay below 2^31: more is more than kEqualKeys)
+      const int units = m > 0 ? static_cast<int>(min(int64_t(p.hkv) * t.count, int64_t(1) << 24)) : 0;
+      const int count = __builtin_amdgcn_readlane(wave_scan(units), 63);
+      const int sum = __builtin_amdgcn_readlane(wave_scan(static_cast<int>(min(int64_t(units) * keys, int64_t(1) << 24))), 63);
+      equal = 2 * count <= grid && sum <= kEqualKeys * grid;
+      int64_t share, x;
+      int pieces = 0;
+      if (equal) {
+        const int each = max(small_div(sum, grid - count) + 1, LEAST);
+        pieces = (keys + each - 1) / each;
+        share = units * pieces;
+        x = wave_scan(units * pieces);
+      } else {
+        share = m > 0 ? p.hkv * t.all() : int64_t(0);
+        x = share;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int64_t y = __shfl_up(x, o, 64);
+          if (lane >= o) x += y;
+        }
+      }
+      all = uniform(__shfl(x, 63, 64));
+      places[lane] = RowPlace{x - share, row.start, row.n, m, pieces};
+      wave_lds_sync();
+      unsigned long long dropped = __ballot(lane < p.rows && row.m < row.given);
+      while (dropped) {
+        const int i = __ffsll(dropped) - 1;
+        dropped &= dropped - 1;
+        if (i % grid == blockIdx.x) clear_dropped<ES, D>(p, load(i));
+      }
+      if (blockIdx.x == 0 && wave == 0 && lane < p.rows && p.flags) {
+        const int32_t f = row_flags(p.cu, p.len, p.total, p.capacity, lane, p.max_chunk);
+        if (f) raise(p.flags, f);
+      }
+    } else {
+      const int each = (p.rows + kThreads - 1) / kThreads, b0 = min(tid * each, p.rows), b1 = min(b0 + each, p.rows);
+      int64_t own = 0;
+      for (int i = b0; i < b1; ++i) {
+        prefix[i] = own;
+        const FullRow r = load(i);
+        const int m = min(r.m, p.max_chunk);
+        if (m > 0) own += p.hkv * tiles(r.n, m).all();
+        if (blockIdx.x == 0 && p.flags) {
+          const int32_t f = row_flags(p.cu, p.len, p.total, p.capacity, i, p.max_chunk);
+          if (f) raise(p.flags, f);
+        }
+      }
+      int64_t x = own;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+      }
+      if (lane == 63) lds.sums[wave] = x;
+      __syncthreads();
+      int64_t first = x - own;
+      all = 0;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        if (i < wave) first += lds.sums[i];
+        all += lds.sums[i];
+      }
+      for (int i = b0; i < b1; ++i) prefix[i] += first;
+      if (tid == 0) prefix[p.rows] = all;
+      __syncthreads();
+      for (int i = blockIdx.x; i < p.rows; i += grid) {
+        const FullRow r = load(i);
+        if (r.m < r.given) clear_dropped<ES, D>(p, r);
+      }
+    }
+    all = uniform(all);
+    per = equal ? 1 : max((all + grid - 1) / grid, int64_t(LEAST));
+    pos = range * per;
+    hi = min(pos + per, all);
+  }
+
+  // The next piece of the range; pos moves behind it.
+  __device__ __forceinline__ Piece next() {
+    Piece x;
+    int m, pieces = 0;
+    int64_t off;
+    if (few) {
+      const RowPlace mine = places[threadIdx.x & 63];
+      x.b = 63 - __clzll(static_cast<long long>(__ballot(mine.m > 0 && mine.before <= pos)));
+      const RowPlace r = places[x.b];
+      x.n = uniform(r.n);
+      x.start = uniform(r.start);
+      m = uniform(r.m);
+      pieces = uniform(r.pieces);
+      off = pos - uniform(r.before);
+    } else {
+      if (prefix[b + 1] <= pos) {   // prefix[lo] <= pos < prefix[end]
+        int lo = b, end = p.rows;
+        while (end - lo > 1) {
+          const int mid = (lo + end) >> 1;
+          if (prefix[mid] <= pos) lo = mid;
+          else end = mid;
+        }
+        b = uniform(lo);
+      }
+      x.b = b;
+      const FullRow r = load(b);
+      x.n = uniform(r.n);
+      x.start = uniform(r.start);
+      m = min(uniform(r.m), p.max_chunk);
+      off = pos - uniform(prefix[b]);
+    }
+    const Tiles<TRI> ts = tiles(x.n, m);
+    int t;
+    if (equal) {
+      const int o = uniform(static_cast<int>(off)), unit = small_div(o, pieces);
+      x.h = small_div(unit, ts.count);
+      t = unit - x.h * ts.count;
+      x.keys = ts.keys(t);
+      x.pieces = pieces;
+      x.index = o - unit * pieces;
+      x.first = range - x.index;
+      const int size = (small_div(x.keys + pieces - 1, pieces) + 31) & ~31;
+      x.k0 = min(x.index * size, x.keys);
+      x.k1 = min(x.k0 + size, x.keys);
+      pos = hi;
+    } else {
+      const int64_t per_head = ts.all();
+      x.h = uniform(static_cast<int>(off / per_head));
+      const int64_t in_head = off - x.h * per_head;
+      t = uniform(ts.at(in_head));
+      x.keys = ts.keys(t);
+      x.k0 = uniform(static_cast<int>(in_head - ts.before(t)));
+      x.k1 = uniform(static_cast<int>(min(int64_t(x.keys), x.k0 + (hi - pos))));
+      const int64_t begin = pos - x.k0;   // the unit's first key
+      x.first = uniform(static_cast<int>(begin / per));
+      x.index = range - x.first;
+      x.pieces = uniform(static_cast<int>((begin + x.keys - 1) / per)) - x.first + 1;
+      pos += x.k1 - x.k0;
+    }
+    x.col0 = ts.first_col(t, G);
+    x.cols = min(TRI ? ts.step * G : ts.step, m * G - x.col0);
+    return x;
+  }
+};
+
+// A record: [D / 2][tile columns] pairs of the accumulator's elements, then [tile
+// columns] (running maximum, sum): a wave, whose lanes hold different columns, writes
+// and reads whole lines.
+// The record of a piece: that of a unit that started in an earlier range in its
+// range's first place, that of one that goes on in the next range in the second.
+__device__ __forceinline__ int record_index(int first, int index) { return 2 * (first + index) + (index == 0 ? 1 : 0); }
+__device__ __forceinline__ float *record_of(const FullParams &p, int first, int index) {
+  return p.partials + record_index(first, index) * p.record_floats;
 }
 
 // E floats to E elements in memory, rounded to nearest even.
@@ -393,6 +529,175 @@ __device__ __forceinline__ void store_out(char *dst, const float *f) {
   } else {
     *reinterpret_cast<uint2 *>(dst) = make_uint2(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]));
   }
+}
+
+// In one launch records go between workgroups of different XCDs, whose L2 caches are
+// not kept coherent: they are written through, 8 bytes at a time (relaxed atomics of
+// the agent's scope), and read with plain loads after an acquire fence, which only
+// the workgroup that joins makes.
+__device__ __forceinline__ void put2(const FullParams &q, float *p, float a, float b) {
+  if (q.one_launch) {
+    const uint64_t x = (uint64_t(__float_as_uint(b)) << 32) | __float_as_uint(a);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  } else {
+    *reinterpret_cast<float2 *>(p) = make_float2(a, b);
+  }
+}
+
+// Joins records from, from + step .. (`count` >= 2 of them) of a unit: into the first
+// of them, or the output.  The statistics of all columns and records first (to LDS,
+// as weights), then the accumulators, two columns' pairs (16 bytes) AT_ONCE times to a
+// thread, all of a step's reads in flight together.  Columns begin (even) .. end - 1.
+constexpr int kJoinPairs = 1024;
+template <int ES, int D, int AT_ONCE>
+__device__ __forceinline__ void join_records(const FullParams &p, const Piece &x, int begin, int end, int from, int step,
+                                             int count, bool last, float2 *w) {
+  const int tid = threadIdx.x, G = p.hq / p.hkv, most = (kJoinPairs / count) & ~1, tc = p.tile_cols;
+  float *into = record_of(p, x.first, from);
+  for (int c0 = begin; c0 < end; c0 += most) {
+    const int cols = min(most, end - c0), halves = (cols + 1) >> 1;   // (a record's columns are an even number)
+    const int64_t stats = int64_t(tc) * D + 2 * c0;
+    __syncthreads();
+    for (int i = tid; i < cols * count; i += kThreads) {
+      const int col = i / count;
+      w[i] = *reinterpret_cast<const float2 *>(record_of(p, x.first, from + (i - col * count) * step) + stats + 2 * col);
+    }
+    __syncthreads();
+    if (tid < cols) {
+      float2 *c = w + tid * count;
+      float top = c[0].x, sum = 0.0f;
+      for (int i = 1; i < count; ++i) top = fmaxf(top, c[i].x);
+      for (int i = 0; i < count; ++i) {
+        c[i].x = fast_exp2(c[i].x - top);
+        sum = fmaf(c[i].y, c[i].x, sum);
+      }
+      c[0].y = sum;
+      const int i = div_group(p, x.col0 + c0 + tid), head = x.h * G + (x.col0 + c0 + tid) - i * G;
+      if (!last) put2(p, into + stats + 2 * tid, top, sum);
+      else if (p.lse) p.lse[int64_t(x.start + i) * p.hq + head] = (top + __log2f(sum)) * kLn2;
+    }
+    __syncthreads();
+    // item: two columns' pair number e2
+    for (int base = tid; base < halves * (D / 2); base += AT_ONCE * kThreads) {
+      f32x4_t o[AT_ONCE] = {};
+      int e2[AT_ONCE], ca[AT_ONCE], cb[AT_ONCE];
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const int item = min(base + k * kThreads, halves * (D / 2) - 1);
+        e2[k] = (halves & (halves - 1)) == 0 ? item >> (31 - __clz(halves)) : item / halves;
+        ca[k] = 2 * (item - e2[k] * halves);
+        cb[k] = min(ca[k] + 1, cols - 1);
+      }
+#pragma unroll 4
+      for (int i = 0; i < count; ++i) {
+        const float *r = record_of(p, x.first, from + i * step) + 2 * c0;
+        f32x4_t a[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) a[k] = *reinterpret_cast<const f32x4_t *>(r + 2 * (e2[k] * tc + ca[k]));
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+          const float fa = w[ca[k] * count + i].x, fb = w[cb[k] * count + i].x;
+          o[k][0] = fmaf(a[k][0], fa, o[k][0]);
+          o[k][1] = fmaf(a[k][1], fa, o[k][1]);
+          o[k][2] = fmaf(a[k][2], fb, o[k][2]);
+          o[k][3] = fmaf(a[k][3], fb, o[k][3]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        if (base + k * kThreads >= halves * (D / 2)) break;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int cc = ca[k] + u;
+          if (cc >= cols) break;
+          if (last) {
+            const int col = x.col0 + c0 + cc, i = div_group(p, col), head = x.h * G + col - i * G;
+            const float inv = 1.0f / w[cc * count].y, a = o[k][2 * u] * inv, b = o[k][2 * u + 1] * inv;
+            char *dst = static_cast<char *>(p.out) + (int64_t(x.start + i) * p.os[0] + head * p.os[1] + 2 * e2[k]) * ES;
+            if constexpr (ES == 2) *reinterpret_cast<uint32_t *>(dst) = cvt_pk_bf16(a, b);
+            else *reinterpret_cast<float2 *>(dst) = make_float2(a, b);
+          } else {
+            put2(p, into + 2 * (e2[k] * tc + c0 + cc), o[k][2 * u], o[k][2 * u + 1]);
+          }
+        }
+      }
+    }
+  }
+}
+
+// The cut units of a workgroup's range, at most two (one that started in an earlier
+// range, one that goes on in the next).
+struct Cuts {
+  Piece piece[2];
+  int last[2], n;
+};
+
+// Joins what is complete once the workgroup's records are written: each wave's
+// stores have arrived before the barrier lets it through (vmcnt 0), and the last
+// workgroup to count reads only after it has counted; it leaves the counter at 0.
+// Counting at the end of the range, not after each piece, keeps the wait out of the
+// stream of keys.  More than kJoin pieces are joined in groups of kJoin first, so
+// that no workgroup reads more than a few dozen records.  Counters: one per record for
+// the groups that start with it, one per range for the unit that starts in it.
+constexpr int kJoin = 16;
+__device__ __forceinline__ int count_up(int32_t *counter, int count) {
+  const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (before == count - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return before == count - 1;
+}
+template <int ES, int D>
+__device__ __forceinline__ void join_cuts(const FullParams &p, Cuts &cuts, void *lds) {
+  float2 *w = static_cast<float2 *>(lds);
+  if (!p.one_launch) {
+    if (threadIdx.x == 0) {
+      Piece *unit = p.cut_units + range_of_block(gridDim.x);   // the one that starts here and goes on
+      if (cuts.n > 0 && cuts.piece[cuts.n - 1].index == 0) *unit = cuts.piece[cuts.n - 1];
+      else unit->pieces = 0;
+    }
+    return;
+  }
+  wait_vmcnt<0>();
+  __syncthreads();
+  const int n = uniform(cuts.n);
+  if (n == 0) return;
+  auto unit_counter = [&](const Piece &x) { return p.counters + 2 * p.places + x.first; };
+  if (threadIdx.x < n) {
+    const Piece &x = cuts.piece[threadIdx.x];
+    const int from = x.index / kJoin * kJoin;
+    cuts.last[threadIdx.x] = x.pieces > kJoin ? count_up(p.counters + record_index(x.first, from), min(kJoin, x.pieces - from))
+                                              : count_up(unit_counter(x), x.pieces);
+  }
+  __syncthreads();
+  for (int i = 0; i < n; ++i) {
+    if (!uniform(cuts.last[i])) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    const Piece x = cuts.piece[i];
+    if (x.pieces <= kJoin) {
+      join_records<ES, D, 4>(p, x, 0, x.cols, 0, 1, x.pieces, true, w);
+      continue;
+    }
+    const int from = x.index / kJoin * kJoin, groups = (x.pieces + kJoin - 1) / kJoin;
+    const int members = min(kJoin, x.pieces - from);
+    if (members > 1) join_records<ES, D, 4>(p, x, 0, x.cols, from, 1, members, false, w);
+    wait_vmcnt<0>();
+    __syncthreads();
+    if (threadIdx.x == 0) cuts.last[i] = count_up(unit_counter(x), groups);
+    __syncthreads();
+    if (!uniform(cuts.last[i])) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    join_records<ES, D, 4>(p, x, 0, x.cols, 0, kJoin, groups, true, w);
+  }
+}
+
+// The second launch: a workgroup per range (one unit at most starts in it and goes
+// on) and `step` columns.
+template <int ES, int D>
+__global__ __launch_bounds__(kThreads) void full_join_kernel(FullParams p, int step) {
+  __shared__ float2 w[kJoinPairs];
+  const Piece x = p.cut_units[blockIdx.x];
+  const int begin = blockIdx.y * step;
+  if (x.pieces < 2 || begin >= x.cols) return;
+  join_records<ES, D, 1>(p, x, begin, min(begin + step, x.cols), 0, 1, x.pieces, true, w);
 }
 
 // ---------------------------------------------------------------------------
@@ -571,9 +876,6 @@ struct Narrow<4, D> {
   }
 };
 
-// Fewest keys of a workgroup's range.
-constexpr int kNarrowRange = 256;
-
 // SMALL: pages of fewer tokens than a block.
 template <int ES, int D, int NT, bool SMALL, bool SPLIT_KEYS>
 __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) {
@@ -582,40 +884,29 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
   constexpr int COLS = 16 * NT * (SPLIT_KEYS ? 1 : kWaves);
   constexpr bool TRI = !SPLIT_KEYS;
   extern __shared__ int64_t prefix[];
-  __shared__ int64_t sums[kWaves];
-  __shared__ __align__(16) float area[SPLIT_KEYS ? kWaves : 1][16][JS];
+  __shared__ SpaceLds space_lds;
+  __shared__ Cuts cuts;
+  __shared__ __align__(16) float area[SPLIT_KEYS ? kWaves : 2][16][JS];
   __shared__ float stat[kWaves][16][2];
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.hq / p.hkv;
 
-  if (blockIdx.x == 0 && p.flags) {
-    int32_t f = 0;
-    for (int b = tid; b < p.rows; b += kThreads) f |= row_flags(p.cu, p.len, p.total, p.capacity, b, p.max_chunk);
-    if (f) raise(p.flags, f);
-  }
-  const int64_t all = scan_rows(prefix, sums, p.rows, [&](int b) { return row_keys<TRI>(p, b, G); });
-  clear_dropped<ES, D>(p);
-  const int range = range_of_block(gridDim.x);
-  const int64_t per = max((all + gridDim.x - 1) / gridDim.x, int64_t(kNarrowRange));
-  const int64_t lo = range * per, hi = min(lo + per, all);
-  bool cut = false;
-  int b = lo < hi ? row_at_key(prefix, p.rows, lo) : 0;
-
-  for (int64_t pos = lo; pos < hi;) {
-    const Piece x = next_piece<TRI>(p, prefix, b, pos, hi, G);
-    b = x.b;
+  Space<ES, D, TRI, kNarrowRange> space(p, prefix, space_lds);
+  if (tid == 0) cuts.n = 0;
+  while (space.pos < space.hi) {
+    const Piece x = space.next();
     const int col0 = x.col0 + (SPLIT_KEYS ? 0 : wave * 16 * NT), cols = min(16 * NT, x.col0 + x.cols - col0);   // this wave's
     // Keys that this wave's columns see, and the last key that they all do.
-    const int keys = SPLIT_KEYS ? x.keys : cols > 0 ? x.n + (col0 + cols - 1) / G + 1 : 0;
-    const int full_end = x.n + col0 / G;
+    const int keys = SPLIT_KEYS ? x.keys : cols > 0 ? x.n + div_group(p, col0 + cols - 1) + 1 : 0;
+    const int full_end = x.n + div_group(p, col0);
 
     typename X::Query q[NT];
     int lim[NT];   // the last key that this lane's column sees
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int c = t * 16 + c16;
-      const int i = (col0 + c) / G, head = x.h * G + (col0 + c) - i * G;
+      const int i = div_group(p, col0 + c), head = x.h * G + (col0 + c) - i * G;
       lim[t] = x.n + i;
       if (c < cols) {
         const char *src = static_cast<const char *>(p.q) + (int64_t(x.start + i) * p.qs[0] + head * p.qs[1]) * ES +
@@ -629,7 +920,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
       }
     }
 
-    const int32_t *table = p.table + int64_t(b) * p.max_pages;
+    const int32_t *table = p.table + int64_t(x.b) * p.max_pages;
     const int kb1 = (min(x.k1, keys) + KEYS - 1) / KEYS;
     // Pages of a block: the block's, or those of this lane's keys and values.
     struct Pages { int x[SMALL ? 2 * U : 1]; };
@@ -767,25 +1058,17 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
       }
     }
 
-    const bool whole = x.k0 == 0 && x.k1 == x.keys;
-    float *rec = p.partials + (int64_t(range) * 2 + (x.k0 == 0 ? 1 : 0)) * p.record_floats;
-    // E elements e0 .. of a column of the tile: to the output, or its record.
+    const bool whole = x.pieces == 1;
+    float *rec = record_of(p, x.first, x.index);
+    // E elements e0 .. of a column of the tile to the output.
     auto put = [&](int col, int e0, float top, float sum, float (&o)[E]) {
-      if (whole) {
-        const int i = (x.col0 + col) / G, head = x.h * G + (x.col0 + col) - i * G;
-        const int64_t token = x.start + i;
-        const float inv = 1.0f / sum;
+      const int i = div_group(p, x.col0 + col), head = x.h * G + (x.col0 + col) - i * G;
+      const int64_t token = x.start + i;
+      const float inv = 1.0f / sum;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= inv;
-        store_out<ES, E>(static_cast<char *>(p.out) + (token * p.os[0] + head * p.os[1] + e0) * ES, o);
-        if (p.lse && e0 == 0) p.lse[token * p.hq + head] = (top + __log2f(sum)) * kLn2;
-      } else {
-        store_out<4, E>(reinterpret_cast<char *>(rec + col * D + e0), o);
-        if (e0 == 0) {
-          rec[COLS * D + 2 * col] = top;
-          rec[COLS * D + 2 * col + 1] = sum;
-        }
-      }
+      for (int e = 0; e < E; ++e) o[e] *= inv;
+      store_out<ES, E>(static_cast<char *>(p.out) + (token * p.os[0] + head * p.os[1] + e0) * ES, o);
+      if (p.lse && e0 == 0) p.lse[token * p.hq + head] = (top + __log2f(sum)) * kLn2;
     };
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -804,38 +1087,62 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
             *reinterpret_cast<f32x4_t *>(&area[wave][c16][(g4 * 4 + r) * E + j]) =
                 f32x4_t{acc[t][j][r], acc[t][j + 1][r], acc[t][j + 2][r], acc[t][j + 3][r]};
         __syncthreads();
-        const int c = tid >> 4, e0 = (tid & 15) * E, col = t * 16 + c;
+        // to the output 16 threads take a column, to a record 16 columns' pairs
+        const int c = whole ? tid >> 4 : tid & 15, part = whole ? tid & 15 : tid >> 4, col = t * 16 + c;
         if (col < x.cols) {
           float top = stat[0][c][0];
 #pragma unroll
           for (int w = 1; w < kWaves; ++w) top = fmaxf(top, stat[w][c][0]);
-          float sum = 0.0f, o[E] = {};
+          float sum = 0.0f, f[kWaves];
 #pragma unroll
           for (int w = 0; w < kWaves; ++w) {
-            const float f = fast_exp2(stat[w][c][0] - top);
-            sum = fmaf(stat[w][c][1], f, sum);
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(area[w][c][e0 + e], f, o[e]);
+            f[w] = fast_exp2(stat[w][c][0] - top);
+            sum = fmaf(stat[w][c][1], f[w], sum);
           }
-          put(col, e0, top, sum, o);
+          if (whole) {
+            float o[E] = {};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+              for (int e = 0; e < E; ++e) o[e] = fmaf(area[w][c][part * E + e], f[w], o[e]);
+            put(col, part * E, top, sum, o);
+          } else {
+#pragma unroll
+            for (int k = 0; k < E / 2; ++k) {
+              const int e2 = k * 16 + part;
+              float a = 0.0f, bb = 0.0f;
+#pragma unroll
+              for (int w = 0; w < kWaves; ++w) {
+                a = fmaf(area[w][c][2 * e2], f[w], a);
+                bb = fmaf(area[w][c][2 * e2 + 1], f[w], bb);
+              }
+              put2(p, rec + 2 * (e2 * COLS + col), a, bb);
+            }
+            if (part == 0) put2(p, rec + COLS * D + 2 * col, top, sum);
+          }
         }
       } else if (t * 16 + c16 < cols) {
+        const int col = wave * 16 * NT + t * 16 + c16;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+          const int e0 = (g4 * 4 + r) * E;
           float o[E];
 #pragma unroll
           for (int j = 0; j < E; ++j) o[j] = acc[t][j][r];
-          put(wave * 16 * NT + t * 16 + c16, (g4 * 4 + r) * E, mx[t], l, o);
+          if (whole) {
+            put(col, e0, mx[t], l, o);
+          } else {
+#pragma unroll
+            for (int j = 0; j < E; j += 2) put2(p, rec + 2 * ((e0 + j) / 2 * COLS + col), o[j], o[j + 1]);
+            if (e0 == 0) put2(p, rec + COLS * D + 2 * col, mx[t], l);
+          }
         }
       }
     }
-    if (x.k0 == 0 && x.k1 < x.keys) {
-      cut = true;
-      if (tid == 0) describe_unit(p.units + range, x, pos, per, range, G);
-    }
-    pos += x.k1 - x.k0;
+    if (!whole && tid == 0) cuts.piece[cuts.n++] = x;
   }
-  if (tid == 0 && !cut) p.units[range].pieces = 0;
+  static_assert(sizeof(area) >= kJoinPairs * sizeof(float2), "join area");
+  join_cuts<ES, D>(p, cuts, area);
 }
 
 // ---------------------------------------------------------------------------
@@ -851,7 +1158,6 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
 // registers the operand of the second product.  Block kb's exponentials run between
 // the score products of block kb + 1.
 // ---------------------------------------------------------------------------
-constexpr int kWideRange = 1024;   // fewest keys of a workgroup's range
 constexpr int kWideCols = 128;
 
 template <int D>
@@ -870,23 +1176,13 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
     else return ring3;
   };
   extern __shared__ int64_t prefix[];
-  __shared__ int64_t sums[kWaves];
+  __shared__ SpaceLds space_lds;
+  __shared__ Cuts cuts;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hb = lane >> 5;
   const int G = p.hq / p.hkv;
-  if (blockIdx.x == 0 && p.flags) {
-    int32_t f = 0;
-    for (int b = tid; b < p.rows; b += kThreads) f |= row_flags(p.cu, p.len, p.total, p.capacity, b, p.max_chunk);
-    if (f) raise(p.flags, f);
-  }
-  const int64_t all = scan_rows(prefix, sums, p.rows, [&](int b) { return row_keys<true>(p, b, G); });
-  clear_dropped<2, D>(p);
-  const int range = range_of_block(gridDim.x);
-  const int64_t per = max((all + gridDim.x - 1) / gridDim.x, int64_t(kWideRange));
-  const int64_t lo = range * per, hi = min(lo + per, all);
-  bool cut = false;
-  int b = lo < hi ? row_at_key(prefix, p.rows, lo) : 0;
+  Space<2, D, true, kWideRange> space(p, prefix, space_lds);
   const float sl2 = p.scale_log2;
   const int mask = (1 << p.log2p) - 1;
 
@@ -907,18 +1203,18 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
   uint32_t traddr[NTL][2];
   tr_offsets<D, 1>(lane, traddr);
 
-  for (int64_t pos = lo; pos < hi;) {
-    const Piece x = next_piece<true>(p, prefix, b, pos, hi, G);
-    b = x.b;
-    const int c = wave * 32 + col, ti = (x.col0 + c) / G, head = x.h * G + (x.col0 + c) - ti * G;
+  if (tid == 0) cuts.n = 0;
+  while (space.pos < space.hi) {
+    const Piece x = space.next();
+    const int c = wave * 32 + col, ti = div_group(p, x.col0 + c), head = x.h * G + (x.col0 + c) - ti * G;
     const bool colv = c < x.cols;
     const int64_t token = x.start + ti;
     const int lim = x.n + ti;   // the last key that this column sees
     const int blk0 = (x.k0 + 31) >> 5, nblk = (x.k1 + 31) >> 5;
     // Keys < wave_hi feed this wave, those up to full_end all of its columns.
     const int wcols = min(32, x.cols - wave * 32);
-    const int wave_hi = wcols > 0 ? min(x.n + (x.col0 + wave * 32 + wcols - 1) / G + 1, nblk * 32) : 0;
-    const int full_end = x.n + (x.col0 + wave * 32) / G;
+    const int wave_hi = wcols > 0 ? min(x.n + div_group(p, x.col0 + wave * 32 + wcols - 1) + 1, nblk * 32) : 0;
+    const int full_end = x.n + div_group(p, x.col0 + wave * 32);
 
     uint4 qop[KS];
     {
@@ -933,7 +1229,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
     for (int i = 0; i < NTL; ++i) acc[i] = f32x16_t{};
     bool left_out = false;
 
-    const int32_t *table = p.table + int64_t(b) * p.max_pages;
+    const int32_t *table = p.table + int64_t(x.b) * p.max_pages;
     struct Pages { int x[DPW]; };
     auto pages_of = [&](int kb) {
       Pages pg;
@@ -1072,7 +1368,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
     }
 
     ls += __shfl_xor(ls, 32, 64);
-    const bool whole = x.k0 == 0 && x.k1 == x.keys;
+    const bool whole = x.pieces == 1;
     if (colv) {
       if (whole) {
         const float inv = 1.0f / ls;
@@ -1086,83 +1382,22 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
           }
         if (p.lse && hb == 0) p.lse[token * p.hq + head] = (m + __log2f(ls)) * kLn2;
       } else {
-        float *rec = p.partials + (int64_t(range) * 2 + (x.k0 == 0 ? 1 : 0)) * p.record_floats;
+        float *rec = record_of(p, x.first, x.index);
+        const uint32_t at = (2 * hb * kWideCols + c) * 8;   // bytes; the rest is the same for all lanes
 #pragma unroll
         for (int i = 0; i < NTL; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<f32x4_t *>(rec + c * D + 32 * i + 8 * j + 4 * hb) =
-                f32x4_t{acc[i][4 * j], acc[i][4 * j + 1], acc[i][4 * j + 2], acc[i][4 * j + 3]};
-        if (hb == 0) {
-          rec[kWideCols * D + 2 * c] = m;
-          rec[kWideCols * D + 2 * c + 1] = ls;
-        }
+          for (int j = 0; j < 16; j += 2) {
+            const char *row = uniform_ptr(reinterpret_cast<const char *>(rec) + (16 * i + 4 * (j >> 2) + (j & 3) / 2) * kWideCols * 8);
+            put2(p, reinterpret_cast<float *>(const_cast<char *>(row) + at), acc[i][j], acc[i][j + 1]);
+          }
+        if (hb == 0) put2(p, rec + kWideCols * D + 2 * c, m, ls);
       }
     }
-    if (x.k0 == 0 && x.k1 < x.keys) {
-      cut = true;
-      if (tid == 0) describe_unit(p.units + range, x, pos, per, range, G);
-    }
-    pos += x.k1 - x.k0;
+    if (!whole && tid == 0) cuts.piece[cuts.n++] = x;
   }
-  if (tid == 0 && !cut) p.units[range].pieces = 0;
-}
-
-// Joins the records of a unit that was cut: o = sum_i 2^(m_i - M) acc_i / sum_i
-// 2^(m_i - M) l_i.  A workgroup per range (one unit at most starts in it and goes
-// on) and 8 columns; D / 4 lanes' groups of 4 elements, the groups that columns do
-// not need sharing the records.
-template <int ES, int D>
-__global__ __launch_bounds__(kThreads) void full_combine_kernel(FullParams p, int tile_cols) {
-  constexpr int LPG = D / 4, GROUPS = kThreads / LPG, CPW = 8;   // lanes of a group
-  const int range = blockIdx.x, col0 = blockIdx.y * CPW;
-  const FullUnit u = p.units[range];
-  const int cols = min(CPW, u.cols - col0);
-  if (u.pieces == 0 || cols <= 0) return;
-  __shared__ __align__(16) float part[GROUPS][D];
-  const int tid = threadIdx.x, group = tid / LPG, gl = tid % LPG;
-  int slices = 1;   // groups per column
-  while (slices * 2 * cols <= GROUPS) slices *= 2;
-  const int G = p.hq / p.hkv;
-  auto record = [&](int i) { return p.partials + (int64_t(range + i) * 2 + (i == 0 ? 1 : 0)) * p.record_floats; };
-  for (int first = 0; first < cols; first += GROUPS / slices) {
-    const int cc = first + group / slices, slice = group % slices;
-    const bool on = cc < cols;
-    const int col = col0 + (on ? cc : 0);
-    float top = lowest(), sum = 0.0f;
-    for (int i = gl; i < u.pieces; i += LPG) {
-      const float *ml = record(i) + tile_cols * D + 2 * col;
-      const float mn = fmaxf(top, ml[0]);
-      sum = sum * fast_exp2(top - mn) + ml[1] * fast_exp2(ml[0] - mn);
-      top = mn;
-    }
-#pragma unroll
-    for (int o = 1; o < LPG; o <<= 1) {
-      const float to = __shfl_xor(top, o, LPG), so = __shfl_xor(sum, o, LPG), mn = fmaxf(top, to);
-      sum = sum * fast_exp2(top - mn) + so * fast_exp2(to - mn);
-      top = mn;
-    }
-    f32x4_t o = f32x4_t{};
-#pragma unroll 4
-    for (int i = slice; i < u.pieces; i += slices) {
-      const float *r = record(i);
-      const f32x4_t x = *reinterpret_cast<const f32x4_t *>(r + col * D + 4 * gl);
-      const float f = fast_exp2(r[tile_cols * D + 2 * col] - top);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
-    }
-    *reinterpret_cast<f32x4_t *>(&part[group][4 * gl]) = o;
-    __syncthreads();
-    if (on && slice == 0) {
-      for (int s = 1; s < slices; ++s) o += *reinterpret_cast<const f32x4_t *>(&part[group + s][4 * gl]);
-      const int i = (u.first_col + col) / G, head = u.head + (u.first_col + col) - i * G;
-      const int64_t token = u.row_start + i;
-      const float inv = 1.0f / sum, f[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-      store_out<ES, 4>(static_cast<char *>(p.out) + (token * p.os[0] + head * p.os[1] + 4 * gl) * ES, f);
-      if (p.lse && gl == 0) p.lse[token * p.hq + head] = (top + __log2f(sum)) * kLn2;
-    }
-    __syncthreads();
-  }
+  static_assert(sizeof(ring0) >= kJoinPairs * sizeof(float2), "join area");
+  join_cuts<2, D>(p, cuts, ring0);
 }
 
 template <int ES, int D, int NT, bool SPLIT_KEYS>
@@ -1188,7 +1423,7 @@ hipError_t launch_rotation(const RotateParams &p, bool paged, hipStream_t s) {
 
 template <int ES, int D>
 hipError_t attend(const FullParams &p, hipStream_t s) {
-  const size_t lds = (size_t(p.rows) + 1) * sizeof(int64_t);
+  const size_t lds = p.rows <= 64 ? 0 : (size_t(p.rows) + 1) * sizeof(int64_t);   // the sums before every row
   if constexpr (ES == 2) {
     if (p.tile_cols == kWideCols) hipLaunchKernelGGL((full_wide_kernel<D>), dim3(p.places), dim3(kThreads), lds, s, p);
     else if (p.tile_cols == 32) launch_narrow<ES, D, 2, true>(p, lds, s);
@@ -1197,8 +1432,11 @@ hipError_t attend(const FullParams &p, hipStream_t s) {
     if (p.tile_cols == 64) launch_narrow<ES, D, 1, false>(p, lds, s);
     else launch_narrow<ES, D, 1, true>(p, lds, s);
   }
-  const int cols = static_cast<int>(std::min<int64_t>(p.tile_cols, int64_t(p.max_chunk) * (p.hq / p.hkv)));
-  hipLaunchKernelGGL((full_combine_kernel<ES, D>), dim3(p.places, (cols + 7) / 8), dim3(kThreads), 0, s, p, p.tile_cols);
+  if (!p.one_launch) {
+    const int cols = static_cast<int>(std::min<int64_t>(p.tile_cols, int64_t(p.max_chunk) * (p.hq / p.hkv)));
+    const int step = cols > 16 ? 8 : 2;
+    hipLaunchKernelGGL((full_join_kernel<ES, D>), dim3(p.places, (cols + step - 1) / step), dim3(kThreads), 0, s, p, step);
+  }
   return hipGetLastError();
 }
 

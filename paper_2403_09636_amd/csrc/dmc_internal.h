@@ -402,8 +402,11 @@ struct RotateParams {
 hipError_t launch_rotate(int elem_bytes, int head_dim, bool paged, const RotateParams &p, hipStream_t s);
 
 // Attention of new tokens over a full cache.
-struct FullUnit {                // a unit that starts in a range of the work and goes on in the next one
-  int32_t pieces, row_start, head, first_col, cols;   // pieces 0: none (the others are not set then)
+// A piece of a unit: keys k0 .. k1 - 1 of the `keys` that tile columns col0 .. col0 +
+// cols - 1 of row b and kv head h take; piece `index` of `pieces`, which are those of
+// ranges first, first + 1, ...
+struct FullPiece {
+  int32_t b, n, start, h, col0, cols, keys, k0, k1, first, index, pieces;
 };
 struct FullParams {
   const void *q;
@@ -413,11 +416,15 @@ struct FullParams {
   const int32_t *cu, *len, *table;
   const char *kp, *vp;
   int32_t *flags;                // optional
-  FullUnit *units;               // workspace: [places]
+  int32_t *counters;             // workspace: [3][places], 0 between calls (one launch)
+  FullPiece *cut_units;          // workspace: [places] (two launches)
+  int32_t one_launch;
   float *partials;               // workspace: [places][2][record_floats]
   int64_t record_floats;
   float scale_log2;
-  int32_t total, rows, hq, hkv, log2p, max_pages, num_pages, capacity, max_chunk, places, tile_cols;
+  uint32_t group_magic;          // a / G = mulhi(a, group_magic) >> group_shift for a < 2^31 (G = 1: group_shift -1)
+  int32_t group_shift;
+  int32_t total, rows, hq, hkv, log2p, max_pages, num_pages, capacity, max_chunk, places, tile_cols, tile_tokens;
 };
 // Workgroups of the attention: two to each of 256 compute units.
 constexpr int kFullPlaces = 512;
@@ -427,6 +434,11 @@ constexpr inline int full_tile_cols(int elem_bytes, int64_t max_chunk, int group
   const int64_t cols = max_chunk * group;
   if (elem_bytes == 4) return cols <= 16 || group > 64 ? 16 : 64;
   return cols <= 16 ? 16 : cols <= 32 || group > 128 ? 32 : 128;
+}
+// Whether records are joined within the attention's launch: where the rows' capacity
+// is small (tiles: column tiles of all rows).  The capacity decides, not the lengths.
+constexpr inline bool full_one_launch(int64_t tiles, int hkv, int64_t capacity) {
+  return tiles * hkv * capacity <= int64_t(1) << 19;
 }
 hipError_t launch_full_attend(int elem_bytes, int head_dim, const FullParams &p, hipStream_t s);
 
