@@ -506,6 +506,38 @@ class _PackedCall:
         return t.data_ptr()
 
 
+class _RowsCall:
+    """Like _PackedCall, for calls of a few tensors whose host time is the larger part of a step: every
+    condition is tested on every call, the strides' array is kept while the strides stay the same."""
+
+    def __init__(self, dtype, device, d, es):
+        import torch
+        self.Tensor, self.dtype, self.device, self.d, self.es = torch.Tensor, dtype, device, d, es
+        self.f32, self.i32 = torch.float32, torch.int32
+        self.values, self.array = None, None
+
+    def take(self, t, shape):
+        """(address, token stride, head stride, end) of a tensor of this shape [T, heads, d], or None."""
+        if not (isinstance(t, self.Tensor) and t.dtype is self.dtype and t.shape == shape and t.device == self.device):
+            return None
+        s0, s1, s2 = t.stride()
+        p = t.data_ptr()
+        if s2 != 1 or (s0 | s1) & 7 or p & 15:
+            return None
+        return p, s0, s1, p + ((shape[0] - 1) * s0 + (shape[1] - 1) * s1 + self.d) * self.es
+
+    def flat(self, t, dtype, shape):
+        """Address of a contiguous tensor of this type and shape, or None."""
+        if isinstance(t, self.Tensor) and t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+            return t.data_ptr()
+        return None
+
+    def strides(self, *values):
+        if values != self.values:
+            self.values, self.array = values, (c_int64 * len(values))(*values)
+        return self.array
+
+
 def check_chunk_args(cfg, device, q, k, v, cu_seqlens, out=None, accepted=None, slot_index=None):
     """dmc_chunk_attend (with out) and dmc_chunk_append: packed k, v [T, Hkv, d] and, for attention,
     q, out [T, Hq, d]; otherwise q [T, Hq] or [T, Hq, *] (only element 0 is read); cu_seqlens int32
@@ -1012,30 +1044,43 @@ class DMCRotation:
         self._cfg_ref = byref(cfg)
         self.device = _cuda_device(device)
         fp32 = cfg.dtype == DMC_FP32
-        self._call = _PackedCall(torch.float32 if fp32 else torch.bfloat16, self.device, cfg.head_dim, 4 if fp32 else 2)
-        self.inv_freq = inv_freq
+        self._call = _RowsCall(torch.float32 if fp32 else torch.bfloat16, self.device, cfg.head_dim, 4 if fp32 else 2)
+        self._inv_freq, self._freq_span = None, (0, 0)
         if cfg.rotary_dim:
             _check("inv_freq", inv_freq, torch.float32, (cfg.rotary_dim // 2,), align16=False)
             _on_device(self.device, inv_freq=inv_freq)
+            self._inv_freq, self._freq_span = inv_freq, (inv_freq.data_ptr(), inv_freq.data_ptr() + 2 * cfg.rotary_dim)
+
+    inv_freq = property(lambda self: self._inv_freq)
+
+    def _quick(self, q, k, positions, q_out, k_out):
+        """Addresses and strides of the call's tensors, or None if the full check has to look at them."""
+        call, cfg = self._call, self.cfg
+        if not (isinstance(q, call.Tensor) and q.dim() == 3 and q.shape[0] > 0):
+            return None
+        T = q.shape[0]
+        q_shape, k_shape = (T, cfg.num_q_heads, cfg.head_dim), (T, cfg.num_kv_heads, cfg.head_dim)
+        a, b, x, y = call.take(q, q_shape), call.take(k, k_shape), call.take(q_out, q_shape), call.take(k_out, k_shape)
+        pos = call.flat(positions, call.i32, (T,))
+        if a is None or b is None or x is None or y is None or pos is None:
+            return None
+        q0, q1, k0, k1, x0, x1, y0, y1 = a[0], a[3], b[0], b[3], x[0], x[3], y[0], y[3]
+        p1, (f0, f1) = pos + 4 * T, self._freq_span
+        if (x0 < q1 and q0 < x1 or x0 < k1 and k0 < x1 or x0 < p1 and pos < x1 or x0 < f1 and f0 < x1 or y0 < q1 and q0 < y1
+                or y0 < k1 and k0 < y1 or y0 < p1 and pos < y1 or y0 < f1 and f0 < y1 or y0 < x1 and x0 < y1):
+            return None
+        return T, q0, k0, pos, x0, y0, call.strides(a[1], a[2], b[1], b[2], x[1], x[2], y[1], y[2])
 
     def _rotate(self, q, k, positions, q_out, k_out, inverse, stream):
         q_out = torch_empty_like(q) if q_out is None else q_out
         k_out = torch_empty_like(k) if k_out is None else k_out
-        call, cfg = self._call, self.cfg
-        T = call.rows(q)
-        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
-        pos, args = call.array(positions, call.i32, (T,)), None
-        freq = self.inv_freq.data_ptr() if cfg.rotary_dim else None
-        if pos is not None and T > 0:
-            read = [(pos, pos + 4 * T)]
-            if freq is not None:
-                read.append((freq, freq + 2 * cfg.rotary_dim))
-            args = call.tensors(T, ((q, Hq), (k, Hkv)), ((q_out, Hq), (k_out, Hkv)), read)
+        args = self._quick(q, k, positions, q_out, k_out)
         if args is None:
-            check_rotary_args(cfg, self.device, q, k, positions, self.inv_freq, q_out, k_out)
-            args, pos = _packed_args(q, k, q_out, k_out), positions.data_ptr()
-        (qp, kp, qop, kop), st = args
-        check(lib.dmc_rotate(self._cfg_ref, qp, st, kp, byref(st, 16), pos, freq, T, inverse, qop, byref(st, 32), kop,
+            check_rotary_args(self.cfg, self.device, q, k, positions, self.inv_freq, q_out, k_out)
+            (q0, k0, x0, y0), st = _packed_args(q, k, q_out, k_out)
+            args = q.shape[0], q0, k0, positions.data_ptr(), x0, y0, st
+        T, q0, k0, pos, x0, y0, st = args
+        check(lib.dmc_rotate(self._cfg_ref, q0, st, k0, byref(st, 16), pos, self._freq_span[0], T, inverse, x0, byref(st, 32), y0,
                              byref(st, 48), _stream(stream, self.device)))
         return q_out, k_out
 
@@ -1083,28 +1128,36 @@ class DMCFull:
         if cfg.rotary_dim:
             _check("inv_freq", inv_freq, torch.float32, (cfg.rotary_dim // 2,), align16=False)
             _on_device(self.device, inv_freq=inv_freq)
+        # pools, page table, lengths and flags in one allocation: one range to keep the calls' tensors apart from
+        dev, es = self.device, 4 if cfg.dtype == DMC_FP32 else 2
+        self._layer_bytes = cfg.num_pages * cfg.num_kv_heads * cfg.page_size * cfg.head_dim * es
+        pools = num_layers * self._layer_bytes
+        sizes = [pools, pools, 4 * cfg.batch * cfg.max_pages, 4 * cfg.batch, 4]
+        starts = [0]
+        for n_bytes in sizes:
+            starts.append(starts[-1] + (n_bytes + 255) // 256 * 256)
+        self._buffer = torch.empty(starts[-1] + 256, dtype=torch.uint8, device=dev)
+        at = -self._buffer.data_ptr() % 256
+        parts = [self._buffer[at + lo:at + lo + n_bytes] for lo, n_bytes in zip(starts, sizes)]
         shape = (num_layers, cfg.num_pages, cfg.num_kv_heads, cfg.page_size, cfg.head_dim)
-        dev, i32 = self.device, torch.int32
-        self._storage = dict(k_pages=torch.empty(shape, dtype=self.dtype, device=dev),
-                             v_pages=torch.empty(shape, dtype=self.dtype, device=dev),
-                             page_table=torch.zeros((cfg.batch, cfg.max_pages), dtype=i32, device=dev),
-                             lengths=torch.zeros(cfg.batch, dtype=i32, device=dev),
-                             flags=torch.zeros(1, dtype=i32, device=dev))
+        self._storage = dict(k_pages=parts[0].view(self.dtype).view(shape), v_pages=parts[1].view(self.dtype).view(shape),
+                             page_table=parts[2].view(torch.int32).view(cfg.batch, cfg.max_pages),
+                             lengths=parts[3].view(torch.int32), flags=parts[4].view(torch.int32))
+        for name in ("page_table", "lengths", "flags"):
+            self._storage[name].zero_()
+        self._kp, self._vp, self._table, self._lens, self._flags = (t.data_ptr() for t in self._storage.values())
+        self._span = self._buffer.data_ptr(), self._buffer.data_ptr() + self._buffer.numel()
+        self._freq_span = 0, 0
         if cfg.rotary_dim:
             self._storage["inv_freq"] = inv_freq
+            self._freq_span = inv_freq.data_ptr(), inv_freq.data_ptr() + 2 * cfg.rotary_dim
         self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=dev)
         at = -self.workspace.data_ptr() % 256
         self.workspace[at:at + DMC_FULL_COUNTER_BYTES].zero_()
         self._ws = c_void_p(self.workspace.data_ptr() + at)
         self._ws_bytes = n
-        es = 4 if cfg.dtype == DMC_FP32 else 2
-        self._call = _PackedCall(self.dtype, dev, cfg.head_dim, es)
+        self._call = _RowsCall(self.dtype, dev, cfg.head_dim, es)
         self._cu_shape = (cfg.batch + 1,)
-        self._layer_bytes = self.k_pages[0].numel() * es
-        # where the object's own tensors lie, for the calls (the attributes cannot be rebound)
-        self._spans = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._storage.values()]
-        self._kp, self._vp, self._table, self._lens, self._flags = (lo for lo, _ in self._spans[:5])
-        self._freq = inv_freq.data_ptr() if cfg.rotary_dim else None
 
     k_pages = property(lambda self: self._storage["k_pages"])
     v_pages = property(lambda self: self._storage["v_pages"])
@@ -1117,14 +1170,60 @@ class DMCFull:
             _fail(f"layer {layer} outside [0, {self.num_layers})")
         return self._kp + layer * self._layer_bytes, self._vp + layer * self._layer_bytes
 
-    def _rows(self, T, cu_seqlens):
-        """Address and byte ranges of the boundaries; False if the full check has to look at them."""
+    def _rows(self, t, cu_seqlens):
+        """(tokens, address of the boundaries or 0) of a call, or None if the full check has to look at them."""
+        call = self._call
+        if not (isinstance(t, call.Tensor) and t.dim() == 3):
+            return None
+        T = t.shape[0]
         if T > self.max_tokens:
             _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
+        if T == 0:
+            return None
         if cu_seqlens is None:
-            return (None, ()) if T == self.cfg.batch else False
-        cu = self._call.array(cu_seqlens, self._call.i32, self._cu_shape)
-        return False if cu is None else (cu, ((cu, cu + 4 * self.cfg.batch + 4),))
+            return (T, 0) if T == self.cfg.batch else None
+        cu = call.flat(cu_seqlens, call.i32, self._cu_shape)
+        return None if cu is None else (T, cu)
+
+    def _quick_append(self, k, v, q, q_out, cu_seqlens):
+        rows = self._rows(k, cu_seqlens)
+        if rows is None:
+            return None
+        (T, cu), call, cfg, (o0, o1) = rows, self._call, self.cfg, self._span
+        shape = T, cfg.num_kv_heads, cfg.head_dim
+        a, b = call.take(k, shape), call.take(v, shape)
+        if a is None or b is None:
+            return None
+        k0, k1, v0, v1, c1 = a[0], a[3], b[0], b[3], cu + 4 * cfg.batch + 4
+        if o0 < k1 and k0 < o1 or o0 < v1 and v0 < o1 or o0 < c1 and cu < o1:
+            return None
+        if q is None:
+            return (T, cu or None, k0, v0, None, None, call.strides(a[1], a[2], b[1], b[2])) if q_out is None else None
+        shape = T, cfg.num_q_heads, cfg.head_dim
+        c, x = call.take(q, shape), call.take(q_out, shape)
+        if c is None or x is None:
+            return None
+        q0, q1, x0, x1, (f0, f1) = c[0], c[3], x[0], x[3], self._freq_span
+        if (o0 < q1 and q0 < o1 or o0 < x1 and x0 < o1 or x0 < k1 and k0 < x1 or x0 < v1 and v0 < x1 or x0 < q1 and q0 < x1
+                or x0 < c1 and cu < x1 or x0 < f1 and f0 < x1):
+            return None
+        return T, cu or None, k0, v0, q0, x0, call.strides(a[1], a[2], b[1], b[2], c[1], c[2], x[1], x[2])
+
+    def _quick_attend(self, q, out, lse, cu_seqlens):
+        rows = self._rows(q, cu_seqlens)
+        if rows is None:
+            return None
+        (T, cu), call, cfg, (o0, o1) = rows, self._call, self.cfg, self._span
+        Hq = cfg.num_q_heads
+        shape = T, Hq, cfg.head_dim
+        a, x, l0 = call.take(q, shape), call.take(out, shape), call.flat(lse, call.f32, (T, Hq))
+        if a is None or x is None or l0 is None:
+            return None
+        q0, q1, x0, x1, l1, c1, (f0, f1) = a[0], a[3], x[0], x[3], l0 + 4 * T * Hq, cu + 4 * cfg.batch + 4, self._freq_span
+        if (x0 < q1 and q0 < x1 or x0 < o1 and o0 < x1 or x0 < l1 and l0 < x1 or x0 < c1 and cu < x1 or l0 < q1 and q0 < l1
+                or l0 < o1 and o0 < l1 or l0 < c1 and cu < l1 or x0 < f1 and f0 < x1 or l0 < f1 and f0 < l1):
+            return None
+        return T, cu or None, q0, x0, l0, call.strides(a[1], a[2], x[1], x[2])
 
     def append(self, layer, k, v, q=None, q_out=None, cu_seqlens=None, stream=None):
         """Append new tokens' keys, turned by their positions, and values [T, Hkv, d] to the layer's pages: one per
@@ -1132,26 +1231,17 @@ class DMCFull:
         With q [T, Hq, d], returns q_out, the queries turned likewise (q_out may be q itself)."""
         if q is not None and q_out is None:
             q_out = torch_empty_like(q)
-        call, cfg = self._call, self.cfg
         kp, vp = self._pages(layer)
-        T = call.rows(k)
-        Hq, Hkv = cfg.num_q_heads, cfg.num_kv_heads
-        rows, args = self._rows(T, cu_seqlens), None
-        if rows and T > 0:
-            if q is None:
-                args = call.tensors(T, ((k, Hkv), (v, Hkv)), (), rows[1], self._spans[:2])
-            else:
-                args = call.tensors(T, ((k, Hkv), (v, Hkv), (q, Hq)), ((q_out, Hq),), (*rows[1], *self._spans[2:]),
-                                    self._spans[:2])
+        args = self._quick_append(k, v, q, q_out, cu_seqlens)
         if args is None:
-            check_full_append_args(cfg, self.device, self._storage, k, v, q, q_out, cu_seqlens)
-            args = _packed_args(k, v) if q is None else _packed_args(k, v, q, q_out)
-            rows = (None if cu_seqlens is None else cu_seqlens.data_ptr(),)
-        ptrs, st = args
-        qp, qop = ptrs[2:] if q is not None else (None, None)
-        check(lib.dmc_full_append(self._cfg_ref, ptrs[0], st, ptrs[1], byref(st, 16), qp, byref(st, 32) if qp else None,
-                                  self._freq, rows[0], T, self._lens, self._table, kp, vp, qop,
-                                  byref(st, 48) if qp else None, self._flags, _stream(stream, self.device)))
+            check_full_append_args(self.cfg, self.device, self._storage, k, v, q, q_out, cu_seqlens)
+            ptrs, st = _packed_args(k, v) if q is None else _packed_args(k, v, q, q_out)
+            args = (k.shape[0], None if cu_seqlens is None else cu_seqlens.data_ptr(), *ptrs[:2],
+                    *(ptrs[2:] if q is not None else (None, None)), st)
+        T, cu, k0, v0, q0, x0, st = args
+        check(lib.dmc_full_append(self._cfg_ref, k0, st, v0, byref(st, 16), q0, byref(st, 32) if q0 else None,
+                                  self._freq_span[0], cu, T, self._lens, self._table, kp, vp, x0,
+                                  byref(st, 48) if q0 else None, self._flags, _stream(stream, self.device)))
         return q_out
 
     def attend(self, layer, q, cu_seqlens=None, max_chunk=None, out=None, lse=None, stream=None):
@@ -1163,22 +1253,18 @@ class DMCFull:
             out = torch_empty_like(q)
         if lse is None:
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        call, cfg = self._call, self.cfg
         kp, vp = self._pages(layer)
-        T, Hq = call.rows(q), cfg.num_q_heads
         max_chunk = 1 if cu_seqlens is None else self.max_chunk if max_chunk is None else max_chunk
         if max_chunk > self.max_chunk:
             _fail(f"chunks of {max_chunk} tokens, the workspace holds {self.max_chunk}")
-        rows, args, lp = self._rows(T, cu_seqlens), None, call.array(lse, call.f32, (T, Hq))
-        if rows and lp is not None and T > 0:
-            args = call.tensors(T, ((q, Hq),), ((out, Hq),), (*rows[1], *self._spans), ((lp, lp + 4 * T * Hq),))
+        args = self._quick_attend(q, out, lse, cu_seqlens)
         if args is None:
-            check_full_attend_args(cfg, self.device, self._storage, q, out, lse, cu_seqlens)
-            args, lp = _packed_args(q, out), lse.data_ptr()
-            rows = (None if cu_seqlens is None else cu_seqlens.data_ptr(),)
-        (qp, op), st = args
-        check(lib.dmc_full_attend(self._cfg_ref, qp, st, rows[0], T, max_chunk, self._lens, self._table, kp, vp, op,
-                                  byref(st, 16), lp, self._flags, self._ws, self._ws_bytes, _stream(stream, self.device)))
+            check_full_attend_args(self.cfg, self.device, self._storage, q, out, lse, cu_seqlens)
+            (q0, x0), st = _packed_args(q, out)
+            args = q.shape[0], None if cu_seqlens is None else cu_seqlens.data_ptr(), q0, x0, lse.data_ptr(), st
+        T, cu, q0, x0, l0, st = args
+        check(lib.dmc_full_attend(self._cfg_ref, q0, st, cu, T, max_chunk, self._lens, self._table, kp, vp, x0,
+                                  byref(st, 16), l0, self._flags, self._ws, self._ws_bytes, _stream(stream, self.device)))
         return out, lse
 
     def check(self):

@@ -265,14 +265,57 @@ def test_config_structs_match_the_header(name, struct):
 
 
 def test_one_pass_checks_agree_with_the_full_ones():
-    """What _PackedCall accepts on its device has the full check's approval."""
+    """What the one-pass checks accept on their device has the full check's approval; whatever they decline goes to
+    it."""
     full = P.DMCFull(CFG, max_tokens=T, max_chunk=2, inv_freq=torch.zeros(R // 2), device="cpu")
-    call = full._call
-    a = _append()
-    ok = call.tensors(T, ((a["k"], HKV), (a["v"], HKV), (a["q"], HQ)), ((a["q_out"], HQ),), full._spans[2:], full._spans[:2])
-    assert ok[0] == [a[x].data_ptr() for x in ("k", "v", "q", "q_out")]
-    k = full.k_pages.view(-1, HKV, D)[:T]
-    assert call.tensors(T, ((k, HKV), (a["v"], HKV), (a["q"], HQ)), ((a["q_out"], HQ),), full._spans[2:], full._spans[:2]) is None
-    q = full.v_pages.view(-1, HQ, D)[:T]
-    assert call.tensors(T, ((a["q"], HQ),), ((q, HQ),), full._spans) is None
-    assert call.tensors(T, ((a["q"], HQ),), ((a["q"], HQ),), full._spans) is None
+    rot = P.DMCRotation(P.make_rotary_config(HQ, HKV, D, rotary_dim=R), full._storage["inv_freq"], device="cpu")
+    pool_k, pool_q = full.k_pages.view(-1, HKV, D)[:T], full.v_pages.view(-1, HQ, D)[:T]
+    x = torch.zeros(T + 1, HQ + HKV, D, dtype=BF)
+
+    def agree(quick, check, a, good):
+        if good:
+            assert quick(**a) is not None
+            check(a)   # does not raise
+        else:
+            assert quick(**a) is None
+
+    def append(a):
+        Bd.check_full_append_args(CFG, CPU, full._storage, **a)
+
+    def attend(a):
+        Bd.check_full_attend_args(CFG, CPU, full._storage, **a)
+
+    def rotate(a):
+        Bd.check_rotary_args(rot.cfg, CPU, inv_freq=rot.inv_freq, **a)
+
+    ok = {n: t for n, t in _append().items() if n != "storage"}
+    agree(full._quick_append, append, ok, True)
+    assert full._quick_append(**ok)[2:6] == tuple(ok[n].data_ptr() for n in ("k", "v", "q", "q_out"))
+    agree(full._quick_append, append, dict(ok, q=None, q_out=None), True)
+    agree(full._quick_append, append, dict(ok, q=x[:T, :HQ], k=x[:T, HQ:]), True)
+    for bad in (dict(k=pool_k), dict(v=pool_k), dict(q=pool_q), dict(q_out=pool_q), dict(q_out=x[1:, :HQ], k=x[:T, HQ:]),
+                dict(k=ok["k"].float()), dict(v=ok["v"][:3]), dict(q_out=ok["q"]), dict(cu_seqlens=None), dict(q=None),
+                dict(cu_seqlens=full.page_table.view(-1)[:B + 1]), dict(q_out=ok["q_out"].transpose(0, 1)), dict(k="k"), dict(q_out=None)):
+        agree(full._quick_append, append, dict(ok, **bad), False)
+    ok = {n: t for n, t in _attend().items() if n != "storage"}
+    agree(full._quick_attend, attend, ok, True)
+    assert full._quick_attend(**ok)[2:5] == tuple(ok[n].data_ptr() for n in ("q", "out", "lse"))
+    for bad in (dict(out=pool_q), dict(out=ok["q"]), dict(lse=ok["lse"].t()), dict(lse=torch.zeros(T, HQ, dtype=BF)),
+                dict(lse=full.k_pages.view(torch.float32).view(-1)[:T * HQ].view(T, HQ)), dict(q=ok["q"].float()),
+                dict(out=ok["out"][..., :32]), dict(cu_seqlens=ok["cu_seqlens"].long()), dict(q=None)):
+        agree(full._quick_attend, attend, dict(ok, **bad), False)
+    ok = {n: t for n, t in _rotary().items() if n != "inv_freq"}
+    agree(rot._quick, rotate, ok, True)
+    for bad in (dict(q_out=ok["q"]), dict(k_out=x[:T, :HKV], q_out=x[:T, :HQ]), dict(positions=ok["q_out"].view(I32).view(-1)[:T]),
+                dict(positions=ok["positions"].long()), dict(q=ok["q"][:0]), dict(k=ok["k"][1:]), dict(k_out=None)):
+        agree(rot._quick, rotate, dict(ok, **bad), False)
+
+
+def test_strides_are_those_of_the_call():
+    full = P.DMCFull(CFG, max_tokens=T, max_chunk=2, inv_freq=torch.zeros(R // 2), device="cpu")
+    a = {n: t for n, t in _attend().items() if n != "storage"}
+    wide = torch.zeros(T, HQ, 2 * D, dtype=BF)
+    first = full._quick_attend(**a)[-1]
+    assert list(first) == [HQ * D, D, HQ * D, D] and full._quick_attend(**a)[-1] is first
+    assert list(full._quick_attend(**dict(a, q=wide[..., :D]))[-1]) == [2 * HQ * D, 2 * D, HQ * D, D]
+    assert list(first) == [HQ * D, D, HQ * D, D]   # (the earlier call's array stays as it was)
