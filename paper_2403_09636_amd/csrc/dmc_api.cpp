@@ -1467,8 +1467,9 @@ dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int6
   p.tile_cols = L.tile_cols;
   const int G = cfg->num_q_heads / cfg->num_kv_heads;
   p.tile_tokens = std::max(1, L.tile_cols / G);
-  const int64_t tiles = int64_t(total) * G / L.tile_cols + cfg->batch;
-  p.one_launch = dmc::full_one_launch(tiles, cfg->num_kv_heads, p.capacity);
+  const int64_t tiles = cu ? int64_t(total) * G / L.tile_cols + cfg->batch
+                           : int64_t(cfg->batch) * ((G + L.tile_cols - 1) / L.tile_cols);
+  p.one_launch = dmc::full_one_launch(L.tile_cols, tiles, cfg->num_kv_heads, p.capacity);
   p.group_shift = ilog2(G) - 1;
   p.group_magic = G > 1 ? static_cast<uint32_t>(((uint64_t(1) << (31 + ilog2(G))) + G - 1) / G) : 0;
   int dev = 0;

@@ -73,6 +73,13 @@ __device__ __forceinline__ int row_of_token(const int32_t *cu, int rows, int tot
 // ---------------------------------------------------------------------------
 constexpr int kRotTokens = 4;
 
+// A store that cannot be to LDS (from pointers of several origins the compiler makes
+// flat stores, which count as LDS accesses too).
+__device__ __forceinline__ void store_global(char *p, const uint4 &v) {
+  typedef __attribute__((address_space(1))) u32x4 gv;
+  *reinterpret_cast<gv *>(reinterpret_cast<uintptr_t>(p)) = __builtin_bit_cast(u32x4, v);
+}
+
 template <int ES, int D, bool PAGED>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int shift) {
   constexpr int N = 16 / ES, UPR = D * ES / 32;   // elements of a vector, units of a row
@@ -209,8 +216,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
         x[j][0] = V16<ES>::pack(a);
         x[j][1] = V16<ES>::pack(b);
       }
-      st16(dst[j], x[j][0]);
-      st16(dst[j] + gap[j], x[j][1]);
+      store_global(dst[j], x[j][0]);
+      store_global(dst[j] + gap[j], x[j][1]);
     }
   }
 }
@@ -282,7 +289,7 @@ __device__ __forceinline__ int table_entry(const int32_t *table, int i) {
 }
 
 // Fewest keys of a piece, and the most per workgroup for which units are cut equally.
-constexpr int kNarrowRange = 256, kWideRange = 1024, kEqualKeys = 1024;
+constexpr int kNarrowRange = 128, kWideRange = 512, kEqualKeys = 1024;
 
 // a / G for a < 2^31, by a multiplication (G = 1: group_shift < 0).
 __device__ __forceinline__ int div_group(const FullParams &p, int a) {
@@ -348,7 +355,7 @@ struct Space {
   int64_t *prefix;
   RowPlace *places;
   int64_t all, per, pos, hi;   // pos, hi: what is left of this workgroup's range
-  int G, range, b;             // b: where the last piece was found
+  int G, range;
   bool few, equal;             // equal: equal pieces of every unit
 
   __device__ __forceinline__ Tiles<TRI> tiles(int n, int m) const { return Tiles<TRI>(n, m, G, p.tile_cols, p.tile_tokens); }
@@ -357,7 +364,7 @@ struct Space {
   // Sums up the rows; writes the rows of dropped tokens, and in the first workgroup
   // the flags of what it finds wrong.
   __device__ __forceinline__ Space(const FullParams &p_, int64_t *prefix_, SpaceLds &lds)
-      : p(p_), prefix(prefix_), G(p_.hq / p_.hkv), range(range_of_block(gridDim.x)), b(0), few(p_.rows <= 64), equal(false) {
+      : p(p_), prefix(prefix_), G(p_.hq / p_.hkv), range(range_of_block(gridDim.x)), few(p_.rows <= 64), equal(false) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int grid = gridDim.x;
     places = lds.rows[wave];
@@ -438,71 +445,98 @@ struct Space {
     }
     all = uniform(all);
     per = equal ? 1 : max((all + grid - 1) / grid, int64_t(LEAST));
-    pos = range * per;
-    hi = min(pos + per, all);
+    pos = boundary(range);
+    hi = boundary(range + 1);
+  }
+
+  // A range's end that lies within kSnap keys of a unit's end moves there: a cut unit
+  // costs two records and their join, as much as some hundred keys.
+  static constexpr int kSnap = TRI ? 512 : 128;
+  __device__ __forceinline__ int64_t boundary(int i) {
+    const int64_t v = min(i * per, all);
+    if (equal || v == 0 || v == all) return v;
+    const Unit u = unit_at(v);
+    return v - u.begin <= kSnap ? u.begin : u.begin + u.keys - v <= kSnap ? u.begin + u.keys : v;
+  }
+
+  // The unit that holds key (or range) v of the space: tile t of a row and head.
+  struct Unit {
+    int b, n, start, m, pieces, h, t, keys, index;   // index: piece (equal pieces)
+    int64_t begin;                                   // its first key (not of equal pieces)
+  };
+  __device__ __forceinline__ Unit unit_at(int64_t v) {
+    Unit u;
+    int64_t off;
+    u.pieces = 0;
+    if (few) {
+      const RowPlace mine = places[threadIdx.x & 63];
+      u.b = 63 - __clzll(static_cast<long long>(__ballot(mine.m > 0 && mine.before <= v)));
+      const RowPlace r = places[u.b];
+      u.n = uniform(r.n);
+      u.start = uniform(r.start);
+      u.m = uniform(r.m);
+      u.pieces = uniform(r.pieces);
+      off = v - uniform(r.before);
+    } else {
+      int lo = 0, end = p.rows;   // prefix[lo] <= v < prefix[end]
+      while (end - lo > 1) {
+        const int mid = (lo + end) >> 1;
+        if (prefix[mid] <= v) lo = mid;
+        else end = mid;
+      }
+      u.b = uniform(lo);
+      const FullRow r = load(u.b);
+      u.n = uniform(r.n);
+      u.start = uniform(r.start);
+      u.m = min(uniform(r.m), p.max_chunk);
+      off = v - uniform(prefix[u.b]);
+    }
+    const Tiles<TRI> ts = tiles(u.n, u.m);
+    if (equal) {
+      const int o = static_cast<int>(off), unit = small_div(o, u.pieces);
+      u.index = o - unit * u.pieces;
+      u.h = small_div(unit, ts.count);
+      u.t = unit - u.h * ts.count;
+    } else {
+      const int64_t per_head = ts.all();
+      u.h = uniform(static_cast<int>(off / per_head));
+      const int64_t in_head = off - u.h * per_head;
+      u.t = uniform(ts.at(in_head));
+      u.begin = v - in_head + ts.before(u.t);
+    }
+    u.keys = ts.keys(u.t);
+    return u;
   }
 
   // The next piece of the range; pos moves behind it.
   __device__ __forceinline__ Piece next() {
+    const Unit u = unit_at(pos);
     Piece x;
-    int m, pieces = 0;
-    int64_t off;
-    if (few) {
-      const RowPlace mine = places[threadIdx.x & 63];
-      x.b = 63 - __clzll(static_cast<long long>(__ballot(mine.m > 0 && mine.before <= pos)));
-      const RowPlace r = places[x.b];
-      x.n = uniform(r.n);
-      x.start = uniform(r.start);
-      m = uniform(r.m);
-      pieces = uniform(r.pieces);
-      off = pos - uniform(r.before);
-    } else {
-      if (prefix[b + 1] <= pos) {   // prefix[lo] <= pos < prefix[end]
-        int lo = b, end = p.rows;
-        while (end - lo > 1) {
-          const int mid = (lo + end) >> 1;
-          if (prefix[mid] <= pos) lo = mid;
-          else end = mid;
-        }
-        b = uniform(lo);
-      }
-      x.b = b;
-      const FullRow r = load(b);
-      x.n = uniform(r.n);
-      x.start = uniform(r.start);
-      m = min(uniform(r.m), p.max_chunk);
-      off = pos - uniform(prefix[b]);
-    }
-    const Tiles<TRI> ts = tiles(x.n, m);
-    int t;
+    x.b = u.b;
+    x.n = u.n;
+    x.start = u.start;
+    x.h = u.h;
+    x.keys = u.keys;
     if (equal) {
-      const int o = uniform(static_cast<int>(off)), unit = small_div(o, pieces);
-      x.h = small_div(unit, ts.count);
-      t = unit - x.h * ts.count;
-      x.keys = ts.keys(t);
-      x.pieces = pieces;
-      x.index = o - unit * pieces;
+      x.pieces = u.pieces;
+      x.index = u.index;
       x.first = range - x.index;
-      const int size = (small_div(x.keys + pieces - 1, pieces) + 31) & ~31;
+      const int size = (small_div(x.keys + x.pieces - 1, x.pieces) + 31) & ~31;
       x.k0 = min(x.index * size, x.keys);
       x.k1 = min(x.k0 + size, x.keys);
       pos = hi;
     } else {
-      const int64_t per_head = ts.all();
-      x.h = uniform(static_cast<int>(off / per_head));
-      const int64_t in_head = off - x.h * per_head;
-      t = uniform(ts.at(in_head));
-      x.keys = ts.keys(t);
-      x.k0 = uniform(static_cast<int>(in_head - ts.before(t)));
-      x.k1 = uniform(static_cast<int>(min(int64_t(x.keys), x.k0 + (hi - pos))));
-      const int64_t begin = pos - x.k0;   // the unit's first key
-      x.first = uniform(static_cast<int>(begin / per));
+      x.k0 = static_cast<int>(pos - u.begin);
+      x.k1 = static_cast<int>(min(int64_t(x.keys), x.k0 + (hi - pos)));
+      // ranges that end within the unit: at i per in (begin + kSnap, begin + keys - kSnap)
+      x.first = static_cast<int>((u.begin + min(kSnap, x.keys - 1)) / per);
+      x.pieces = max(static_cast<int>((u.begin + x.keys - kSnap - 1) / per) - x.first, 0) + 1;
       x.index = range - x.first;
-      x.pieces = uniform(static_cast<int>((begin + x.keys - 1) / per)) - x.first + 1;
       pos += x.k1 - x.k0;
     }
-    x.col0 = ts.first_col(t, G);
-    x.cols = min(TRI ? ts.step * G : ts.step, m * G - x.col0);
+    const Tiles<TRI> ts = tiles(u.n, u.m);
+    x.col0 = ts.first_col(u.t, G);
+    x.cols = min(TRI ? ts.step * G : ts.step, u.m * G - x.col0);
     return x;
   }
 };
@@ -721,6 +755,21 @@ __global__ __launch_bounds__(kThreads) void full_join_kernel(FullParams p, int s
 // No variant spills registers (fp32 at d = 128 takes blocks of 16 keys and 16
 // columns for that).
 // ---------------------------------------------------------------------------
+// Loads through pointers of the global address space: from generic ones the compiler
+// makes flat loads, which count as LDS accesses too, so that every wait for one of
+// those (or for a scalar load) waits for all keys and values in flight.
+typedef const __attribute__((address_space(1))) char gchar;
+template <typename V, bool STREAM>
+__device__ __forceinline__ V load_global(gchar *p) {
+  typedef const __attribute__((address_space(1))) V gv;
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<gv *>(p));
+  else return *reinterpret_cast<gv *>(p);
+}
+// A wave-uniform address (SGPRs).
+__device__ __forceinline__ gchar *uniform_global(const char *p) {
+  return reinterpret_cast<gchar *>(reinterpret_cast<uintptr_t>(uniform_ptr(p)));
+}
+
 template <int ES, int D>
 struct Narrow;
 
@@ -735,13 +784,13 @@ struct Narrow<2, D> {
   static constexpr int kKeyStep = 64;             // bytes between a lane's slices of a row
   __device__ static __forceinline__ int key_offset(int g) { return g * 16; }
   template <bool STREAM>
-  __device__ static __forceinline__ void load_row(uint4 (&x)[KC], const char *row) {
+  __device__ static __forceinline__ void load_row(uint4 (&x)[KC], gchar *row) {
 #pragma unroll
-    for (int c = 0; c < KC; ++c) x[c] = STREAM ? ld16_stream(row + c * kKeyStep) : ld16(row + c * kKeyStep);
+    for (int c = 0; c < KC; ++c) x[c] = __builtin_bit_cast(uint4, load_global<u32x4, STREAM>(row + c * kKeyStep));
   }
   template <bool STREAM>
-  __device__ static __forceinline__ vrow_t load_value(const char *p) {
-    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const vrow_t *>(p)) : *reinterpret_cast<const vrow_t *>(p);
+  __device__ static __forceinline__ vrow_t load_value(gchar *p) {
+    return load_global<vrow_t, STREAM>(p);
   }
   __device__ static __forceinline__ f32x4_t scores(const uint4 (&k)[KC], const Query &q) {
     f32x4_t s = f32x4_t{};
@@ -813,20 +862,16 @@ struct Narrow<4, D> {
   static constexpr int kKeyStep = 64;
   __device__ static __forceinline__ int key_offset(int g) { return g * 16; }
   template <bool STREAM>
-  __device__ static __forceinline__ f32x4_t load4f(const char *p) {
-    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(p)) : *reinterpret_cast<const f32x4_t *>(p);
-  }
-  template <bool STREAM>
-  __device__ static __forceinline__ void load_row(f32x4_t (&x)[KC], const char *row) {
+  __device__ static __forceinline__ void load_row(f32x4_t (&x)[KC], gchar *row) {
 #pragma unroll
-    for (int c = 0; c < KC; ++c) x[c] = load4f<STREAM>(row + c * kKeyStep);
+    for (int c = 0; c < KC; ++c) x[c] = load_global<f32x4_t, STREAM>(row + c * kKeyStep);
   }
   template <bool STREAM>
-  __device__ static __forceinline__ vrow_t load_value(const char *p) {
+  __device__ static __forceinline__ vrow_t load_value(gchar *p) {
     vrow_t v;
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) {
-      const f32x4_t x = load4f<STREAM>(p + 16 * i);
+      const f32x4_t x = load_global<f32x4_t, STREAM>(p + 16 * i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[4 * i + e] = x[e];
     }
@@ -883,6 +928,9 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
   constexpr int E = X::E, U = X::U, KEYS = 16 * U, RB = D * ES, JS = D + 4, STEP = SPLIT_KEYS ? kWaves : 1;
   constexpr int COLS = 16 * NT * (SPLIT_KEYS ? 1 : kWaves);
   constexpr bool TRI = !SPLIT_KEYS;
+  // (keys are read in 64-byte parts of a line: with 32 columns plain loads are 4 %
+  // faster, with 16 and long rows 4 % slower)
+  constexpr bool STREAM_KEYS = SPLIT_KEYS && NT == 1;
   extern __shared__ int64_t prefix[];
   __shared__ SpaceLds space_lds;
   __shared__ Cuts cuts;
@@ -940,7 +988,12 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
     const int mask = (1 << p.log2p) - 1;
     // First byte of kv head h's rows in a page.
     auto page_at = [&](const char *pool, int page) {
-      return pool + ((int64_t(checked_page(p, page)) * p.hkv + x.h) << p.log2p) * RB;
+      return reinterpret_cast<gchar *>(reinterpret_cast<uintptr_t>(pool)) +
+             ((int64_t(checked_page(p, page)) * p.hkv + x.h) << p.log2p) * RB;
+    };
+    auto block_at = [&](const char *pool, int page, int kb) {   // of a block that lies in one page
+      return uniform_global(pool + ((int64_t(checked_page(p, page)) * p.hkv + x.h) << p.log2p) * RB +
+                            int64_t((kb * KEYS) & mask) * RB);
     };
     typename X::Keys kx;
     typename X::Values vx;
@@ -948,28 +1001,28 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
       if constexpr (SMALL) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          X::template load_row<SPLIT_KEYS>(kx.x[u], page_at(p.kp, pg.x[u]) +
+          X::template load_row<STREAM_KEYS>(kx.x[u], page_at(p.kp, pg.x[u]) +
               (min(kb * KEYS + u * 16 + c16, keys - 1) & mask) * RB + X::key_offset(g4));
       } else {
-        const char *at = uniform_ptr(page_at(p.kp, pg.x[0]) + int64_t((kb * KEYS) & mask) * RB);
+        gchar *at = block_at(p.kp, pg.x[0], kb);
         const uint32_t last = keys - 1 - kb * KEYS;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          X::template load_row<SPLIT_KEYS>(kx.x[u], at + (min(uint32_t(u * 16 + c16), last) * RB + X::key_offset(g4)));
+          X::template load_row<STREAM_KEYS>(kx.x[u], at + (min(uint32_t(u * 16 + c16), last) * RB + X::key_offset(g4)));
       }
     };
     auto load_values = [&](int kb, const Pages &pg) {
       if constexpr (SMALL) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const char *at = page_at(p.vp, pg.x[U + u]) + c16 * (E * ES);
+          gchar *at = page_at(p.vp, pg.x[U + u]) + c16 * (E * ES);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             vx.x[u * 4 + i] = X::template load_value<SPLIT_KEYS>(
                 at + (min(kb * KEYS + u * 16 + g4 * 4 + i, keys - 1) & mask) * RB);
         }
       } else {
-        const char *at = uniform_ptr(page_at(p.vp, pg.x[0]) + int64_t((kb * KEYS) & mask) * RB);
+        gchar *at = block_at(p.vp, pg.x[0], kb);
         const uint32_t last = keys - 1 - kb * KEYS;
 #pragma unroll
         for (int i = 0; i < 4 * U; ++i)
@@ -990,9 +1043,10 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
     }
     int kb = (x.k0 + KEYS - 1) / KEYS + (SPLIT_KEYS ? wave : 0);
     if (kb < kb1) {
-      Pages cur = pages_of(kb), next = pages_of(min(kb + STEP, kb1 - 1));
-      load_keys(kb, cur);
-      load_values(kb, cur);
+      Pages next = pages_of(kb);
+      load_keys(kb, next);
+      load_values(kb, next);
+      next = pages_of(min(kb + STEP, kb1 - 1));
       for (; kb < kb1; kb += STEP) {
         float pr[NT][4 * U];
 #pragma unroll
@@ -1004,7 +1058,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
             for (int r = 0; r < 4; ++r) pr[t][4 * u + r] = s[r];
           }
         const bool more = kb + STEP < kb1;
-        cur = next;
+        const Pages cur = next;
         if (more) {
           next = pages_of(min(kb + 2 * STEP, kb1 - 1));
           load_keys(kb + STEP, cur);
@@ -1044,7 +1098,8 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
           for (int i = 0; i < KEYS; ++i) {
             const int key = kb * KEYS + i;
             if (key >= keys) break;
-            const char *row = page_at(p.vp, table_entry(table, key >> p.log2p)) + int64_t(key & mask) * RB;
+            const char *row = p.vp + (((int64_t(checked_page(p, table_entry(table, key >> p.log2p))) * p.hkv + x.h) << p.log2p) +
+                                      (key & mask)) * RB;
 #pragma unroll
             for (int rj = 0; rj < 4 * E; ++rj) {
               const float f = load_elem<ES>(row, g4 * 4 * E + rj);
@@ -1388,10 +1443,13 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
         for (int i = 0; i < NTL; ++i)
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
+            // (wide tiles always take two launches: plain stores)
+            typedef __attribute__((address_space(1))) uint64_t gpair;
             const char *row = uniform_ptr(reinterpret_cast<const char *>(rec) + (16 * i + 4 * (j >> 2) + (j & 3) / 2) * kWideCols * 8);
-            put2(p, reinterpret_cast<float *>(const_cast<char *>(row) + at), acc[i][j], acc[i][j + 1]);
+            *reinterpret_cast<gpair *>(reinterpret_cast<uintptr_t>(row) + at) =
+                (uint64_t(__float_as_uint(acc[i][j + 1])) << 32) | __float_as_uint(acc[i][j]);
           }
-        if (hb == 0) put2(p, rec + kWideCols * D + 2 * c, m, ls);
+        if (hb == 0) *reinterpret_cast<float2 *>(rec + kWideCols * D + 2 * c) = make_float2(m, ls);
       }
     }
     if (!whole && tid == 0) cuts.piece[cuts.n++] = x;

@@ -437,8 +437,8 @@ constexpr inline int full_tile_cols(int elem_bytes, int64_t max_chunk, int group
 }
 // Whether records are joined within the attention's launch: where the rows' capacity
 // is small (tiles: column tiles of all rows).  The capacity decides, not the lengths.
-constexpr inline bool full_one_launch(int64_t tiles, int hkv, int64_t capacity) {
-  return tiles * hkv * capacity <= int64_t(1) << 19;
+constexpr inline bool full_one_launch(int tile_cols, int64_t tiles, int hkv, int64_t capacity) {
+  return tile_cols <= 32 && tiles * hkv * capacity <= int64_t(1) << 18;
 }
 hipError_t launch_full_attend(int elem_bytes, int head_dim, const FullParams &p, hipStream_t s);
 
