@@ -1358,6 +1358,9 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
 #pragma unroll
           for (int i = 0; i < NTL; ++i) acc[i] *= f;
         }
+        // This wave's matrix work goes before the other wave's vector work (4 rows, 64/8
+        // heads, 512 tokens on 12000: 929 -> 877 us).
+        __builtin_amdgcn_s_setprio(1);
         f32x16_t sc = f32x16_t{};
         float ev[16];
 #pragma unroll
@@ -1374,6 +1377,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
           __builtin_amdgcn_sched_barrier(0);
         }
         scn = sc;
+        __builtin_amdgcn_s_setprio(2);
         // P enters the value product rounded to bf16 (off by at most 2^-8 of a
         // probability, at random); its sum is taken in fp32 before that.
         uint4 pb[2];
@@ -1396,6 +1400,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
         for (int i = 0; i < NTL; ++i)
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk) acc[i] = mfma_32x32x16(va[i][kk], pb[kk], acc[i]);
+        __builtin_amdgcn_s_setprio(0);
       };
       // Whole rounds of four steps (a step past the last block only keeps the
       // barriers and transfer counts in step).
