@@ -435,3 +435,89 @@ def test_many_rows(torch_cuda):
     c = Case(P, held[:3000], lens, hq=2, hkv=1, d=64, page=16)
     out, lse = c.attend()
     c.check(out.cpu(), lse.cpu(), rows=set(range(0, 3000, 37)) | {76, 77, 78, 2999})
+
+
+def test_many_rows_of_wide_chunks(torch_cuda):
+    """More than 64 rows (their sums in LDS beside the wide tiles' ring; fp32 tiles of 64 columns), long chunks among
+    short and empty ones."""
+    import paper_2403_09636_amd as P
+    g = torch.Generator().manual_seed(16)
+    for dtype in ("bf16", "fp32"):
+        held = torch.randint(-2, 90, (300,), generator=g).tolist()
+        lens = torch.randint(0, 9, (300,), generator=g).tolist()
+        held[11], lens[11], held[298], lens[298], held[150], lens[150] = 700, 150, 0, 90, 60, 40
+        c = Case(P, held, lens, hq=4, hkv=1, d=64, page=16, dtype=dtype, tail=1)
+        out, lse = c.attend()
+        c.check(out.cpu(), lse.cpu(), rows=set(range(0, 300, 13)) | {10, 11, 12, 150, 298, 299})
+        c.full.check()
+
+
+def test_counters_are_left_at_zero(torch_cuda):
+    import paper_2403_09636_amd as P
+    for held, lens, hq, hkv in (([900], [1], 16, 4), ([140001], [1], 8, 1), ([3000, 5, 700], [2, 1, 3], 8, 2)):
+        c = Case(P, held, lens, hq=hq, hkv=hkv, d=64, packed=len(held) > 1)
+        for _ in range(3):
+            c.attend()
+        at = -c.full.workspace.data_ptr() % 256
+        assert not c.full.workspace[at:at + P.binding.DMC_FULL_COUNTER_BYTES].any()
+
+
+def test_calls_without_lse_and_flags(torch_cuda):
+    import ctypes
+    import paper_2403_09636_amd as P
+    lib = P.binding.lib
+    c = Case(P, [100, -1, 33, 2000], [1, 1, 1, 1], hq=8, hkv=2, d=128, packed=False)
+    want, _ = c.attend()
+    q, out, f = c.q.cuda(), torch.zeros_like(want), c.full
+    st = (ctypes.c_int64 * 2)(8 * 128, 128)
+    ptr = [ctypes.c_void_p(t.data_ptr()) for t in (q, f.lengths, f.page_table, f.k_pages, f.v_pages, out)]
+    assert lib.dmc_full_attend(ctypes.byref(f.cfg), ptr[0], st, None, 4, 1, *ptr[1:], st, None, None, f._ws, f._ws_bytes,
+                               torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out, want)
+    kv = torch.randn(4, 2, 128, device="cuda").bfloat16()
+    st = (ctypes.c_int64 * 2)(2 * 128, 128)
+    p = ctypes.c_void_p(kv.data_ptr())
+    assert lib.dmc_full_append(ctypes.byref(f.cfg), p, st, p, st, None, None, None, None, 4, *ptr[1:3], *ptr[3:5], None, None,
+                               None, torch.cuda.current_stream().cuda_stream) == 0
+    for b, n in ((0, 100), (2, 33), (3, 2000)):
+        at = int(c.table[b, n // 32])
+        assert torch.equal(f.k_pages[0, at, :, n % 32], kv[b]) and torch.equal(f.v_pages[0, at, :, n % 32], kv[b])
+
+
+@pytest.mark.parametrize("chunk,hq", [(5, 8), (40, 8)])
+def test_captured_chunks_at_other_lengths(torch_cuda, chunk, hq):
+    """Drafts (two launches) and pieces (wide tiles), captured once; replayed over caches of other lengths, pages and
+    boundaries, and compared with eager calls."""
+    import paper_2403_09636_amd as P
+    B, hkv, d, page, width = 6, 2, 64, 32, 400
+    g = torch.Generator().manual_seed(chunk)
+    cfg = P.make_full_config(B, hq, hkv, d, page_size=page, max_pages=width, num_pages=600)
+    a, b = (P.DMCFull(cfg, max_tokens=B * chunk, max_chunk=chunk) for _ in range(2))
+    for x in (a, b):
+        for pool, s in ((x.k_pages, 1), (x.v_pages, 2)):
+            pool.copy_(torch.randn(pool.shape, generator=torch.Generator().manual_seed(s)).bfloat16())
+    q, out, cu = torch.empty(B * chunk, hq, d, device="cuda").bfloat16(), torch.zeros(B * chunk, hq, d, device="cuda").bfloat16(), \
+        torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(B * chunk, hq, device="cuda")
+    a.attend(0, q, cu_seqlens=cu, out=out, lse=lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.attend(0, q, cu_seqlens=cu, out=out, lse=lse)
+    for i in range(6):
+        lens = torch.randint(0, chunk + 1, (B,), generator=g)
+        held = torch.randint(-1, (60, 500, 12000)[i % 3], (B,), generator=g)
+        table = torch.randint(0, 600, (B, width), generator=g)   # (shared pages are only read here)
+        cu.copy_(torch.cat([torch.zeros(1, dtype=torch.long), lens.cumsum(0)]).int())
+        q.copy_(torch.randn(q.shape, generator=g).bfloat16())
+        for x in (a, b):
+            x.lengths.copy_(held.int())
+            x.page_table.copy_(table.int())
+        out.fill_(3)
+        lse.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        o, z = torch.full_like(out, 3), torch.full_like(lse, 3)
+        b.attend(0, q, cu_seqlens=cu, out=o, lse=z)
+        assert torch.equal(out, o) and torch.equal(lse, z), f"replay {i}"
+    a.check()
