@@ -514,7 +514,7 @@ class _RowsCall:
         import torch
         self.Tensor, self.dtype, self.device, self.d, self.es = torch.Tensor, dtype, device, d, es
         self.f32, self.i32 = torch.float32, torch.int32
-        self.values, self.array = None, None
+        self.kept = None, None
 
     def take(self, t, shape):
         """(address, token stride, head stride, end) of a tensor of this shape [T, heads, d], or None."""
@@ -533,9 +533,10 @@ class _RowsCall:
         return None
 
     def strides(self, *values):
-        if values != self.values:
-            self.values, self.array = values, (c_int64 * len(values))(*values)
-        return self.array
+        kept = self.kept   # (one attribute: threads that share the object get their own call's)
+        if values != kept[0]:
+            self.kept = kept = values, (c_int64 * len(values))(*values)
+        return kept[1]
 
 
 def check_chunk_args(cfg, device, q, k, v, cu_seqlens, out=None, accepted=None, slot_index=None):

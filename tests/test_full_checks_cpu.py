@@ -319,3 +319,18 @@ def test_strides_are_those_of_the_call():
     assert list(first) == [HQ * D, D, HQ * D, D] and full._quick_attend(**a)[-1] is first
     assert list(full._quick_attend(**dict(a, q=wide[..., :D]))[-1]) == [2 * HQ * D, 2 * D, HQ * D, D]
     assert list(first) == [HQ * D, D, HQ * D, D]   # (the earlier call's array stays as it was)
+
+
+def test_strides_of_two_threads_do_not_mix():
+    """One object used from two threads with tensors of other strides: each call gets its own, also if the other
+    thread's call comes between the comparison with the kept strides and the use of their array."""
+    call = Bd._RowsCall(BF, DEV, D, 2)
+
+    class Between(int):
+        def __eq__(self, other):
+            call.strides(72, 128)
+            return int(self) == int(other)
+        __hash__ = int.__hash__
+    assert tuple(call.strides(64, 128)) == (64, 128)
+    assert tuple(call.strides(Between(64), 128)) == (64, 128)
+    assert tuple(call.strides(64, 128)) == (64, 128)
