@@ -1111,7 +1111,10 @@ class DMCFull:
     - page_table, int32 [batch, max_pages]: the pages of every row, shared by the layers;
     - lengths, int32 [batch]: the tokens that every row holds before a call (negative: row not in use); the
       program adds the new ones once all layers have appended and attended;
-    - k_pages, v_pages [num_layers, num_pages, Hkv, page_size, d], to copy whole pages in or out."""
+    - k_pages, v_pages [num_layers, num_pages, Hkv, page_size, d], to copy whole pages in or out.
+
+    Calls of attend share the object's workspace: those that may run at the same time, on two streams, need objects
+    of their own."""
 
     def __init__(self, cfg: FullConfig, max_tokens=None, max_chunk=1, inv_freq=None, num_layers=1, device="cuda"):
         import torch

@@ -1269,11 +1269,14 @@ static dmc_status validate_full(const dmc_full_config *c) {
   return DMC_OK;
 }
 
+// (a launch has less than 2^32 threads: 64 for each token)
+constexpr int32_t kMaxRotatedTokens = 1 << 24;
+
 // The rows and tokens of a call on a full cache.
 static dmc_status check_full_rows(const dmc_full_config &c, const int32_t *cu, int32_t total, const int32_t *lengths,
                                   const int32_t *table, const void *k_pages, const void *v_pages) {
   if (total < 0) return fail(DMC_ERR_INVALID_ARG, "total_tokens must be >= 0");
-  if (int64_t(total) * (c.num_q_heads + 2 * c.num_kv_heads) * c.head_dim > (int64_t(1) << 36) || total > (1 << 24))
+  if (int64_t(total) * (c.num_q_heads + 2 * c.num_kv_heads) * c.head_dim > (int64_t(1) << 36) || total > kMaxRotatedTokens)
     return fail(DMC_ERR_UNSUPPORTED, "too many tokens for one call");
   if (!cu && total != 0 && total != c.batch)
     return fail(DMC_ERR_INVALID_ARG, "%d tokens without cu_seqlens, one for each of %d rows expected", total, c.batch);
@@ -1305,6 +1308,7 @@ dmc_status dmc_rotate(const dmc_rotary_config *cfg, const void *q, const int64_t
                                  cfg->rotary_pairs);
   if (st == DMC_OK) st = check_packed_counts(0, total);
   if (st != DMC_OK) return st;
+  if (total > kMaxRotatedTokens) return fail(DMC_ERR_UNSUPPORTED, "more than %d tokens in one call", kMaxRotatedTokens);
   if (total == 0) return DMC_OK;
   const int es = cfg->dtype == DMC_FP32 ? 4 : 2;
   for (const Packed &t : {Packed{"q", q, q_strides, cfg->num_q_heads, false, false},

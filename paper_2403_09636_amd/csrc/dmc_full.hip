@@ -583,6 +583,7 @@ __device__ __forceinline__ void put2(const FullParams &q, float *p, float a, flo
 // as weights), then the accumulators, two columns' pairs (16 bytes) AT_ONCE times to a
 // thread, all of a step's reads in flight together.  Columns begin (even) .. end - 1.
 constexpr int kJoinPairs = 1024;
+static_assert(kJoinPairs >= 2 * kFullPlaces, "a step takes two columns of every record");
 template <int ES, int D, int AT_ONCE>
 __device__ __forceinline__ void join_records(const FullParams &p, const Piece &x, int begin, int end, int from, int step,
                                              int count, bool last, float2 *w) {

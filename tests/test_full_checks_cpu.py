@@ -334,3 +334,9 @@ def test_strides_of_two_threads_do_not_mix():
     assert tuple(call.strides(64, 128)) == (64, 128)
     assert tuple(call.strides(Between(64), 128)) == (64, 128)
     assert tuple(call.strides(64, 128)) == (64, 128)
+
+
+def test_more_tokens_than_a_launch_takes():
+    """2^26 tokens in groups of four, 256 threads each, would be 2^32 threads."""
+    for total in ((1 << 24) + 1, 1 << 26):
+        assert _c_rotate(total=total) == 2 and "16777216" in Bd.last_error()

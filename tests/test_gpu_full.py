@@ -521,3 +521,15 @@ def test_captured_chunks_at_other_lengths(torch_cuda, chunk, hq):
         b.attend(0, q, cu_seqlens=cu, out=o, lse=z)
         assert torch.equal(out, o) and torch.equal(lse, z), f"replay {i}"
     a.check()
+
+
+def test_the_largest_batch_with_wide_chunks(torch_cuda):
+    """4096 rows: their sums (32 KB) beside the ring of the wide tiles (64 KB) and the workgroup's places."""
+    import paper_2403_09636_amd as P
+    held, lens = [-1] * 4096, [0] * 4096
+    for b, n, m in ((0, 40, 70), (1, 0, 0), (2000, 300, 33), (4094, 7, 1), (4095, 600, 140)):
+        held[b], lens[b] = n, m
+    c = Case(P, held, lens, hq=4, hkv=1, d=128, page=32, tail=1)
+    out, lse = c.attend()
+    c.check(out.cpu(), lse.cpu(), rows={0, 1, 2000, 4094, 4095})
+    c.full.check()
