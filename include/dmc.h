@@ -479,7 +479,7 @@ dmc_status dmc_causal_backward(const dmc_causal_config *cfg, const void *q_dev,
  *     may be broadcast (strides of 0); the rows of an output may not overlap each
  *     other, nor an output another tensor, but q_out may be q itself and k_out k
  *     itself (same pointer and strides).
- *   positions_dev: int32 [total_tokens], any value; up to 2^24 tokens a call.
+ *   positions_dev: int32 [total_tokens], any value; up to 2^23 tokens a call.
  *   inv_freq_dev: fp32 [rotary_dim / 2]; not read (may be NULL) if rotary_dim is 0.
  * The call only enqueues a kernel, so it can be captured in a HIP graph.
  * ------------------------------------------------------------------------- */
@@ -526,7 +526,7 @@ dmc_status dmc_rotate(const dmc_rotary_config *cfg, const void *q_dev, const int
  *   of the token and head axes (d contiguous), 16-byte aligned, strides
  *   non-negative multiples of 8.  Inputs may be broadcast (strides of 0); the rows
  *   of an output may not overlap each other, nor an output another tensor.
- *   A call takes up to 2^24 tokens.
+ *   A call takes up to 2^23 tokens.
  *   flags_dev: optional int32 word in device memory, into which the kernels OR
  *     what they find (dmc_full_flag); the caller clears and reads it.
  *     ROW_FULL: a token's position is past max_pages * page_size - 1: it is

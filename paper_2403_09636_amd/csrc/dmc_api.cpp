@@ -1269,8 +1269,8 @@ static dmc_status validate_full(const dmc_full_config *c) {
   return DMC_OK;
 }
 
-// (a launch has less than 2^32 threads: 64 for each token)
-constexpr int32_t kMaxRotatedTokens = 1 << 24;
+// (a launch has less than 2^32 threads: 256 for each token)
+constexpr int32_t kMaxRotatedTokens = 1 << 23;
 
 // The rows and tokens of a call on a full cache.
 static dmc_status check_full_rows(const dmc_full_config &c, const int32_t *cu, int32_t total, const int32_t *lengths,
@@ -1401,20 +1401,20 @@ static dmc_status check_full_sizes(const dmc_full_config *c, int32_t total, int3
 
 static_assert(DMC_FULL_COUNTER_BYTES >= dmc::kFullPlaces * 3 * sizeof(int32_t), "counters");
 
+static int64_t full_record_floats(int tile_cols, int head_dim) { return int64_t(tile_cols) * (head_dim + 2); }
+
 struct FullLayout {
   int tile_cols;
-  int64_t record_floats;
   size_t counters, cut_units, partials, total;
 };
 
 static FullLayout full_layout(const dmc_full_config &c, int32_t max_chunk) {
   FullLayout L{};
   L.tile_cols = dmc::full_tile_cols(c.dtype == DMC_FP32 ? 4 : 2, max_chunk, c.num_q_heads / c.num_kv_heads);
-  L.record_floats = int64_t(L.tile_cols) * (c.head_dim + 2);
   L.counters = 0;
   L.cut_units = DMC_FULL_COUNTER_BYTES;
   L.partials = L.cut_units + align_up(size_t(dmc::kFullPlaces) * sizeof(dmc::FullPiece), 256);
-  L.total = L.partials + align_up(size_t(dmc::kFullPlaces) * 2 * L.record_floats * 4, 256);
+  L.total = L.partials + align_up(size_t(dmc::kFullPlaces) * 2 * full_record_floats(L.tile_cols, c.head_dim) * 4, 256);
   return L;
 }
 
@@ -1456,7 +1456,6 @@ dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int6
   p.counters = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + L.counters);
   p.cut_units = reinterpret_cast<dmc::FullPiece *>(static_cast<char *>(ws) + L.cut_units);
   p.partials = reinterpret_cast<float *>(static_cast<char *>(ws) + L.partials);
-  p.record_floats = L.record_floats;
   p.scale_log2 = static_cast<float>(1.4426950408889634 / std::sqrt(double(cfg->head_dim)));
   p.total = total;
   p.rows = cfg->batch;
@@ -1468,12 +1467,13 @@ dmc_status dmc_full_attend(const dmc_full_config *cfg, const void *q, const int6
   p.capacity = cfg->max_pages * cfg->page_size;
   p.max_chunk = max_chunk;
   p.places = dmc::kFullPlaces;
-  p.tile_cols = L.tile_cols;
   const int G = cfg->num_q_heads / cfg->num_kv_heads;
-  p.tile_tokens = std::max(1, L.tile_cols / G);
-  const int64_t tiles = cu ? int64_t(total) * G / L.tile_cols + cfg->batch
-                           : int64_t(cfg->batch) * ((G + L.tile_cols - 1) / L.tile_cols);
-  p.one_launch = dmc::full_one_launch(L.tile_cols, tiles, cfg->num_kv_heads, p.capacity);
+  const int narrow = std::min(L.tile_cols, es == 4 ? 16 : 32);
+  const int64_t tiles = cu ? int64_t(total) * G / narrow + cfg->batch : int64_t(cfg->batch) * ((G + narrow - 1) / narrow);
+  p.one_launch = dmc::full_one_launch(tiles, cfg->num_kv_heads, p.capacity);
+  p.tile_cols = p.one_launch ? narrow : L.tile_cols;
+  p.tile_tokens = std::max(1, p.tile_cols / G);
+  p.record_floats = full_record_floats(p.tile_cols, cfg->head_dim);
   p.group_shift = ilog2(G) - 1;
   p.group_magic = G > 1 ? static_cast<uint32_t>(((uint64_t(1) << (31 + ilog2(G))) + G - 1) / G) : 0;
   int dev = 0;

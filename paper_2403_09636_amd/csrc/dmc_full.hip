@@ -64,15 +64,14 @@ __device__ __forceinline__ int row_of_token(const int32_t *cu, int rows, int tot
 }
 
 // ---------------------------------------------------------------------------
-// Rotation and append.  A workgroup takes 1 << shift tokens (1 or 4): one wave
-// per token forms the cosines and sines of its pairs (in 64 bits up to the
-// fraction of a turn), which every head of the token uses from LDS; then each
-// thread moves units of two 16-byte vectors of a head, the two halves of 16 / ES
-// pairs (or 16 / ES adjacent pairs), in grid.y shares of the group's units.
-// Bound by HBM, each element read and written once.
+// Rotation and append.  A workgroup takes one token: its first wave forms the cosines
+// and sines of the pairs (in 64 bits up to the fraction of a turn), which every head
+// uses from LDS; then each thread moves units of two 16-byte vectors of a head, the
+// two halves of 16 / ES pairs (or 16 / ES adjacent pairs), in grid.y shares of the
+// token's units.  Bound by HBM, each element read and written once: 8192 tokens of 32 +
+// 32 heads of 128 in bf16 take 100 us (5.4 TB/s of reads and writes).  Four tokens to a
+// workgroup: 106 us, 6 prompts of up to 4096 in append 157 us against 148.
 // ---------------------------------------------------------------------------
-constexpr int kRotTokens = 4;
-
 // A store that cannot be to LDS (from pointers of several origins the compiler makes
 // flat stores, which count as LDS accesses too).
 __device__ __forceinline__ void store_global(char *p, const uint4 &v) {
@@ -81,14 +80,13 @@ __device__ __forceinline__ void store_global(char *p, const uint4 &v) {
 }
 
 template <int ES, int D, bool PAGED>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int shift) {
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p) {
   constexpr int N = 16 / ES, UPR = D * ES / 32;   // elements of a vector, units of a row
   constexpr int kBatch = 4;                       // units of a thread whose loads are in flight at once
-  __shared__ __align__(16) float cosv[kRotTokens][64], sinv[kRotTokens][64];
-  __shared__ int64_t place[kRotTokens];   // element offset of the token's slot of kv head 0 (-1: none)
-  __shared__ int state[kRotTokens];       // 0: no token of a row, 1: here, 2: dropped
+  __shared__ __align__(16) float cosv[64], sinv[64];
+  __shared__ int64_t place;   // element offset of the token's slot of kv head 0 (-1: none)
+  __shared__ int state;       // 0: no token of a row, 1: here, 2: dropped
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if constexpr (PAGED) {
     if (blockIdx.x == gridDim.x - 1) {   // the rows' boundaries and lengths
       if (blockIdx.y == 0 && p.flags) {
@@ -99,15 +97,14 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
       return;
     }
   }
-  const int t0 = blockIdx.x << shift, ntok = min(1 << shift, p.total - t0);
-  if (wave < ntok) {
-    const int t = t0 + wave;
+  const int64_t t = blockIdx.x;
+  if (tid < 64) {
     int pos, st = 1;
     int64_t at = -1;
     if constexpr (PAGED) {
-      const int b = p.cu ? row_of_token(p.cu, p.rows, p.total, t) : t;
+      const int b = p.cu ? row_of_token(p.cu, p.rows, p.total, blockIdx.x) : blockIdx.x;
       const FullRow r = full_row(p.cu, p.len, p.total, p.capacity, b);
-      const int i = t - r.start;
+      const int i = static_cast<int>(blockIdx.x) - r.start;
       pos = r.n + i;
       st = i < 0 || i >= r.given ? 0 : i < r.m ? 1 : 2;
       if (st == 1) {
@@ -121,26 +118,28 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
       pos = p.positions[t];
     }
     if (lane == 0) {
-      place[wave] = at;
-      state[wave] = st;
+      place = at;
+      state = st;
     }
     if (lane < p.r / 2) {
       // turns: the product and its fraction in 64 bits
       const double turns = pos * (double(p.inv_freq[lane]) * 0.15915494309189533577);
       float s, c;
       sincospif(2.0f * static_cast<float>(turns - rint(turns)), &s, &c);
-      cosv[wave][lane] = c;
-      sinv[wave][lane] = p.inverse ? -s : s;
+      cosv[lane] = c;
+      sinv[lane] = p.inverse ? -s : s;
     }
   }
   __syncthreads();
 
-  const int nrows = p.hq + (PAGED ? 2 : 1) * p.hkv, units = ntok * nrows * UPR;
+  const int st = PAGED ? state : 1;
+  if (st == 0) return;
+  const int units = (p.hq + (PAGED ? 2 : 1) * p.hkv) * UPR;
   const int rv2 = p.r * ES / 32, stride = kThreads * gridDim.y;   // rotated units of a row
   for (int base = blockIdx.y * kThreads + tid; base < units; base += stride * kBatch) {
     uint4 x[kBatch][2];
     char *dst[kBatch];       // of the first vector (nullptr: nothing to write)
-    int gap[kBatch], cs[kBatch];   // bytes to the second one; first pair (token * 64 + pair), -1: not rotated
+    int gap[kBatch], cs[kBatch];   // bytes to the second one; first pair, -1: not rotated
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int idx = base + j * stride;
@@ -149,14 +148,11 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
       cs[j] = -1;
       x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
       if (idx >= units) continue;
-      const int u = idx % UPR, rr = idx / UPR, tok = rr / nrows, row = rr - tok * nrows;
-      const int st = PAGED ? state[tok] : 1;
-      if (PAGED && st == 0) continue;
-      const int64_t t = t0 + tok;
+      const int u = idx % UPR, row = idx / UPR;
       const bool is_q = row < p.hq, is_v = PAGED && row >= p.hq + p.hkv;
       int v0 = 2 * u;
       if (u < rv2 && !is_v) {
-        cs[j] = tok * 64 + u * N;
+        cs[j] = u * N;
         if (p.halves) {
           v0 = u;
           gap[j] = rv2 * 16;
@@ -171,8 +167,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
         src = is_v ? static_cast<const char *>(p.v) + (t * p.vs[0] + h * p.vs[1]) * ES
                    : static_cast<const char *>(p.k) + (t * p.ks[0] + h * p.ks[1]) * ES;
         if constexpr (PAGED) {
-          if (place[tok] < 0) continue;
-          dst[j] = (is_v ? p.vp : p.kp) + (place[tok] + ((int64_t(h) * D) << p.log2p)) * ES + v0 * 16;
+          if (place < 0) continue;
+          dst[j] = (is_v ? p.vp : p.kp) + (place + ((int64_t(h) * D) << p.log2p)) * ES + v0 * 16;
         } else {
           dst[j] = static_cast<char *>(p.ko) + (t * p.kos[0] + h * p.kos[1]) * ES + v0 * 16;
         }
@@ -193,8 +189,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
         V16<ES>::unpack(x[j][1], b);
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-          *reinterpret_cast<f32x4_t *>(c + i) = *reinterpret_cast<const f32x4_t *>(&cosv[0][0] + cs[j] + i);
-          *reinterpret_cast<f32x4_t *>(s + i) = *reinterpret_cast<const f32x4_t *>(&sinv[0][0] + cs[j] + i);
+          *reinterpret_cast<f32x4_t *>(c + i) = *reinterpret_cast<const f32x4_t *>(cosv + cs[j] + i);
+          *reinterpret_cast<f32x4_t *>(s + i) = *reinterpret_cast<const f32x4_t *>(sinv + cs[j] + i);
         }
         if (p.halves) {
 #pragma unroll
@@ -227,8 +223,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
 // columns: the pairs of a new token and a head of one kv head's group) of one row
 // and kv head; it takes as many keys as its row holds (or its last token sees).
 // Units are cut into pieces of keys, in ranges, one to a workgroup:
-//   - few units and keys (latency counts): every unit in equal pieces, one piece to
-//     a workgroup;
+//   - few units and keys (latency counts): every unit in equal pieces (one, where there
+//     are about as many units as workgroups), one piece to a workgroup;
 //   - else the units of all rows lie one after another in a space of keys, row by
 //     row, which is cut into equal ranges; a block of keys belongs to the range that
 //     its first key lies in.  A range may hold several pieces.
@@ -236,7 +232,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p, int sh
 // record (running maximum, sum and accumulator), to be joined in the order of the
 // keys: o = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i.  That is done by the
 // workgroup that finishes a unit's last piece (a counter tells) where the caches'
-// capacity is small, else by a second launch (p.one_launch).
+// capacity is small (full_one_launch), else by a second launch, since the counting and
+// the writes through to memory cost more than a launch there.
 // ---------------------------------------------------------------------------
 
 // A wave-uniform value, made visibly so (SGPRs).
@@ -288,8 +285,20 @@ __device__ __forceinline__ int table_entry(const int32_t *table, int i) {
   return reinterpret_cast<const_i32_t *>(reinterpret_cast<uintptr_t>(table))[__builtin_amdgcn_readfirstlane(i)];
 }
 
-// Fewest keys of a piece, and the most per workgroup for which units are cut equally.
-constexpr int kNarrowRange = 128, kWideRange = 512, kEqualKeys = 1024;
+// Fewest keys of a piece: shorter ones cost more in records than they gain.  Narrow
+// tiles (each wave takes a fourth of the keys; 16/4 heads of 128 in bf16, one row of 900
+// keys): 64 14.0 us, 128 11.3, 256 11.6; 5 rows of up to 1500, fp32: 17.2, 15.0, 19.6.
+// fp32 chunks, whose waves take every key (64 tokens on 500, 4 rows of 8/4 heads of
+// 128): 32 26.4 us, 64 27.8, 128 35.5; 256 in an empty cache: 28.7, 27.0, 34.5.  Wide
+// tiles (64 tokens on 16000, 32/8 heads): 256 46.2 us, 512 46.5, 1024 68.4; 4 rows of
+// 512 tokens on 12000, 64/8 heads: 862, 855, 858.
+// kEqualKeys: the keys per workgroup up to which units are cut equally where there are
+// at least 4 workgroups to a unit, half of it where there are fewer (then the ranges
+// fill the chip better).  64 tokens on 16000: 46.5 us, with 256 58.8; 8 rows of 8 tokens
+// on 4000, 32 heads: 90 us, with 4096 144.  Units that are not cut (60 rows of up to 500
+// keys, 8 kv heads): 20.2 us, in ranges 27.6; the rule's edge, 40 rows of up to 1000:
+// 33.7 us against 30.4.
+constexpr int kNarrowRange = 128, kChunkRange = 64, kWideRange = 512, kEqualKeys = 1024;
 
 // a / G for a < 2^31, by a multiplication (G = 1: group_shift < 0).
 __device__ __forceinline__ int div_group(const FullParams &p, int a) {
@@ -377,11 +386,11 @@ struct Space {
       const int units = m > 0 ? static_cast<int>(min(int64_t(p.hkv) * t.count, int64_t(1) << 24)) : 0;
       const int count = __builtin_amdgcn_readlane(wave_scan(units), 63);
       const int sum = __builtin_amdgcn_readlane(wave_scan(static_cast<int>(min(int64_t(units) * keys, int64_t(1) << 24))), 63);
-      equal = 2 * count <= grid && sum <= kEqualKeys * grid;
+      equal = count <= grid && sum <= (4 * count <= grid ? kEqualKeys : kEqualKeys / 2) * grid;
       int64_t share, x;
       int pieces = 0;
       if (equal) {
-        const int each = max(small_div(sum, grid - count) + 1, LEAST);
+        const int each = max(small_div(sum, max(grid - count, 1)) + 1, LEAST);
         pieces = (keys + each - 1) / each;
         share = units * pieces;
         x = wave_scan(units * pieces);
@@ -450,8 +459,11 @@ struct Space {
   }
 
   // A range's end that lies within kSnap keys of a unit's end moves there: a cut unit
-  // costs two records and their join, as much as some hundred keys.
-  static constexpr int kSnap = TRI ? 512 : 128;
+  // costs two records and their join, as much as some hundred keys (32 rows of 200 keys,
+  // 32 heads: 20.7 us, without 34.4; 4 prompts of up to 2048 tokens, 32/8 heads, wide:
+  // 138 us, without 152; fp32 chunks with 512 in place of 128, 2 rows of 1000 tokens:
+  // 149 us against 86).
+  static constexpr int kSnap = TRI && ES == 2 ? 512 : 128;
   __device__ __forceinline__ int64_t boundary(int i) {
     const int64_t v = min(i * per, all);
     if (equal || v == 0 || v == all) return v;
@@ -941,7 +953,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = p.hq / p.hkv;
 
-  Space<ES, D, TRI, kNarrowRange> space(p, prefix, space_lds);
+  Space<ES, D, TRI, SPLIT_KEYS ? kNarrowRange : kChunkRange> space(p, prefix, space_lds);
   if (tid == 0) cuts.n = 0;
   while (space.pos < space.hi) {
     const Piece x = space.next();
@@ -1474,14 +1486,14 @@ void launch_narrow(const FullParams &p, size_t lds, hipStream_t s) {
 
 template <int ES, int D>
 hipError_t launch_rotation(const RotateParams &p, bool paged, hipStream_t s) {
-  // Few tokens: one to a workgroup, their heads shared out, so that the chip is filled.
-  const int64_t units = int64_t(p.total) * (p.hq + (paged ? 2 : 1) * p.hkv) * (D * ES / 32);
-  const bool few = units < int64_t(2048) * kThreads;
-  const int shift = few ? 0 : 2, groups = (p.total + (1 << shift) - 1) >> shift;
-  const int shares = few ? static_cast<int>((units / p.total + kThreads - 1) / kThreads) : 1;
-  const dim3 grid(groups + (paged ? 1 : 0), shares);
-  if (paged) hipLaunchKernelGGL((rotate_kernel<ES, D, true>), grid, dim3(kThreads), 0, s, p, shift);
-  else hipLaunchKernelGGL((rotate_kernel<ES, D, false>), grid, dim3(kThreads), 0, s, p, shift);
+  // Few tokens: the heads of each shared out to workgroups of 256 units, so that the
+  // chip is filled (1024 tokens of 48 heads: 9.8 us for both; 2048: 13.3 us shared, 12.4
+  // not; a decode step of 32 rows: 4.3 us).
+  const int units = (p.hq + (paged ? 2 : 1) * p.hkv) * (D * ES / 32);
+  const int shares = int64_t(units) * p.total < int64_t(2048) * kThreads ? (units + kThreads - 1) / kThreads : 1;
+  const dim3 grid(p.total + (paged ? 1 : 0), shares);
+  if (paged) hipLaunchKernelGGL((rotate_kernel<ES, D, true>), grid, dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((rotate_kernel<ES, D, false>), grid, dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

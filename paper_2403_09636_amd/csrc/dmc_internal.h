@@ -426,19 +426,26 @@ struct FullParams {
   int32_t group_shift;
   int32_t total, rows, hq, hkv, log2p, max_pages, num_pages, capacity, max_chunk, places, tile_cols, tile_tokens;
 };
-// Workgroups of the attention: two to each of 256 compute units.
+// Workgroups of the attention: two to each of 256 compute units (with three, 64 rows of
+// up to 1000 keys take 47.7 us instead of 40.1, wide tiles 1044 us instead of 855).
 constexpr int kFullPlaces = 512;
 // Query columns of a tile: 16 or 32 (bf16) that all waves of a workgroup share; wider
-// ones, of whole tokens, once a row has more: 128 (bf16) or 64 (fp32).
+// ones, of whole tokens, once a row has more: 128 (bf16) or 64 (fp32).  Drafts of 4
+// tokens, 64/8 heads, 16 rows of up to 8192 keys: 69.5 us with 32 columns, 83.0 with 16,
+// 91.7 with 128; fp32 chunks of 64 tokens on 8000, 8/4 heads of 128: 190 us with 64
+// columns, 290 with 16.
 constexpr inline int full_tile_cols(int elem_bytes, int64_t max_chunk, int group) {
   const int64_t cols = max_chunk * group;
   if (elem_bytes == 4) return cols <= 16 || group > 64 ? 16 : 64;
   return cols <= 16 ? 16 : cols <= 32 || group > 128 ? 32 : 128;
 }
-// Whether records are joined within the attention's launch: where the rows' capacity
-// is small (tiles: column tiles of all rows).  The capacity decides, not the lengths.
-constexpr inline bool full_one_launch(int tile_cols, int64_t tiles, int hkv, int64_t capacity) {
-  return tile_cols <= 32 && tiles * hkv * capacity <= int64_t(1) << 18;
+// Whether the work is small whatever the lengths are (tiles: narrow column tiles of all
+// rows): then all tiles are narrow and their records are joined within the launch.
+// A row of 900 keys: 11.2 us, in two launches 12.3; 77 tokens on 700, 2 rows of 32/8 heads:
+// 21.3 us, with wide tiles in two launches 27.7.  Larger work joined within the launch: 64
+// rows of up to 1000 keys 43.9 us against 40.1, 16 rows of up to 24000 152 against 147.
+constexpr inline bool full_one_launch(int64_t tiles, int hkv, int64_t capacity) {
+  return tiles * hkv * capacity <= int64_t(1) << 18;
 }
 hipError_t launch_full_attend(int elem_bytes, int head_dim, const FullParams &p, hipStream_t s);
 

@@ -337,6 +337,7 @@ def test_strides_of_two_threads_do_not_mix():
 
 
 def test_more_tokens_than_a_launch_takes():
-    """2^26 tokens in groups of four, 256 threads each, would be 2^32 threads."""
-    for total in ((1 << 24) + 1, 1 << 26):
-        assert _c_rotate(total=total) == 2 and "16777216" in Bd.last_error()
+    """2^24 tokens, 256 threads each, would be 2^32 threads."""
+    for total in ((1 << 23) + 1, 1 << 24):
+        assert _c_rotate(total=total) == 2 and "8388608" in Bd.last_error()
+        assert _c_append(total=total) == 2 and "too many tokens" in Bd.last_error()

@@ -11,6 +11,18 @@ pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 
 
+ROOM = [0]
+
+
+@pytest.fixture(params=[0, 1 << 19], ids=["small", "roomy"])
+def room(request):
+    """Caches as large as their rows, and such that could hold half a million tokens a row: joined in one launch
+    from narrow tiles or in two, from wide ones where a row has many columns."""
+    ROOM[0] = request.param
+    yield
+    ROOM[0] = 0
+
+
 class Case:
     """Rows of held[b] cached tokens and lens[b] new ones (in the pages already); every other place of the pools
     holds NaN."""
@@ -21,7 +33,7 @@ class Case:
         self.wide = (max(max(lens), 1) if max_chunk is None else max_chunk) * (hq // hkv) > 32   # columns of a row
         self.held, self.lens, self.page, self.layer, self.hq, self.hkv, self.d = held, lens, page, layer, hq, hkv, d
         need = [-(-(n + m) // page) if n >= 0 else 0 for n, m in zip(held, lens)]
-        width = max(max(need), 1) if width is None else width
+        width = max(max(need), 1, ROOM[0] // page) if width is None else width
         cfg = P.make_full_config(len(lens), hq, hkv, d, dtype, page_size=page, max_pages=width, num_pages=sum(need) + 2)
         T = sum(lens) + tail
         self.max_chunk = max(max(lens), 1) if max_chunk is None else max_chunk
@@ -86,7 +98,7 @@ STEP = [0, 1, 30, 31, 32, 63, 64, -1, 127, 255, 256, 300, 511, 700]
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("hq,hkv", [(2, 2), (8, 1), (6, 2), (34, 2)])
 @pytest.mark.parametrize("page", [8, 32])
-def test_step(torch_cuda, dtype, d, hq, hkv, page):
+def test_step(torch_cuda, room, dtype, d, hq, hkv, page):
     if (dtype, d, hq, page) == ("fp32", 128, 34, 8):
         pytest.skip("an earlier kernel for it (32 columns, registers spilled) faulted once, cause not found; that kernel is gone")
     import paper_2403_09636_amd as P
@@ -95,7 +107,7 @@ def test_step(torch_cuda, dtype, d, hq, hkv, page):
 
 @pytest.mark.parametrize("page", [16, 64, 1024])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-def test_step_of_other_pages(torch_cuda, page, dtype):
+def test_step_of_other_pages(torch_cuda, room, page, dtype):
     import paper_2403_09636_amd as P
     Case(P, [0, 15, 16, 1023, 1024, 1500], [1] * 6, hq=8, hkv=2, d=128, dtype=dtype, page=page, packed=False).run()
 
@@ -114,7 +126,7 @@ CHUNKS = [([0, 0, 0, 5], [1, 7, 33, 4]), ([100, 31, 32, 33, 0, 500], [2, 1, 0, 4
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("hq,hkv", [(2, 2), (4, 1), (8, 1), (15, 3)])
 @pytest.mark.parametrize("i", range(len(CHUNKS)))
-def test_chunks(torch_cuda, dtype, d, hq, hkv, i):
+def test_chunks(torch_cuda, room, dtype, d, hq, hkv, i):
     import paper_2403_09636_amd as P
     held, lens = CHUNKS[i]
     Case(P, held, lens, hq=hq, hkv=hkv, d=d, dtype=dtype, page=(32, 8, 64)[i], tail=3).run()
@@ -122,19 +134,19 @@ def test_chunks(torch_cuda, dtype, d, hq, hkv, i):
 
 @pytest.mark.parametrize("hq,hkv,d,dtype,page", [(8, 8, 128, "bf16", 32), (16, 2, 64, "bf16", 16), (71, 1, 64, "bf16", 32),
                                                 (6, 2, 128, "bf16", 128), (4, 2, 64, "fp32", 32), (2, 1, 128, "fp32", 8)])
-def test_pieces(torch_cuda, hq, hkv, d, dtype, page):
+def test_pieces(torch_cuda, room, hq, hkv, d, dtype, page):
     """Long chunks: whole prompts in an empty cache, pieces behind a context, few tokens among them."""
     import paper_2403_09636_amd as P
     Case(P, [0, 700, 77, 3000, 20], [300, 129, 0, 257, 1], hq=hq, hkv=hkv, d=d, dtype=dtype, page=page, tail=1).run()
 
 
-def test_two_tokens_of_one_row_over_everything(torch_cuda):
+def test_two_tokens_of_one_row_over_everything(torch_cuda, room):
     import paper_2403_09636_amd as P
     Case(P, [0, 40000, 0], [0, 200, 0], hq=8, hkv=1, d=128, page=32).run()
 
 
 @pytest.mark.parametrize("cols", [1, 2, 3, 4, 5, 8, 9, 16, 17, 32, 33, 64, 65, 128, 129])
-def test_column_counts(torch_cuda, cols):
+def test_column_counts(torch_cuda, room, cols):
     """Every kind of column tile, full and not."""
     import paper_2403_09636_amd as P
     Case(P, [333, 64], [cols, min(cols, 2)], hq=1, hkv=1, d=64).run()
@@ -144,7 +156,7 @@ def test_column_counts(torch_cuda, cols):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("lens", [[1, 1, 1], [6, 3, 1], [150, 40, 1]])
-def test_what_a_query_does_not_see_never_reaches_it(torch_cuda, dtype, lens):
+def test_what_a_query_does_not_see_never_reaches_it(torch_cuda, room, dtype, lens):
     """Infinities and NaN in later tokens of the same chunk (and behind every row, as everywhere here): each token's
     outputs are those of a row that ends with it, bit for bit."""
     import paper_2403_09636_amd as P
@@ -171,7 +183,7 @@ def test_what_a_query_does_not_see_never_reaches_it(torch_cuda, dtype, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-def test_infinite_values_that_are_seen(torch_cuda, dtype):
+def test_infinite_values_that_are_seen(torch_cuda, room, dtype):
     import paper_2403_09636_amd as P
     c = Case(P, [100, 3], [1, 1], hq=2, hkv=1, d=64, dtype=dtype, packed=False, scale=0.5)
     c.V[int(c.table[0, 1]), 0, 5, 10] = math.inf
@@ -191,7 +203,7 @@ def test_infinite_values_that_are_seen(torch_cuda, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-def test_scores_of_any_size(torch_cuda, dtype):
+def test_scores_of_any_size(torch_cuda, room, dtype):
     """One key far above the others, all far below zero, and all equal."""
     import paper_2403_09636_amd as P
     c = Case(P, [200, 200, 200], [1, 1, 1], hq=1, hkv=1, d=64, dtype=dtype, packed=False, scale=1.0)
@@ -241,7 +253,7 @@ def test_bad_boundaries_raise_the_flag(torch_cuda):
         assert int(c.full.flags) & 4, cu
 
 
-def test_same_bits_every_time_and_in_any_batch(torch_cuda):
+def test_same_bits_every_time_and_in_any_batch(torch_cuda, room):
     import paper_2403_09636_amd as P
     c = Case(P, [3000, 10, 700, 64], [3, 1, 2, 5], hq=8, hkv=2, d=128)
     first = c.attend()
@@ -250,7 +262,7 @@ def test_same_bits_every_time_and_in_any_batch(torch_cuda):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
-def test_strided_tensors_and_layers(torch_cuda):
+def test_strided_tensors_and_layers(torch_cuda, room):
     import paper_2403_09636_amd as P
     c = Case(P, [100, 33, 0], [2, 1, 3], hq=4, hkv=2, d=64, num_layers=3, layer=2)
     plain = c.attend()
@@ -437,7 +449,7 @@ def test_many_rows(torch_cuda):
     c.check(out.cpu(), lse.cpu(), rows=set(range(0, 3000, 37)) | {76, 77, 78, 2999})
 
 
-def test_many_rows_of_wide_chunks(torch_cuda):
+def test_many_rows_of_wide_chunks(torch_cuda, room):
     """More than 64 rows (their sums in LDS beside the wide tiles' ring; fp32 tiles of 64 columns), long chunks among
     short and empty ones."""
     import paper_2403_09636_amd as P
@@ -452,7 +464,7 @@ def test_many_rows_of_wide_chunks(torch_cuda):
         c.full.check()
 
 
-def test_counters_are_left_at_zero(torch_cuda):
+def test_counters_are_left_at_zero(torch_cuda, room):
     import paper_2403_09636_amd as P
     for held, lens, hq, hkv in (([900], [1], 16, 4), ([140001], [1], 8, 1), ([3000, 5, 700], [2, 1, 3], 8, 2)):
         c = Case(P, held, lens, hq=hq, hkv=hkv, d=64, packed=len(held) > 1)
