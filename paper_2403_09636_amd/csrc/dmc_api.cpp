@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/dmc.h"
+#include "dmc_full.h"
 #include "dmc_internal.h"
 
 using dmc::align_up;

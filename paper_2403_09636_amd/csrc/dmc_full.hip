@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "dmc_full.h"
 #include "dmc_mfma.h"
 
 namespace dmc {
