@@ -545,3 +545,55 @@ def test_the_largest_batch_with_wide_chunks(torch_cuda):
     out, lse = c.attend()
     c.check(out.cpu(), lse.cpu(), rows={0, 1, 2000, 4094, 4095})
     c.full.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [32, 33, 48, 63, 64, 65])
+def test_about_as_many_units_as_workgroups(torch_cuda, room, dtype, rows):
+    """256 to 520 units of 8 kv heads and up to 500 keys: cut equally, left whole, or in ranges."""
+    import paper_2403_09636_amd as P
+    g = torch.Generator().manual_seed(rows)
+    held = torch.randint(-40, 500, (rows,), generator=g).tolist()
+    held[0], held[-1] = 499, 320
+    c = Case(P, held, [1] * rows, hq=16, hkv=8, d=64, dtype=dtype, packed=False)
+    out, lse = c.attend()
+    c.check(out.cpu(), lse.cpu(), rows=set(range(0, rows, 7)) | {rows - 1})
+    c.full.check()
+
+
+@pytest.mark.parametrize("tokens", [255, 256, 257, 400, 512, 520])
+def test_prompts_of_about_as_many_units_as_workgroups(torch_cuda, room, tokens):
+    import paper_2403_09636_amd as P
+    Case(P, [0], [tokens], hq=32, hkv=8, d=64).run()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_calls_of_either_kind_on_one_workspace(torch_cuda, dtype):
+    """Small calls (joined within their launch) and large ones (joined by a second) in turn on one object; every one gives
+    the same bits as on an object of its own."""
+    import paper_2403_09636_amd as P
+    B, hq, hkv, d, page, width = 4, 16, 8, 64, 32, 64
+    g = torch.Generator().manual_seed(3)
+    cfg = P.make_full_config(B, hq, hkv, d, dtype, page_size=page, max_pages=width)
+    make = lambda: P.DMCFull(cfg, max_tokens=1200, max_chunk=300)
+    a, pools = make(), [torch.randn(make().k_pages.shape, generator=g).to(DT[dtype]) for _ in range(2)]
+    table = torch.randperm(B * width, generator=g).view(B, width).int()
+    held = torch.tensor([1500, 40, 0, 700], dtype=torch.int32)
+
+    def fill(x):
+        x.k_pages.copy_(pools[0])
+        x.v_pages.copy_(pools[1])
+        x.page_table.copy_(table)
+        x.lengths.copy_(held)
+        return x
+    fill(a)
+    calls = []
+    for lens in ([1, 1, 1, 1], [300, 300, 300, 300], [2, 0, 7, 1], [300, 5, 280, 300], [60, 1, 0, 2]):
+        cu = torch.tensor([0] + lens).cumsum(0).int().cuda()
+        q = torch.randn(sum(lens), hq, d, generator=g).to(DT[dtype]).cuda()
+        calls.append((q, cu, fill(make()).attend(0, q, cu_seqlens=cu)))
+    for _ in range(3):
+        for q, cu, want in calls:
+            got = a.attend(0, q, cu_seqlens=cu)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), cu.tolist()
+    a.check()
