@@ -685,7 +685,8 @@ struct Cuts {
 // workgroup to count reads only after it has counted; it leaves the counter at 0.
 // Counting at the end of the range, not after each piece, keeps the wait out of the
 // stream of keys.  More than kJoin pieces are joined in groups of kJoin first, so
-// that no workgroup reads more than a few dozen records.  Counters: one per record for
+// that no workgroup reads more than a few dozen records (a row of 100000 keys, 8/1 heads:
+// groups of 8 36.2 us, 16 30.5, 32 31.6; 30000, 64/8 heads: 33.7, 34.6, 38.2).  Counters: one per record for
 // the groups that start with it, one per range for the unit that starts in it.
 constexpr int kJoin = 16;
 __device__ __forceinline__ int count_up(int32_t *counter, int count) {
@@ -738,7 +739,8 @@ __device__ __forceinline__ void join_cuts(const FullParams &p, Cuts &cuts, void 
 }
 
 // The second launch: a workgroup per range (one unit at most starts in it and goes
-// on) and `step` columns.
+// on) and `step` columns; 5 to 6 us beside 144 of the first (16 rows of up to 24000).
+// Steps of 32 columns in place of 8: drafts of 4 tokens 72.1 us against 68.7.
 template <int ES, int D>
 __global__ __launch_bounds__(kThreads) void full_join_kernel(FullParams p, int step) {
   __shared__ float2 w[kJoinPairs];
@@ -751,7 +753,10 @@ __global__ __launch_bounds__(kThreads) void full_join_kernel(FullParams p, int s
 // ---------------------------------------------------------------------------
 // Tiles of 16 and 32 columns in registers: decode steps, drafts, all of fp32.
 // Bound by HBM: keys and values go from memory straight into the operands of the
-// 16x16 matrix instructions, without LDS.  Blocks of 16 U keys; with lane l = 16 g +
+// 16x16 matrix instructions, without LDS (each is used by one wave only).  48 rows of
+// 4095 keys, 32 heads of 128: 483 us, 6.7 TB/s; 16 rows of up to 24000, 64/8 heads: 144
+// us, 6.2 TB/s.  Short rows are bound by latency: one row of 900, 16/4 heads: 10.5 us.
+// Blocks of 16 U keys; with lane l = 16 g +
 // c (g < 4, c < 16):
 //   S[key][col] = K Q^T: lane rows are keys 16 u + c, and its slices of the head dim
 //     any 16 bytes, as long as Q's are the same; the result's registers hold keys
@@ -942,8 +947,9 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
   constexpr int E = X::E, U = X::U, KEYS = 16 * U, RB = D * ES, JS = D + 4, STEP = SPLIT_KEYS ? kWaves : 1;
   constexpr int COLS = 16 * NT * (SPLIT_KEYS ? 1 : kWaves);
   constexpr bool TRI = !SPLIT_KEYS;
-  // (keys are read in 64-byte parts of a line: with 32 columns plain loads are 4 %
-  // faster, with 16 and long rows 4 % slower)
+  // Keys are read in 64-byte parts of a line: with 32 columns plain loads are faster
+  // (drafts of 4 tokens on 8192, 64/8 heads: 68.7 us, streamed 71.9), with 16 slower (16
+  // rows of up to 24000, 64/8 heads: 154.5 us, streamed 147.5).
   constexpr bool STREAM_KEYS = SPLIT_KEYS && NT == 1;
   extern __shared__ int64_t prefix[];
   __shared__ SpaceLds space_lds;
@@ -1216,7 +1222,9 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
 
 // ---------------------------------------------------------------------------
 // Wide tiles (128 columns, bf16): pieces of prompts, turns, long drafts.  Bound by
-// the matrix cores and the vector work of the softmax beside them.  One workgroup =
+// the matrix cores and the vector work of the softmax beside them (busy 49 % and 44 % of
+// the cycles, which share the issue slots): 4 rows of 512 tokens on 12000, 64/8 heads,
+// take 855 to 910 us, 900 to 960 TFLOP/s, 80 % of a large product's.  One workgroup =
 // 4 waves, a wave owning 32 columns (lane l: column l % 32, half l / 32), so that
 // all heads of a kv head's group share its keys.  Keys and values stream through LDS
 // in blocks of 32 (direct global -> LDS transfers, a ring of four blocks, three
