@@ -69,21 +69,26 @@ __device__ __forceinline__ int row_of_token(const int32_t *cu, int rows, int tot
 // and sines of the pairs (in 64 bits up to the fraction of a turn), which every head
 // uses from LDS; then each thread moves units of two 16-byte vectors of a head, the
 // two halves of 16 / ES pairs (or 16 / ES adjacent pairs), in grid.y shares of the
-// token's units.  Bound by HBM, each element read and written once: 8192 tokens of 32 +
-// 32 heads of 128 in bf16 take 100 us (5.4 TB/s of reads and writes).  Four tokens to a
-// workgroup: 106 us, 6 prompts of up to 4096 in append 157 us against 148.
+// token's units.  Bound by HBM, each element read and written once: 6 sequences of up to
+// 4096 tokens, 32 + 32 heads of 128 in bf16, take 87 us (5.9 TB/s of reads and writes), in
+// append 148.  Four tokens to a workgroup: 102 and 157 us; four units of a thread in flight
+// at once, with fewer waves: 2048 tokens 28.6 us against 24.7.  The rotation's stores
+// stream (without: 91 us; the causal attention that reads them next takes the same time
+// after either), the append's do not (with: 157 us).
 // ---------------------------------------------------------------------------
 // A store that cannot be to LDS (from pointers of several origins the compiler makes
 // flat stores, which count as LDS accesses too).
+template <bool STREAM>
 __device__ __forceinline__ void store_global(char *p, const uint4 &v) {
   typedef __attribute__((address_space(1))) u32x4 gv;
-  *reinterpret_cast<gv *>(reinterpret_cast<uintptr_t>(p)) = __builtin_bit_cast(u32x4, v);
+  gv *at = reinterpret_cast<gv *>(reinterpret_cast<uintptr_t>(p));
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), at);
+  else *at = __builtin_bit_cast(u32x4, v);
 }
 
 template <int ES, int D, bool PAGED>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p) {
   constexpr int N = 16 / ES, UPR = D * ES / 32;   // elements of a vector, units of a row
-  constexpr int kBatch = 4;                       // units of a thread whose loads are in flight at once
   __shared__ __align__(16) float cosv[64], sinv[64];
   __shared__ int64_t place;   // element offset of the token's slot of kv head 0 (-1: none)
   __shared__ int state;       // 0: no token of a row, 1: here, 2: dropped
@@ -136,86 +141,68 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p) {
   const int st = PAGED ? state : 1;
   if (st == 0) return;
   const int units = (p.hq + (PAGED ? 2 : 1) * p.hkv) * UPR;
-  const int rv2 = p.r * ES / 32, stride = kThreads * gridDim.y;   // rotated units of a row
-  for (int base = blockIdx.y * kThreads + tid; base < units; base += stride * kBatch) {
-    uint4 x[kBatch][2];
-    char *dst[kBatch];       // of the first vector (nullptr: nothing to write)
-    int gap[kBatch], cs[kBatch];   // bytes to the second one; first pair, -1: not rotated
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const int idx = base + j * stride;
-      dst[j] = nullptr;
-      gap[j] = 16;
-      cs[j] = -1;
-      x[j][0] = x[j][1] = make_uint4(0, 0, 0, 0);
-      if (idx >= units) continue;
-      const int u = idx % UPR, row = idx / UPR;
-      const bool is_q = row < p.hq, is_v = PAGED && row >= p.hq + p.hkv;
-      int v0 = 2 * u;
-      if (u < rv2 && !is_v) {
-        cs[j] = u * N;
-        if (p.halves) {
-          v0 = u;
-          gap[j] = rv2 * 16;
-        }
-      }
-      const char *src;
-      if (is_q) {
-        src = static_cast<const char *>(p.q) + (t * p.qs[0] + row * p.qs[1]) * ES;
-        dst[j] = static_cast<char *>(p.qo) + (t * p.qos[0] + row * p.qos[1]) * ES + v0 * 16;
+  const int rv2 = p.r * ES / 32;   // rotated units of a row
+  for (int idx = blockIdx.y * kThreads + tid; idx < units; idx += kThreads * gridDim.y) {
+    const int u = idx % UPR, row = idx / UPR;
+    const bool is_q = row < p.hq, is_v = PAGED && row >= p.hq + p.hkv;
+    const bool turned = u < rv2 && !is_v && st == 1;
+    int v0 = 2 * u, gap = 16;   // first vector; bytes to the second one
+    if (u < rv2 && !is_v && p.halves) {
+      v0 = u;
+      gap = rv2 * 16;
+    }
+    const char *src;
+    char *dst;
+    if (is_q) {
+      src = static_cast<const char *>(p.q) + (t * p.qs[0] + row * p.qs[1]) * ES;
+      dst = static_cast<char *>(p.qo) + (t * p.qos[0] + row * p.qos[1]) * ES + v0 * 16;
+    } else {
+      const int h = row - p.hq - (is_v ? p.hkv : 0);
+      src = is_v ? static_cast<const char *>(p.v) + (t * p.vs[0] + h * p.vs[1]) * ES
+                 : static_cast<const char *>(p.k) + (t * p.ks[0] + h * p.ks[1]) * ES;
+      if constexpr (PAGED) {
+        if (place < 0) continue;
+        dst = (is_v ? p.vp : p.kp) + (place + ((int64_t(h) * D) << p.log2p)) * ES + v0 * 16;
       } else {
-        const int h = row - p.hq - (is_v ? p.hkv : 0);
-        src = is_v ? static_cast<const char *>(p.v) + (t * p.vs[0] + h * p.vs[1]) * ES
-                   : static_cast<const char *>(p.k) + (t * p.ks[0] + h * p.ks[1]) * ES;
-        if constexpr (PAGED) {
-          if (place < 0) continue;
-          dst[j] = (is_v ? p.vp : p.kp) + (place + ((int64_t(h) * D) << p.log2p)) * ES + v0 * 16;
-        } else {
-          dst[j] = static_cast<char *>(p.ko) + (t * p.kos[0] + h * p.kos[1]) * ES + v0 * 16;
-        }
+        dst = static_cast<char *>(p.ko) + (t * p.kos[0] + h * p.kos[1]) * ES + v0 * 16;
       }
-      if (st == 2) {   // a dropped token's queries: zeros
-        cs[j] = -1;
-        continue;
-      }
-      x[j][0] = ld16(src + v0 * 16);
-      x[j][1] = ld16(src + v0 * 16 + gap[j]);
     }
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      if (!dst[j]) continue;
-      if (cs[j] >= 0) {
-        float a[N], b[N], c[N], s[N];
-        V16<ES>::unpack(x[j][0], a);
-        V16<ES>::unpack(x[j][1], b);
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          *reinterpret_cast<f32x4_t *>(c + i) = *reinterpret_cast<const f32x4_t *>(cosv + cs[j] + i);
-          *reinterpret_cast<f32x4_t *>(s + i) = *reinterpret_cast<const f32x4_t *>(sinv + cs[j] + i);
-        }
-        if (p.halves) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float xa = a[i], xb = b[i];
-            a[i] = xa * c[i] - xb * s[i];
-            b[i] = xa * s[i] + xb * c[i];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < N / 2; ++i) {
-            const float xa = a[2 * i], xb = a[2 * i + 1], ya = b[2 * i], yb = b[2 * i + 1];
-            a[2 * i] = xa * c[i] - xb * s[i];
-            a[2 * i + 1] = xa * s[i] + xb * c[i];
-            b[2 * i] = ya * c[N / 2 + i] - yb * s[N / 2 + i];
-            b[2 * i + 1] = ya * s[N / 2 + i] + yb * c[N / 2 + i];
-          }
-        }
-        x[j][0] = V16<ES>::pack(a);
-        x[j][1] = V16<ES>::pack(b);
-      }
-      store_global(dst[j], x[j][0]);
-      store_global(dst[j] + gap[j], x[j][1]);
+    uint4 x = make_uint4(0, 0, 0, 0), y = x;   // (a dropped token's queries: zeros)
+    if (st == 1) {
+      x = ld16(src + v0 * 16);
+      y = ld16(src + v0 * 16 + gap);
     }
+    if (turned) {
+      float a[N], b[N], c[N], s[N];
+      V16<ES>::unpack(x, a);
+      V16<ES>::unpack(y, b);
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        *reinterpret_cast<f32x4_t *>(c + i) = *reinterpret_cast<const f32x4_t *>(cosv + u * N + i);
+        *reinterpret_cast<f32x4_t *>(s + i) = *reinterpret_cast<const f32x4_t *>(sinv + u * N + i);
+      }
+      if (p.halves) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float xa = a[i], xb = b[i];
+          a[i] = xa * c[i] - xb * s[i];
+          b[i] = xa * s[i] + xb * c[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          const float xa = a[2 * i], xb = a[2 * i + 1], ya = b[2 * i], yb = b[2 * i + 1];
+          a[2 * i] = xa * c[i] - xb * s[i];
+          a[2 * i + 1] = xa * s[i] + xb * c[i];
+          b[2 * i] = ya * c[N / 2 + i] - yb * s[N / 2 + i];
+          b[2 * i + 1] = ya * s[N / 2 + i] + yb * c[N / 2 + i];
+        }
+      }
+      x = V16<ES>::pack(a);
+      y = V16<ES>::pack(b);
+    }
+    store_global<!PAGED>(dst, x);
+    store_global<!PAGED>(dst + gap, y);
   }
 }
 
@@ -1497,7 +1484,7 @@ template <int ES, int D>
 hipError_t launch_rotation(const RotateParams &p, bool paged, hipStream_t s) {
   // Few tokens: the heads of each shared out to workgroups of 256 units, so that the
   // chip is filled (1024 tokens of 48 heads: 9.8 us for both; 2048: 13.3 us shared, 12.4
-  // not; a decode step of 32 rows: 4.3 us).
+  // not, with four units in flight; a decode step of 32 rows: 4.3 us).
   const int units = (p.hq + (paged ? 2 : 1) * p.hkv) * (D * ES / 32);
   const int shares = int64_t(units) * p.total < int64_t(2048) * kThreads ? (units + kThreads - 1) / kThreads : 1;
   const dim3 grid(p.total + (paged ? 1 : 0), shares);
