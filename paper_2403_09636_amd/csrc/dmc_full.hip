@@ -128,12 +128,16 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateParams p) {
       state = st;
     }
     if (lane < p.r / 2) {
-      // turns: the product and its fraction in 64 bits
+      // turns: the product and its fraction in 64 bits; cosine and sine at the fraction in 32
+      // bits, then turned by what those leave out (at most 2^-26 turns)
       const double turns = pos * (double(p.inv_freq[lane]) * 0.15915494309189533577);
+      const double part = turns - rint(turns);
+      const float near = static_cast<float>(part);
+      const float rest = static_cast<float>(part - near) * 6.2831853071795864769f;
       float s, c;
-      sincospif(2.0f * static_cast<float>(turns - rint(turns)), &s, &c);
-      cosv[lane] = c;
-      sinv[lane] = p.inverse ? -s : s;
+      sincospif(2.0f * near, &s, &c);
+      cosv[lane] = fmaf(-s, rest, c);
+      sinv[lane] = p.inverse ? -fmaf(c, rest, s) : fmaf(c, rest, s);
     }
   }
   __syncthreads();
