@@ -1114,7 +1114,8 @@ class DMCFull:
     - k_pages, v_pages [num_layers, num_pages, Hkv, page_size, d], to copy whole pages in or out.
 
     Calls of attend share the object's workspace: those that may run at the same time, on two streams, need objects
-    of their own."""
+    of their own.  A new object is ready for calls on any stream (the constructor waits for its own; one made while a
+    graph is captured belongs to that graph)."""
 
     def __init__(self, cfg: FullConfig, max_tokens=None, max_chunk=1, inv_freq=None, num_layers=1, device="cuda"):
         import torch
@@ -1162,6 +1163,12 @@ class DMCFull:
         self._ws_bytes = n
         self._call = _RowsCall(self.dtype, dev, cfg.head_dim, es)
         self._cu_shape = (cfg.batch + 1,)
+        # the fills above are done before any call, on whichever stream that comes; in a captured graph they come before
+        # the graph's calls
+        if dev.type == "cuda":
+            with torch.cuda.device(dev):
+                if not torch.cuda.is_current_stream_capturing():
+                    torch.cuda.current_stream().synchronize()
 
     k_pages = property(lambda self: self._storage["k_pages"])
     v_pages = property(lambda self: self._storage["v_pages"])

@@ -1,0 +1,47 @@
+"""Full caches from their first moment on: new objects used on another stream at once, or made within a captured graph."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_new_object_is_ready_on_every_stream(torch_cuda):
+    """What the constructor fills (the counters that have to be zero before the first call, page table, lengths, flags)
+    is in place when it returns, however much work its stream has queued: a call may come on any other stream."""
+    import paper_2403_09636_amd as P
+    cfg = P.make_full_config(2, 4, 2, 64, page_size=32, max_pages=2)
+    P.DMCFull(cfg)
+    busy = torch.empty(1 << 30, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(100):   # some tens of milliseconds of work
+            busy.fill_(1)
+        full = P.DMCFull(cfg)
+        assert side.query(), "fills of the object's tensors are still queued"
+    at = -full.workspace.data_ptr() % 256
+    assert not full.workspace[at:at + P.binding.DMC_FULL_COUNTER_BYTES].any()
+    assert not full.lengths.any() and not full.flags.any()
+
+
+def test_an_object_made_while_a_graph_is_captured(torch_cuda):
+    """The fills are part of the graph there (a wait would end the capture)."""
+    import paper_2403_09636_amd as P
+    cfg = P.make_full_config(1, 2, 1, 64, page_size=32, max_pages=2)
+    x = torch.randn(1, 2, 64, device="cuda").bfloat16()
+    out, lse = torch.empty_like(x), torch.empty(1, 2, device="cuda")
+    first = P.DMCFull(cfg)
+    first.page_table.zero_()
+    first.attend(0, x)   # (the library is loaded and the kernel known)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        full = P.DMCFull(cfg)
+        full.page_table.zero_()
+        full.append(0, x[:, :1], x[:, 1:])
+        full.attend(0, x, out=out, lse=lse)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, x[:, 1:].expand(1, 2, 64))
