@@ -1108,7 +1108,8 @@ class DMCFull:
     (default: one per row), at most max_chunk in a row.  The program owns what a scheduler decides and writes it in
     place:
 
-    - page_table, int32 [batch, max_pages]: the pages of every row, shared by the layers;
+    - page_table, int32 [batch, max_pages]: the pages of every row, shared by the layers; -1 (no page: calls that need
+      it find and flag it) until the program writes it;
     - lengths, int32 [batch]: the tokens that every row holds before a call (negative: row not in use); the
       program adds the new ones once all layers have appended and attended;
     - k_pages, v_pages [num_layers, num_pages, Hkv, page_size, d], to copy whole pages in or out.
@@ -1148,7 +1149,8 @@ class DMCFull:
         self._storage = dict(k_pages=parts[0].view(self.dtype).view(shape), v_pages=parts[1].view(self.dtype).view(shape),
                              page_table=parts[2].view(torch.int32).view(cfg.batch, cfg.max_pages),
                              lengths=parts[3].view(torch.int32), flags=parts[4].view(torch.int32))
-        for name in ("page_table", "lengths", "flags"):
+        self._storage["page_table"].fill_(-1)   # (no page: rows that the program has not given pages yet share none)
+        for name in ("lengths", "flags"):
             self._storage[name].zero_()
         self._kp, self._vp, self._table, self._lens, self._flags = (t.data_ptr() for t in self._storage.values())
         self._span = self._buffer.data_ptr(), self._buffer.data_ptr() + self._buffer.numel()

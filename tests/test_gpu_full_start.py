@@ -45,3 +45,22 @@ def test_an_object_made_while_a_graph_is_captured(torch_cuda):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, x[:, 1:].expand(1, 2, 64))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_calls_before_the_page_table_is_written_are_flagged(torch_cuda, packed):
+    """No row has a page yet: nothing is stored (rows do not overwrite each other in page 0), and the flag says so."""
+    import paper_2403_09636_amd as P
+    full = P.DMCFull(P.make_full_config(3, 4, 2, 64, page_size=32, max_pages=2), max_tokens=6, max_chunk=2)
+    full.k_pages.zero_()
+    full.v_pages.zero_()
+    T = 6 if packed else 3
+    cu = torch.tensor([0, 2, 4, 6], dtype=torch.int32, device="cuda") if packed else None
+    x = torch.ones(T, 2, 64, device="cuda").bfloat16()
+    full.append(0, x, x, cu_seqlens=cu)
+    assert not full.k_pages.any() and not full.v_pages.any()
+    with pytest.raises(P.DMCError, match="outside the pool"):
+        full.check()
+    full.flags.zero_()
+    full.attend(0, torch.ones(T, 4, 64, device="cuda").bfloat16(), cu_seqlens=cu)
+    assert int(full.flags) == P.binding.DMC_FLAG_BAD_PAGE
