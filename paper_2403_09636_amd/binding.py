@@ -1104,9 +1104,9 @@ def make_full_config(batch, num_q_heads, num_kv_heads, head_dim, dtype="bf16", p
 
 
 class DMCFull:
-    """Paged caches of layers that keep every token, with the workspace for calls of up to max_tokens new tokens
-    (default: one per row), at most max_chunk in a row.  The program owns what a scheduler decides and writes it in
-    place:
+    """Paged caches of layers that keep every token, with the workspace for attention of up to max_tokens new tokens
+    (default: one per row), at most max_chunk in a row; append needs none, and is not bound by it.  The program owns
+    what a scheduler decides and writes it in place:
 
     - page_table, int32 [batch, max_pages]: the pages of every row, shared by the layers; -1 (no page: calls that need
       it find and flag it) until the program writes it;
@@ -1189,8 +1189,6 @@ class DMCFull:
         if not (isinstance(t, call.Tensor) and t.dim() == 3):
             return None
         T = t.shape[0]
-        if T > self.max_tokens:
-            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
         if T == 0:
             return None
         if cu_seqlens is None:
@@ -1276,6 +1274,8 @@ class DMCFull:
             (q0, x0), st = _packed_args(q, out)
             args = q.shape[0], None if cu_seqlens is None else cu_seqlens.data_ptr(), q0, x0, lse.data_ptr(), st
         T, cu, q0, x0, l0, st = args
+        if T > self.max_tokens:
+            _fail(f"{T} tokens, the workspace holds {self.max_tokens}")
         check(lib.dmc_full_attend(self._cfg_ref, q0, st, cu, T, max_chunk, self._lens, self._table, kp, vp, x0,
                                   byref(st, 16), l0, self._flags, self._ws, self._ws_bytes, _stream(stream, self.device)))
         return out, lse

@@ -15,3 +15,19 @@ def test_a_new_page_table_names_no_page():
     full = P.DMCFull(CFG, device="cpu")
     assert (full.page_table == -1).all()
     assert not full.lengths.any() and not full.flags.any()
+
+
+def _step(tokens, heads):
+    return torch.zeros(tokens, heads, D, dtype=BF)
+
+
+def test_append_takes_more_tokens_than_the_workspace_is_for():
+    """max_tokens is the attention's: append needs no workspace, so that the default object (one token per row) takes a
+    prompt too."""
+    full = P.DMCFull(CFG, device="cpu")
+    cu = torch.tensor([0, 9, 9, 20], dtype=I32)
+    k, v, q = _step(20, HKV), _step(20, HKV), _step(20, HQ)
+    assert full._quick_append(k, v, q, torch.empty_like(q), cu)[0] == 20
+    assert full._quick_append(k, v, None, None, cu)[0] == 20
+    with pytest.raises(P.DMCError, match="the workspace holds 3"):
+        full.attend(0, q, cu_seqlens=cu)

@@ -64,3 +64,15 @@ def test_calls_before_the_page_table_is_written_are_flagged(torch_cuda, packed):
     full.flags.zero_()
     full.attend(0, torch.ones(T, 4, 64, device="cuda").bfloat16(), cu_seqlens=cu)
     assert int(full.flags) == P.binding.DMC_FLAG_BAD_PAGE
+
+
+def test_a_prompt_enters_the_default_object(torch_cuda):
+    import paper_2403_09636_amd as P
+    full = P.DMCFull(P.make_full_config(1, 4, 2, 64, page_size=32, max_pages=3))
+    full.page_table.copy_(torch.tensor([[2, 0, 1]], dtype=torch.int32))
+    k, v = torch.randn(2, 77, 2, 64, device="cuda").bfloat16()
+    full.append(0, k, v, cu_seqlens=torch.tensor([0, 77], dtype=torch.int32, device="cuda"))
+    full.check()
+    for x, pool in ((k, full.k_pages), (v, full.v_pages)):
+        rows = pool[0, [2, 0, 1]].transpose(1, 2).reshape(96, 2, 64)[:77]
+        assert torch.equal(rows, x)
