@@ -893,6 +893,14 @@ def torch_empty_like(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+def _new_like(name, t):
+    """An output for a call that got none: contiguous, like the tensor t of this name."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        _fail(f"{name} must be a torch.Tensor")
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def make_train_config(batch, seq_len, num_q_heads, num_kv_heads, head_dim, dtype="bf16",
                       decision_bias=5.0, temperature=0.1, window=12, omega_src="lead") -> TrainConfig:
     """A dmc_train_config (defaults: the paper's c = 5, tau = 0.1, w = 12)."""
@@ -1073,8 +1081,8 @@ class DMCRotation:
         return T, q0, k0, pos, x0, y0, call.strides(a[1], a[2], b[1], b[2], x[1], x[2], y[1], y[2])
 
     def _rotate(self, q, k, positions, q_out, k_out, inverse, stream):
-        q_out = torch_empty_like(q) if q_out is None else q_out
-        k_out = torch_empty_like(k) if k_out is None else k_out
+        q_out = _new_like("q", q) if q_out is None else q_out
+        k_out = _new_like("k", k) if k_out is None else k_out
         args = self._quick(q, k, positions, q_out, k_out)
         if args is None:
             check_rotary_args(self.cfg, self.device, q, k, positions, self.inv_freq, q_out, k_out)
@@ -1241,7 +1249,7 @@ class DMCFull:
         row, or with cu_seqlens int32 [batch + 1] row b's being the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1.
         With q [T, Hq, d], returns q_out, the queries turned likewise (q_out may be q itself)."""
         if q is not None and q_out is None:
-            q_out = torch_empty_like(q)
+            q_out = _new_like("q", q)
         kp, vp = self._pages(layer)
         args = self._quick_append(k, v, q, q_out, cu_seqlens)
         if args is None:
@@ -1260,6 +1268,8 @@ class DMCFull:
         rows' caches up to themselves; at most max_chunk (default: the object's) of them in a row.  Returns (out
         [T, Hq, d], lse [T, Hq] fp32); rows of tokens outside every chunk stay as they are."""
         import torch
+        if not isinstance(q, torch.Tensor):
+            _fail("q must be a torch.Tensor")
         if out is None:
             out = torch_empty_like(q)
         if lse is None:

@@ -31,3 +31,31 @@ def test_append_takes_more_tokens_than_the_workspace_is_for():
     assert full._quick_append(k, v, None, None, cu)[0] == 20
     with pytest.raises(P.DMCError, match="the workspace holds 3"):
         full.attend(0, q, cu_seqlens=cu)
+
+
+def _told(fn, name):
+    with pytest.raises(P.DMCError) as e:
+        fn()
+    assert f"{name} must be a torch.Tensor" in str(e.value), str(e.value)
+
+
+@pytest.mark.parametrize("bad", [None, "q", 3.0, [1.0]])
+def test_what_is_no_tensor_is_named(bad):
+    """The checks' message, whether or not the outputs are the caller's."""
+    full = P.DMCFull(CFG, device="cpu")
+    rot = P.DMCRotation(P.make_rotary_config(HQ, HKV, D, rotary_dim=0), device="cpu")
+    q, k, lse, pos = _step(B, HQ), _step(B, HKV), torch.zeros(B, HQ), torch.zeros(B, dtype=I32)
+    _told(lambda: full.attend(0, bad), "q")
+    _told(lambda: full.attend(0, bad, out=q), "q")
+    _told(lambda: full.attend(0, bad, lse=lse), "q")
+    _told(lambda: full.attend(0, bad, out=q, lse=lse), "q")
+    _told(lambda: full.append(0, bad, k), "k")
+    _told(lambda: full.append(0, k, bad), "v")
+    if bad is not None:   # (None: no queries)
+        _told(lambda: full.append(0, k, k.clone(), q=bad), "q")
+        _told(lambda: full.append(0, k, k.clone(), q=bad, q_out=q), "q")
+    for fn in (rot.forward, rot.backward):
+        _told(lambda: fn(bad, k, pos), "q")
+        _told(lambda: fn(q, bad, pos), "k")
+        _told(lambda: fn(bad, k, pos, q.clone(), k.clone()), "q")
+        _told(lambda: fn(q, k, bad), "positions")
