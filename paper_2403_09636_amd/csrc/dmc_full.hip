@@ -252,17 +252,32 @@ __device__ __forceinline__ int range_of_block(int blocks) {
   return (blocks & 7) ? static_cast<int>(blockIdx.x) : (blockIdx.x & 7) * (blocks >> 3) + (blockIdx.x >> 3);
 }
 
-// Rows of out and lse of row b's tokens that are dropped (not in use, or full).
-template <int ES, int D>
-__device__ __forceinline__ void clear_dropped(const FullParams &p, const FullRow &r) {
-  const int first = min(r.m, r.given), items = (r.given - first) * p.hq;
-  constexpr int VPR = D * ES / 16;
-  for (int64_t i = threadIdx.x; i < int64_t(items) * VPR; i += kThreads) {
-    const int64_t x = i / VPR, t = r.start + first + x / p.hq, h = x % p.hq;
-    st16(static_cast<char *>(p.out) + (t * p.os[0] + h * p.os[1]) * ES + (i % VPR) * 16, make_uint4(0, 0, 0, 0));
-    if (p.lse && i % VPR == 0) p.lse[t * p.hq + h] = neg_inf();
+// Rows of out and lse of tokens that are dropped (their row is not in use, or full): `dropped`
+// tokens from `first` on, a token and head at a time, shared out among `parts` workgroups of
+// which this is number `part`; LANES threads of each take part, this one being `lane`.
+// 8192 tokens of 64 heads: 24.7 us, by one workgroup 5225; 4 rows of 512 tokens on 4000, one of
+// them not in use: 255.5 us (as with one token in that row), by one workgroup 578.
+template <int ES, int D, int LANES>
+__device__ __forceinline__ void clear_dropped(const FullParams &p, int first, int dropped, uint32_t part, uint32_t parts,
+                                              uint32_t lane) {
+  constexpr int VPR = D * ES / 16, STEP = LANES / VPR;   // vectors of a row; rows of a workgroup at a time
+  const uint32_t items = uint32_t(dropped) * p.hq;       // (up to 2^30)
+  for (uint32_t x = part * STEP + lane / VPR; x < items; x += parts * STEP) {
+    const uint32_t i = x / uint32_t(p.hq), h = x - i * p.hq, v = lane % VPR;
+    const int64_t t = int64_t(first) + i;
+    st16(static_cast<char *>(p.out) + (t * p.os[0] + h * p.os[1]) * ES + v * 16, make_uint4(0, 0, 0, 0));
+    if (p.lse && v == 0) p.lse[t * p.hq + h] = neg_inf();
   }
 }
+// The part that this workgroup takes of row b's dropped tokens, where all of them share these.
+__device__ __forceinline__ uint32_t part_of_row(int b) { return (blockIdx.x + gridDim.x - b % gridDim.x) % gridDim.x; }
+// Dropped items (tokens times heads) of a row up to which one workgroup alone writes them.
+// In batches of up to 64 rows every workgroup knows the rows, and takes a few cycles for each
+// one that is shared (32 of 64 rows not in use, 64 heads: steps 41.1 us, shared 44.1; 4 tokens
+// a row 43.3, shared 46.6; 8 tokens 47.5 and 50.2).  In larger ones it has to look for those
+// with more (200 rows, one with 200, 600 and 2000 dropped tokens of 8 heads: alone 27.8, 61.6
+// and 184 us, shared 28.3, 28.3 and 28.4; 4096 rows: 218 us without such a row, 231 with one).
+constexpr int kAloneFew = 512, kAloneMany = 2048;
 
 // A page id of the table, page 0 where the table names none.
 __device__ __forceinline__ int checked_page(const FullParams &p, int page) {
@@ -349,6 +364,7 @@ struct RowPlace {
 struct SpaceLds {
   RowPlace rows[kWaves][64];
   int64_t sums[kWaves];
+  int32_t many[kWaves];
 };
 template <int ES, int D, bool TRI, int LEAST>   // LEAST: fewest keys of a piece
 struct Space {
@@ -398,11 +414,19 @@ struct Space {
       all = uniform(__shfl(x, 63, 64));
       places[lane] = RowPlace{x - share, row.start, row.n, m, pieces};
       wave_lds_sync();
-      unsigned long long dropped = __ballot(lane < p.rows && row.m < row.given);
+      const int items = (row.given - row.m) * p.hq;   // dropped (0 in lanes past the rows)
+      static_assert(kFullPlaces >= 64, "a workgroup for every row");
+      const unsigned long long alone = __ballot(items > 0 && items <= kAloneFew);
+      unsigned long long dropped = __ballot(items > kAloneFew);
+      if (blockIdx.x < 64 && (alone >> blockIdx.x & 1)) {
+        const FullRow r = load(blockIdx.x);
+        clear_dropped<ES, D, kThreads>(p, r.start + r.m, r.given - r.m, 0, 1, tid);
+      }
       while (dropped) {
         const int i = __ffsll(dropped) - 1;
         dropped &= dropped - 1;
-        if (i % grid == blockIdx.x) clear_dropped<ES, D>(p, load(i));
+        clear_dropped<ES, D, kThreads>(p, __builtin_amdgcn_readlane(row.start + row.m, i),
+                                       __builtin_amdgcn_readlane(row.given - row.m, i), part_of_row(i), grid, tid);
       }
       if (blockIdx.x == 0 && wave == 0 && lane < p.rows && p.flags) {
         const int32_t f = row_flags(p.cu, p.len, p.total, p.capacity, lane, p.max_chunk);
@@ -411,10 +435,12 @@ struct Space {
     } else {
       const int each = (p.rows + kThreads - 1) / kThreads, b0 = min(tid * each, p.rows), b1 = min(b0 + each, p.rows);
       int64_t own = 0;
+      bool many = false;   // a row with many dropped tokens
       for (int i = b0; i < b1; ++i) {
         prefix[i] = own;
         const FullRow r = load(i);
         const int m = min(r.m, p.max_chunk);
+        many |= (r.given - r.m) * p.hq > kAloneMany;
         if (m > 0) own += p.hkv * tiles(r.n, m).all();
         if (blockIdx.x == 0 && p.flags) {
           const int32_t f = row_flags(p.cu, p.len, p.total, p.capacity, i, p.max_chunk);
@@ -427,21 +453,39 @@ struct Space {
         const int64_t y = __shfl_up(x, o, 64);
         if (lane >= o) x += y;
       }
-      if (lane == 63) lds.sums[wave] = x;
+      many = __any(many);
+      if (lane == 63) {
+        lds.sums[wave] = x;
+        lds.many[wave] = many;
+      }
       __syncthreads();
       int64_t first = x - own;
       all = 0;
+      many = false;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
         if (i < wave) first += lds.sums[i];
         all += lds.sums[i];
+        many |= lds.many[i] != 0;
       }
       for (int i = b0; i < b1; ++i) prefix[i] += first;
       if (tid == 0) prefix[p.rows] = all;
       __syncthreads();
       for (int i = blockIdx.x; i < p.rows; i += grid) {
         const FullRow r = load(i);
-        if (r.m < r.given) clear_dropped<ES, D>(p, r);
+        if (r.m < r.given && (r.given - r.m) * p.hq <= kAloneMany)
+          clear_dropped<ES, D, kThreads>(p, r.start + r.m, r.given - r.m, 0, 1, tid);
+      }
+      for (int base = wave * 64; many && base < p.rows; base += kThreads) {   // each wave for itself
+        FullRow r{0, 0, 0, 0};
+        if (base + lane < p.rows) r = load(base + lane);
+        unsigned long long dropped = __ballot((r.given - r.m) * p.hq > kAloneMany);
+        while (dropped) {
+          const int i = __ffsll(dropped) - 1;
+          dropped &= dropped - 1;
+          clear_dropped<ES, D, 64>(p, __builtin_amdgcn_readlane(r.start + r.m, i), __builtin_amdgcn_readlane(r.given - r.m, i),
+                                   part_of_row(base + i), grid, lane);
+        }
       }
     }
     all = uniform(all);
