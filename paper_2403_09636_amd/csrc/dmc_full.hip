@@ -719,7 +719,8 @@ struct Cuts {
 // stores have arrived before the barrier lets it through (vmcnt 0), and the last
 // workgroup to count reads only after it has counted; it leaves the counter at 0.
 // Counting at the end of the range, not after each piece, keeps the wait out of the
-// stream of keys.  More than kJoin pieces are joined in groups of kJoin first, so
+// stream of keys.  Only tiles of 16 and 32 columns are joined so (JOIN); wider ones always
+// take two launches.  More than kJoin pieces are joined in groups of kJoin first, so
 // that no workgroup reads more than a few dozen records (a row of 100000 keys, 8/1 heads:
 // groups of 8 36.2 us, 16 30.5, 32 31.6; 30000, 64/8 heads: 33.7, 34.6, 38.2).  Counters: one per record for
 // the groups that start with it, one per range for the unit that starts in it.
@@ -729,10 +730,9 @@ __device__ __forceinline__ int count_up(int32_t *counter, int count) {
   if (before == count - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return before == count - 1;
 }
-template <int ES, int D>
+template <int ES, int D, bool JOIN>
 __device__ __forceinline__ void join_cuts(const FullParams &p, Cuts &cuts, void *lds) {
-  float2 *w = static_cast<float2 *>(lds);
-  if (!p.one_launch) {
+  if (!JOIN || !p.one_launch) {
     if (threadIdx.x == 0) {
       Piece *unit = p.cut_units + range_of_block(gridDim.x);   // the one that starts here and goes on
       if (cuts.n > 0 && cuts.piece[cuts.n - 1].index == 0) *unit = cuts.piece[cuts.n - 1];
@@ -740,36 +740,39 @@ __device__ __forceinline__ void join_cuts(const FullParams &p, Cuts &cuts, void 
     }
     return;
   }
-  wait_vmcnt<0>();
-  __syncthreads();
-  const int n = uniform(cuts.n);
-  if (n == 0) return;
-  auto unit_counter = [&](const Piece &x) { return p.counters + 2 * p.places + x.first; };
-  if (threadIdx.x < n) {
-    const Piece &x = cuts.piece[threadIdx.x];
-    const int from = x.index / kJoin * kJoin;
-    cuts.last[threadIdx.x] = x.pieces > kJoin ? count_up(p.counters + record_index(x.first, from), min(kJoin, x.pieces - from))
-                                              : count_up(unit_counter(x), x.pieces);
-  }
-  __syncthreads();
-  for (int i = 0; i < n; ++i) {
-    if (!uniform(cuts.last[i])) continue;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    const Piece x = cuts.piece[i];
-    if (x.pieces <= kJoin) {
-      join_records<ES, D, 4>(p, x, 0, x.cols, 0, 1, x.pieces, true, w);
-      continue;
-    }
-    const int from = x.index / kJoin * kJoin, groups = (x.pieces + kJoin - 1) / kJoin;
-    const int members = min(kJoin, x.pieces - from);
-    if (members > 1) join_records<ES, D, 4>(p, x, 0, x.cols, from, 1, members, false, w);
+  if constexpr (JOIN) {
+    float2 *w = static_cast<float2 *>(lds);
     wait_vmcnt<0>();
     __syncthreads();
-    if (threadIdx.x == 0) cuts.last[i] = count_up(unit_counter(x), groups);
+    const int n = uniform(cuts.n);
+    if (n == 0) return;
+    auto unit_counter = [&](const Piece &x) { return p.counters + 2 * p.places + x.first; };
+    if (threadIdx.x < n) {
+      const Piece &x = cuts.piece[threadIdx.x];
+      const int from = x.index / kJoin * kJoin;
+      cuts.last[threadIdx.x] = x.pieces > kJoin ? count_up(p.counters + record_index(x.first, from), min(kJoin, x.pieces - from))
+                                                : count_up(unit_counter(x), x.pieces);
+    }
     __syncthreads();
-    if (!uniform(cuts.last[i])) continue;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    join_records<ES, D, 4>(p, x, 0, x.cols, 0, kJoin, groups, true, w);
+    for (int i = 0; i < n; ++i) {
+      if (!uniform(cuts.last[i])) continue;
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+      const Piece x = cuts.piece[i];
+      if (x.pieces <= kJoin) {
+        join_records<ES, D, 4>(p, x, 0, x.cols, 0, 1, x.pieces, true, w);
+        continue;
+      }
+      const int from = x.index / kJoin * kJoin, groups = (x.pieces + kJoin - 1) / kJoin;
+      const int members = min(kJoin, x.pieces - from);
+      if (members > 1) join_records<ES, D, 4>(p, x, 0, x.cols, from, 1, members, false, w);
+      wait_vmcnt<0>();
+      __syncthreads();
+      if (threadIdx.x == 0) cuts.last[i] = count_up(unit_counter(x), groups);
+      __syncthreads();
+      if (!uniform(cuts.last[i])) continue;
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+      join_records<ES, D, 4>(p, x, 0, x.cols, 0, kJoin, groups, true, w);
+    }
   }
 }
 
@@ -989,7 +992,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
   extern __shared__ int64_t prefix[];
   __shared__ SpaceLds space_lds;
   __shared__ Cuts cuts;
-  __shared__ __align__(16) float area[SPLIT_KEYS ? kWaves : 2][16][JS];
+  __shared__ __align__(16) float area[SPLIT_KEYS ? kWaves : 1][SPLIT_KEYS ? 16 : 1][JS];   // (all of SPLIT_KEYS)
   __shared__ float stat[kWaves][16][2];
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1243,16 +1246,17 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
             put(col, e0, mx[t], l, o);
           } else {
 #pragma unroll
-            for (int j = 0; j < E; j += 2) put2(p, rec + 2 * ((e0 + j) / 2 * COLS + col), o[j], o[j + 1]);
-            if (e0 == 0) put2(p, rec + COLS * D + 2 * col, mx[t], l);
+            for (int j = 0; j < E; j += 2)
+              *reinterpret_cast<float2 *>(rec + 2 * ((e0 + j) / 2 * COLS + col)) = make_float2(o[j], o[j + 1]);
+            if (e0 == 0) *reinterpret_cast<float2 *>(rec + COLS * D + 2 * col) = make_float2(mx[t], l);
           }
         }
       }
     }
     if (!whole && tid == 0) cuts.piece[cuts.n++] = x;
   }
-  static_assert(sizeof(area) >= kJoinPairs * sizeof(float2), "join area");
-  join_cuts<ES, D>(p, cuts, area);
+  static_assert(!SPLIT_KEYS || sizeof(area) >= kJoinPairs * sizeof(float2), "join area");
+  join_cuts<ES, D, SPLIT_KEYS>(p, cuts, area);
 }
 
 // ---------------------------------------------------------------------------
@@ -1505,7 +1509,6 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
         for (int i = 0; i < NTL; ++i)
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
-            // (wide tiles always take two launches: plain stores)
             typedef __attribute__((address_space(1))) uint64_t gpair;
             const char *row = uniform_ptr(reinterpret_cast<const char *>(rec) + (16 * i + 4 * (j >> 2) + (j & 3) / 2) * kWideCols * 8);
             *reinterpret_cast<gpair *>(reinterpret_cast<uintptr_t>(row) + at) =
@@ -1516,8 +1519,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_wide_kernel(FullParams p) {
     }
     if (!whole && tid == 0) cuts.piece[cuts.n++] = x;
   }
-  static_assert(sizeof(ring0) >= kJoinPairs * sizeof(float2), "join area");
-  join_cuts<2, D>(p, cuts, ring0);
+  join_cuts<2, D, false>(p, cuts, nullptr);
 }
 
 template <int ES, int D, int NT, bool SPLIT_KEYS>
@@ -1543,6 +1545,7 @@ hipError_t launch_rotation(const RotateParams &p, bool paged, hipStream_t s) {
 
 template <int ES, int D>
 hipError_t attend(const FullParams &p, hipStream_t s) {
+  if (p.one_launch && p.tile_cols > (ES == 2 ? 32 : 16)) return hipErrorInvalidValue;   // (only narrow tiles join)
   const size_t lds = p.rows <= 64 ? 0 : (size_t(p.rows) + 1) * sizeof(int64_t);   // the sums before every row
   if constexpr (ES == 2) {
     if (p.tile_cols == kWideCols) hipLaunchKernelGGL((full_wide_kernel<D>), dim3(p.places), dim3(kThreads), lds, s, p);
