@@ -56,8 +56,8 @@ constexpr int kFullPlaces = 512;
 // Query columns of a tile: 16 or 32 (bf16) that all waves of a workgroup share; wider
 // ones, of whole tokens, once a row has more: 128 (bf16) or 64 (fp32).  Drafts of 4
 // tokens, 64/8 heads, 16 rows of up to 8192 keys: 69.5 us with 32 columns, 83.0 with 16,
-// 91.7 with 128; fp32 chunks of 64 tokens on 8000, 8/4 heads of 128: 190 us with 64
-// columns, 290 with 16.
+// 91.7 with 128; fp32 chunks of 64 tokens on 8000, 8 rows of 8/4 heads of 128 (109 us at a
+// large fp32 product's rate): 190 us with 64 columns, 290 with 16.
 constexpr inline int full_tile_cols(int elem_bytes, int64_t max_chunk, int group) {
   const int64_t cols = max_chunk * group;
   if (elem_bytes == 4) return cols <= 16 || group > 64 ? 16 : 64;

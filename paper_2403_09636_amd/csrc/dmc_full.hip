@@ -72,7 +72,7 @@ __device__ __forceinline__ int row_of_token(const int32_t *cu, int rows, int tot
 // token's units.  Bound by HBM, each element read and written once: 6 sequences of up to
 // 4096 tokens, 32 + 32 heads of 128 in bf16, take 87 us (5.9 TB/s of reads and writes), in
 // append 148.  Four tokens to a workgroup: 102 and 157 us; four units of a thread in flight
-// at once, with fewer waves: 2048 tokens 28.6 us against 24.7.  The rotation's stores
+// at once, with fewer waves (not taken): 2048 tokens 28.6 us against 24.7.  The rotation's stores
 // stream (without: 91 us; the causal attention that reads them next takes the same time
 // after either), the append's do not (with: 157 us).
 // ---------------------------------------------------------------------------
@@ -414,19 +414,21 @@ struct Space {
       all = uniform(__shfl(x, 63, 64));
       places[lane] = RowPlace{x - share, row.start, row.n, m, pieces};
       wave_lds_sync();
-      const int items = (row.given - row.m) * p.hq;   // dropped (0 in lanes past the rows)
-      static_assert(kFullPlaces >= 64, "a workgroup for every row");
-      const unsigned long long alone = __ballot(items > 0 && items <= kAloneFew);
-      unsigned long long dropped = __ballot(items > kAloneFew);
-      if (blockIdx.x < 64 && (alone >> blockIdx.x & 1)) {
-        const FullRow r = load(blockIdx.x);
-        clear_dropped<ES, D, kThreads>(p, r.start + r.m, r.given - r.m, 0, 1, tid);
-      }
-      while (dropped) {
-        const int i = __ffsll(dropped) - 1;
-        dropped &= dropped - 1;
-        clear_dropped<ES, D, kThreads>(p, __builtin_amdgcn_readlane(row.start + row.m, i),
-                                       __builtin_amdgcn_readlane(row.given - row.m, i), part_of_row(i), grid, tid);
+      if (__any(row.m < row.given)) {   // (never in lanes past the rows)
+        const int items = (row.given - row.m) * p.hq;
+        static_assert(kFullPlaces >= 64, "a workgroup for every row");
+        const unsigned long long alone = __ballot(items > 0 && items <= kAloneFew);
+        unsigned long long dropped = __ballot(items > kAloneFew);
+        if (blockIdx.x < 64 && (alone >> blockIdx.x & 1)) {
+          const FullRow r = load(blockIdx.x);
+          clear_dropped<ES, D, kThreads>(p, r.start + r.m, r.given - r.m, 0, 1, tid);
+        }
+        while (dropped) {
+          const int i = __ffsll(dropped) - 1;
+          dropped &= dropped - 1;
+          clear_dropped<ES, D, kThreads>(p, __builtin_amdgcn_readlane(row.start + row.m, i),
+                                         __builtin_amdgcn_readlane(row.given - row.m, i), part_of_row(i), grid, tid);
+        }
       }
       if (blockIdx.x == 0 && wave == 0 && lane < p.rows && p.flags) {
         const int32_t f = row_flags(p.cu, p.len, p.total, p.capacity, lane, p.max_chunk);
@@ -1263,7 +1265,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
 // Wide tiles (128 columns, bf16): pieces of prompts, turns, long drafts.  Bound by
 // the matrix cores and the vector work of the softmax beside them (busy 49 % and 44 % of
 // the cycles, which share the issue slots): 4 rows of 512 tokens on 12000, 64/8 heads,
-// take 855 to 910 us, 900 to 960 TFLOP/s, 80 % of a large product's.  One workgroup =
+// take 855 to 925 us (cards differ), 890 to 960 TFLOP/s, 77 to 84 % of a large product's.  One workgroup =
 // 4 waves, a wave owning 32 columns (lane l: column l % 32, half l / 32), so that
 // all heads of a kv head's group share its keys.  Keys and values stream through LDS
 // in blocks of 32 (direct global -> LDS transfers, a ring of four blocks, three
@@ -1532,9 +1534,11 @@ void launch_narrow(const FullParams &p, size_t lds, hipStream_t s) {
 
 template <int ES, int D>
 hipError_t launch_rotation(const RotateParams &p, bool paged, hipStream_t s) {
-  // Few tokens: the heads of each shared out to workgroups of 256 units, so that the
-  // chip is filled (1024 tokens of 48 heads: 9.8 us for both; 2048: 13.3 us shared, 12.4
-  // not, with four units in flight; a decode step of 32 rows: 4.3 us).
+  // Few tokens: the heads of each shared out to workgroups of 256 units, so that the chip is
+  // filled (32 + 32 heads of 128 in bf16: 32 tokens 2.9 us, in one workgroup each 3.6; 512 4.0
+  // and 4.5; 1024 5.1 and 5.2). Many: one workgroup forms a token's angles once (2048: 10.6 us,
+  // shared 10.8; what sharing gains beyond, 3 % at 8192 and 1 % at 14000, is not taken: it
+  // would multiply the workgroups of the largest launches).
   const int units = (p.hq + (paged ? 2 : 1) * p.hkv) * (D * ES / 32);
   const int shares = int64_t(units) * p.total < int64_t(2048) * kThreads ? (units + kThreads - 1) / kThreads : 1;
   const dim3 grid(p.total + (paged ? 1 : 0), shares);
