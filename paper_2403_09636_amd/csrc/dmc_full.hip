@@ -70,7 +70,7 @@ __device__ __forceinline__ int row_of_token(const int32_t *cu, int rows, int tot
 // uses from LDS; then each thread moves units of two 16-byte vectors of a head, the
 // two halves of 16 / ES pairs (or 16 / ES adjacent pairs), in grid.y shares of the
 // token's units.  Bound by HBM, each element read and written once: 6 sequences of up to
-// 4096 tokens, 32 + 32 heads of 128 in bf16, take 87 us (5.9 TB/s of reads and writes), in
+// 4096 tokens, 32 + 32 heads of 128 in bf16, take 88 us (5.9 TB/s of reads and writes), in
 // append 148.  Four tokens to a workgroup: 102 and 157 us; four units of a thread in flight
 // at once, with fewer waves (not taken): 2048 tokens 28.6 us against 24.7.  The rotation's stores
 // stream (without: 91 us; the causal attention that reads them next takes the same time
@@ -795,7 +795,7 @@ __global__ __launch_bounds__(kThreads) void full_join_kernel(FullParams p, int s
 // Bound by HBM: keys and values go from memory straight into the operands of the
 // 16x16 matrix instructions, without LDS (each is used by one wave only).  48 rows of
 // 4095 keys, 32 heads of 128: 483 us, 6.7 TB/s; 16 rows of up to 24000, 64/8 heads: 144
-// us, 6.2 TB/s.  Short rows are bound by latency: one row of 900, 16/4 heads: 10.5 us.
+// us, 6.2 TB/s.  Short rows are bound by latency: one row of 900, 16/4 heads: 10.8 us.
 // Blocks of 16 U keys; with lane l = 16 g +
 // c (g < 4, c < 16):
 //   S[key][col] = K Q^T: lane rows are keys 16 u + c, and its slices of the head dim
@@ -1263,7 +1263,7 @@ __global__ __launch_bounds__(kThreads, 2) void full_narrow_kernel(FullParams p) 
 
 // ---------------------------------------------------------------------------
 // Wide tiles (128 columns, bf16): pieces of prompts, turns, long drafts.  Bound by
-// the matrix cores and the vector work of the softmax beside them (busy 49 % and 44 % of
+// the matrix cores and the vector work of the softmax beside them (busy 48 % and 43 % of
 // the cycles, which share the issue slots): 4 rows of 512 tokens on 12000, 64/8 heads,
 // take 855 to 925 us (cards differ), 890 to 960 TFLOP/s, 77 to 84 % of a large product's.  One workgroup =
 // 4 waves, a wave owning 32 columns (lane l: column l % 32, half l / 32), so that
